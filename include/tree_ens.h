@@ -234,6 +234,145 @@ int tree_ens_predict_topk(const tree_ens_t *h, void *stream, const float *X, int
                           int32_t k, float *scores, int32_t *top_idx, float *top_scores);
 
 /*
+ * Learning from scores. A prompt's sampled answers are a query's candidates: the ensemble scores
+ * them (Section 6 reranks them), and the model that wrote them is trained on the scores. The
+ * functions below need no handle. They enqueue on `stream` and return without waiting; device
+ * pointers belong to the device that is current on the calling thread, as `stream` does. None
+ * allocates memory or keeps any between calls, so all may be captured into a HIP graph: what they
+ * need beside their outputs is a `workspace` of the caller's, of at least the bytes the
+ * ..._workspace function of the same sizes gives (0: it may be NULL), 16-byte aligned, whose
+ * contents need not be set before a call and mean nothing after it. Calls that may overlap in time
+ * need workspaces of their own. Equal inputs give equal bits.
+ *
+ * Tokens are packed: sequence s (an answer) owns tokens [seq_offsets[s], seq_offsets[s+1]) and
+ * group g (a prompt) owns sequences [group_offsets[g], group_offsets[g+1]), as in tree_ens_topk.
+ * Offsets are clamped into the range of what they index, so ill-formed ones never read or write
+ * outside it; results are defined for offsets that do not decrease. Tokens outside every sequence
+ * get a zero gradient, sequences outside every group take no part in its loss.
+ */
+
+/* types of logits */
+#define TREE_ENS_F32 0
+#define TREE_ENS_BF16 1
+#define TREE_ENS_F16 2
+
+/* flags of the functions below */
+#define TREE_ENS_SEQ_MEAN 1u    /* a sequence counts with the mean over its tokens, not the sum */
+#define TREE_ENS_CENTER_ONLY 2u /* advantages are not divided by the standard deviation */
+
+/*
+ * tree_ens_token_logp -- log-probabilities of given tokens under softmax(scale * logits).
+ *
+ *   logits      device, [n_tokens] rows of n_vocab values of type `dtype`, row_stride elements
+ *               apart (>= n_vocab; rows need no alignment beyond the type's).
+ *   dtype       TREE_ENS_F32, TREE_ENS_BF16 or TREE_ENS_F16; sums are held in 32 bits.
+ *   n_vocab     1 .. INT32_MAX.
+ *   targets     device, int64 [n_tokens]: the token of each row. One outside [0, n_vocab) marks a
+ *               row that does not count: its logits are not read, its outputs are 0.
+ *   scale       finite, > 0: the inverse of the sampling temperature.
+ *   logp        device, float [n_tokens]: log softmax(scale * row)[target].
+ *   entropy     device, float [n_tokens], or NULL: entropy of the row's distribution (nats).
+ *   stats       device, float [n_tokens][2], 8-byte aligned, or NULL: the row's largest logit m and
+ *               log sum exp(scale * (x - m)), for tree_ens_token_logp_backward.
+ * Logits of -inf are tokens that cannot be sampled. A row of nothing else has no distribution: its
+ * logp is -inf, its entropy 0, its stats (-inf, 0) and its gradient 0. A NaN or +inf in a row makes
+ * its logp, entropy and gradient NaN.
+ */
+int tree_ens_token_logp(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
+                        int64_t n_vocab, int64_t row_stride, const int64_t *targets, float scale,
+                        float *logp, float *entropy, float *stats, void *workspace,
+                        int64_t workspace_bytes);
+int tree_ens_token_logp_workspace(int32_t dtype, int64_t n_tokens, int64_t n_vocab, int64_t *bytes);
+
+/*
+ * tree_ens_token_logp_backward -- the gradient of sum(grad_logp * logp + grad_entropy * entropy)
+ * with respect to the logits: scale * (grad_logp * ([v == target] - p_v)
+ *                                      - grad_entropy * p_v * (log p_v + entropy)).
+ *
+ *   logits .. scale  as for tree_ens_token_logp, with its stats (float [n_tokens][2]).
+ *   grad_logp        device, float [n_tokens].
+ *   entropy, grad_entropy  device, float [n_tokens] (the forward's entropy), or both NULL.
+ *   grad_logits      device, `dtype` [n_tokens] rows of n_vocab, grad_stride elements apart; every
+ *                    row is written, rounded once (to nearest). May be `logits` itself with the same
+ *                    stride; it may not overlap the logits otherwise (TREE_ENS_E_ARG).
+ * Rows that do not count, and rows whose gradients are both 0, receive zeros and are not read.
+ */
+int tree_ens_token_logp_backward(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
+                                 int64_t n_vocab, int64_t row_stride, const int64_t *targets,
+                                 float scale, const float *stats, const float *grad_logp,
+                                 const float *entropy, const float *grad_entropy,
+                                 void *grad_logits, int64_t grad_stride);
+
+/*
+ * tree_ens_preference_loss -- pairwise logistic loss over the pairs of a group's sequences that
+ * the scores order, on log ratios to a reference model, and its gradient. With
+ *   h_s = beta * (sum or mean over the sequence's counted tokens of logp - ref_logp),
+ * the loss of a group is the mean over its pairs (i, j) with scores[i] > scores[j] of
+ *   -(1 - smoothing) * log sigmoid(h_i - h_j) - smoothing * log sigmoid(h_j - h_i);
+ * groups of two sequences are pairs of a preferred and a rejected answer. Equal scores make no
+ * pair, nor does a NaN score.
+ *
+ *   logp        device, float [n_tokens].
+ *   ref_logp    device, float [n_tokens], or NULL (no reference: 0).
+ *   mask        device, uint8 [n_tokens], or NULL: tokens of mask 0 do not count and may hold
+ *               anything, infinities and NaN included; their gradient is 0.
+ *   n_tokens    >= 0; n_seqs, n_groups 0 .. INT32_MAX.
+ *   scores      device, float [n_seqs].
+ *   beta        finite; smoothing 0 <= .. < 1; grad_scale finite.
+ *   flags       0 or TREE_ENS_SEQ_MEAN.
+ *   loss        device, float [n_groups]; 0 for a group without a pair.
+ *   margins     device, float [n_seqs]: h (0 for a sequence without a counted token).
+ *   grad_logp   device, float [n_tokens], or NULL: the gradient of grad_scale * sum(loss).
+ */
+int tree_ens_preference_loss(void *stream, const float *logp, const float *ref_logp,
+                             const uint8_t *mask, int64_t n_tokens, const int64_t *seq_offsets,
+                             int64_t n_seqs, const float *scores, const int64_t *group_offsets,
+                             int64_t n_groups, float beta, float smoothing, float grad_scale,
+                             uint32_t flags, float *loss, float *margins, float *grad_logp,
+                             void *workspace, int64_t workspace_bytes);
+int tree_ens_preference_workspace(int64_t n_tokens, int64_t n_seqs, int64_t n_groups,
+                                  int64_t *bytes);
+
+/*
+ * tree_ens_group_advantage -- scores relative to their group: (s - mean) / (std + eps), with the
+ * group's mean and population standard deviation; s - mean with TREE_ENS_CENTER_ONLY.
+ *
+ *   scores      device, float [n_docs]; n_docs and n_groups 0 .. INT32_MAX.
+ *   eps         finite, > 0.
+ *   advantages  device, float [n_docs]; 0 for candidates outside every group. May be `scores`.
+ * A NaN or an infinity among a group's scores makes its advantages NaN.
+ */
+int tree_ens_group_advantage(void *stream, const float *scores, int64_t n_docs,
+                             const int64_t *group_offsets, int64_t n_groups, float eps,
+                             uint32_t flags, float *advantages);
+
+/*
+ * tree_ens_policy_loss -- clipped policy loss with a KL term, and its gradient. Per counted token
+ * of sequence s, with ratio = exp(logp - old_logp), q = ref_logp - logp and A = advantages[s]:
+ *   -min(ratio * A, clamp(ratio, 1 - clip_low, 1 + clip_high) * A) + kl_coef * (exp(q) - q - 1).
+ *
+ *   logp        device, float [n_tokens].
+ *   old_logp    device, float [n_tokens], or NULL (the policy that sampled is this one: ratio 1,
+ *               with its gradient).
+ *   ref_logp    device, float [n_tokens], or NULL (kl_coef must be 0 then, and kl is set to 0).
+ *   mask        as for tree_ens_preference_loss.
+ *   advantages  device, float [n_seqs].
+ *   clip_low    0 <= .. <= 1; clip_high >= 0; kl_coef and grad_scale finite.
+ *   flags       0 or TREE_ENS_SEQ_MEAN.
+ *   loss        device, float [n_seqs]: sum or mean over the sequence's counted tokens (0 if none).
+ *   kl          device, float [n_seqs], or NULL: the same of exp(q) - q - 1.
+ *   grad_logp   device, float [n_tokens], or NULL: the gradient of grad_scale * sum(loss). A ratio
+ *               exactly on the clip's edge counts as inside.
+ */
+int tree_ens_policy_loss(void *stream, const float *logp, const float *old_logp,
+                         const float *ref_logp, const uint8_t *mask, int64_t n_tokens,
+                         const int64_t *seq_offsets, int64_t n_seqs, const float *advantages,
+                         float clip_low, float clip_high, float kl_coef, float grad_scale,
+                         uint32_t flags, float *loss, float *kl, float *grad_logp,
+                         void *workspace, int64_t workspace_bytes);
+int tree_ens_policy_workspace(int64_t n_tokens, int64_t n_seqs, int64_t *bytes);
+
+/*
  * tree_ens_info -- facts about a packed model; every output pointer may be NULL.
  *   n_trees        number of trees.
  *   min_features   1 + the largest feature id any node reads (0 if there is none).

@@ -29,6 +29,9 @@ TREE_ENS_RIGHT_IF_GT = 1
 (TREE_ENS_PATH_NONE, TREE_ENS_PATH_WALK, TREE_ENS_PATH_UNIFORM, TREE_ENS_PATH_TERMINAL, TREE_ENS_PATH_ROWS,
  TREE_ENS_PATH_CODEGEN) = range(6)
 TREE_ENS_CODEGEN = 2  # also compile a kernel specialised for the model (hiprtc)
+TREE_ENS_F32, TREE_ENS_BF16, TREE_ENS_F16 = range(3)  # types of logits
+TREE_ENS_SEQ_MEAN = 1  # a sequence counts with the mean over its tokens, not the sum
+TREE_ENS_CENTER_ONLY = 2  # advantages are not divided by the standard deviation
 
 _CODE_NAMES = {0: "OK", -1: "E_ARG", -2: "E_MODEL", -3: "E_SHAPE", -4: "E_DEVICE", -5: "E_NOMEM"}
 
@@ -90,6 +93,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.tree_ens_predict_topk.argtypes = [P, P, P, i64, i32, P, i64, i32, P, P, P]
     lib.tree_ens_info.restype = ctypes.c_int
     lib.tree_ens_info.argtypes = [P, P, P, P, P, P, P]
+    f32 = ctypes.c_float
+    for name, args in {
+            "tree_ens_token_logp": [P, P, i32, i64, i64, i64, P, f32, P, P, P, P, i64],
+            "tree_ens_token_logp_workspace": [i32, i64, i64, P],
+            "tree_ens_token_logp_backward": [P, P, i32, i64, i64, i64, P, f32, P, P, P, P, P, i64],
+            "tree_ens_preference_loss": [P, P, P, P, i64, P, i64, P, P, i64, f32, f32, f32, u32, P, P, P, P, i64],
+            "tree_ens_preference_workspace": [i64, i64, i64, P],
+            "tree_ens_group_advantage": [P, P, i64, P, i64, f32, u32, P],
+            "tree_ens_policy_loss": [P, P, P, P, P, i64, P, i64, P, f32, f32, f32, f32, u32, P, P, P, P, i64],
+            "tree_ens_policy_workspace": [i64, i64, P]}.items():
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = ctypes.c_int, args
     lib.tree_ens_destroy.restype = None
     lib.tree_ens_destroy.argtypes = [P]
     lib.tree_ens_last_error.restype = ctypes.c_char_p
@@ -358,6 +373,206 @@ def tree_ens_predict_topk(h, X, group_offsets, k: int, scores=None, top_idx=None
         top_idx.data_ptr() if n_groups else None, top_scores.data_ptr() if n_groups else None)
     _check(rc, "tree_ens_predict_topk")
     return scores, top_idx, top_scores
+
+
+# ----------------------------------------------------------------------------------------------
+# learning from scores
+# ----------------------------------------------------------------------------------------------
+def _vector(name, t, dtype, n, device):
+    """Check a contiguous device vector of n entries (any number if n is None) of a type."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dtype not in dtype or t.dim() != 1 or \
+            not t.is_contiguous() or (device is not None and t.device != device):
+        raise TypeError(f"{name} must be a contiguous {str(dtype[0])[6:]} vector on the device")
+    if n is not None and t.shape[0] != n:
+        raise TypeError(f"{name} must have {n} entries, not {t.shape[0]}")
+    return t
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None and t.numel() else None
+
+
+class _Launch:
+    """One call's device and stream: memory it allocates belongs to the stream the work runs on."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.device = device
+        self.guards = []
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device)
+        if stream is not None:
+            self.guards.append(torch.cuda.stream(stream))  # makes its device current too
+        elif torch.cuda.current_device() != device.index:
+            self.guards.append(torch.cuda.device(device))
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+    def empty(self, shape, dtype):
+        import torch
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def workspace(self, fn, *sizes):
+        import torch
+        need = ctypes.c_int64()
+        _check(getattr(load_library(), fn)(*sizes, ctypes.byref(need)), fn)
+        return self.empty(need.value, torch.uint8) if need.value else None
+
+    def call(self, fn, *args):
+        _check(getattr(load_library(), fn)(_stream_of(self, None), *args), fn)
+
+
+def _check_logits(logits, targets):
+    """(dtype code, n_tokens, n_vocab, row stride) of device logits [n_tokens, n_vocab]."""
+    import torch
+    codes = {torch.float32: TREE_ENS_F32, torch.bfloat16: TREE_ENS_BF16, torch.float16: TREE_ENS_F16}
+    if not isinstance(logits, torch.Tensor) or logits.device.type != "cuda" or logits.dtype not in codes or \
+            logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError("logits must be a CUDA (HIP) float32, bfloat16 or float16 [n_tokens, n_vocab] tensor with "
+                        "contiguous rows")
+    n, v = logits.shape
+    _vector("targets", targets, (torch.int64,), n, logits.device)
+    return codes[logits.dtype], n, v, logits.stride(0) if n > 1 else v
+
+
+def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool = False, logp=None, entropy=None,
+                        stats=None, stream=None):
+    """Log-probabilities of ``targets`` (device int64 [n_tokens]; outside [0, n_vocab): not counted) under
+    softmax(scale * logits): (logp float32 [n_tokens], entropy float32 [n_tokens] or None, stats float32
+    [n_tokens, 2] for the gradient). Rows of ``logits`` may lie any stride apart."""
+    import torch
+    code, n, v, stride = _check_logits(logits, targets)
+    f32, dev = (torch.float32,), logits.device
+    with _Launch(dev, stream) as on:
+        logp = on.empty(n, torch.float32) if logp is None else _vector("logp", logp, f32, n, dev)
+        if entropy is not None:
+            _vector("entropy", entropy, f32, n, dev)
+        elif want_entropy:
+            entropy = on.empty(n, torch.float32)
+        if stats is None:
+            stats = on.empty((n, 2), torch.float32)
+        elif stats.dtype != torch.float32 or stats.shape != (n, 2) or not stats.is_contiguous() or stats.device != dev:
+            raise TypeError("stats must be a contiguous float32 [n_tokens, 2] tensor on the logits' device")
+        work = on.workspace("tree_ens_token_logp_workspace", code, n, v)
+        on.call("tree_ens_token_logp", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale), _ptr(logp),
+                _ptr(entropy), _ptr(stats), _ptr(work), work.numel() if work is not None else 0)
+    return logp, entropy, stats
+
+
+def tree_ens_token_logp_backward(logits, targets, stats, grad_logp, scale: float = 1.0, entropy=None, grad_entropy=None,
+                                 grad_logits=None, stream=None):
+    """The gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to ``logits``, in their type
+    (``entropy`` as the forward gave it; both or neither). ``grad_logits`` may be ``logits`` itself."""
+    import torch
+    code, n, v, stride = _check_logits(logits, targets)
+    f32, dev = (torch.float32,), logits.device
+    if not isinstance(stats, torch.Tensor) or stats.dtype != torch.float32 or stats.shape != (n, 2) or \
+            not stats.is_contiguous() or stats.device != dev:
+        raise TypeError("stats must be the forward's float32 [n_tokens, 2] tensor")
+    _vector("grad_logp", grad_logp, f32, n, dev)
+    for name, t in (("entropy", entropy), ("grad_entropy", grad_entropy)):
+        if t is not None:
+            _vector(name, t, f32, n, dev)
+    if (entropy is None) != (grad_entropy is None):
+        raise TypeError("entropy and grad_entropy are given together")
+    if grad_logits is not None and (grad_logits.dtype != logits.dtype or grad_logits.shape != logits.shape or
+                                    (v > 1 and grad_logits.stride(1) != 1) or grad_logits.device != dev):
+        raise TypeError("grad_logits must be a tensor of the logits' type, shape and device with contiguous rows")
+    with _Launch(dev, stream) as on:
+        if grad_logits is None:
+            grad_logits = on.empty((n, v), logits.dtype)
+        on.call("tree_ens_token_logp_backward", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale),
+                _ptr(stats), _ptr(grad_logp), _ptr(entropy), _ptr(grad_entropy), _ptr(grad_logits),
+                grad_logits.stride(0) if n > 1 else v)
+    return grad_logits
+
+
+def _check_tokens(logp, seq_offsets, mask, **others):
+    """(n_tokens, n_seqs) of packed sequences; `others` are float vectors over the tokens, or None."""
+    import torch
+    _vector("logp", logp, (torch.float32,), None, None)
+    n, dev = logp.shape[0], logp.device
+    for name, t in others.items():
+        if t is not None:
+            _vector(name, t, (torch.float32,), n, dev)
+    if mask is not None:
+        _vector("mask", mask, (torch.bool, torch.uint8), n, dev)
+    _vector("seq_offsets", seq_offsets, (torch.int64,), None, dev)
+    if seq_offsets.shape[0] < 1:
+        raise TypeError("seq_offsets must have n_seqs + 1 entries")
+    return n, seq_offsets.shape[0] - 1
+
+
+def tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp=None, mask=None, beta: float = 0.1,
+                             smoothing: float = 0.0, grad_scale: float = 1.0, flags: int = 0, want_grad: bool = True,
+                             loss=None, margins=None, grad_logp=None, stream=None):
+    """Pairwise preference loss of each group's sequences, in the order of their ``scores``, on log ratios to a
+    reference model: (loss float32 [n_groups], margins float32 [n_seqs], gradient of grad_scale * loss.sum() with
+    respect to ``logp``, or None without ``want_grad``)."""
+    import torch
+    n, n_seqs = _check_tokens(logp, seq_offsets, mask, ref_logp=ref_logp, grad_logp=grad_logp)
+    f32, dev = (torch.float32,), logp.device
+    _vector("scores", scores, f32, n_seqs, dev)
+    n_groups = _check_offsets(group_offsets, dev)
+    with _Launch(dev, stream) as on:
+        loss = on.empty(n_groups, torch.float32) if loss is None else _vector("loss", loss, f32, n_groups, dev)
+        margins = on.empty(n_seqs, torch.float32) if margins is None else _vector("margins", margins, f32, n_seqs, dev)
+        if grad_logp is None and want_grad:
+            grad_logp = on.empty(n, torch.float32)
+        work = on.workspace("tree_ens_preference_workspace", n, n_seqs, n_groups)
+        on.call("tree_ens_preference_loss", _ptr(logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(), n_seqs,
+                _ptr(scores), group_offsets.data_ptr(), n_groups, float(beta), float(smoothing), float(grad_scale),
+                int(flags), _ptr(loss), _ptr(margins), _ptr(grad_logp), _ptr(work), work.numel() if work is not None else 0)
+    return loss, margins, grad_logp
+
+
+def tree_ens_group_advantage(scores, group_offsets, eps: float = 1e-6, flags: int = 0, advantages=None, stream=None):
+    """Scores relative to their group, (s - mean) / (std + eps): float32 [n_docs]."""
+    import torch
+    _vector("scores", scores, (torch.float32,), None, None)
+    n, dev = scores.shape[0], scores.device
+    n_groups = _check_offsets(group_offsets, dev)
+    with _Launch(dev, stream) as on:
+        if advantages is None:
+            advantages = on.empty(n, torch.float32)
+        else:
+            _vector("advantages", advantages, (torch.float32,), n, dev)
+        on.call("tree_ens_group_advantage", _ptr(scores), n, group_offsets.data_ptr(), n_groups, float(eps), int(flags),
+                _ptr(advantages))
+    return advantages
+
+
+def tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None, mask=None, clip_low: float = 0.2,
+                         clip_high: float = 0.2, kl_coef: float = 0.0, grad_scale: float = 1.0, flags: int = 0,
+                         want_grad: bool = True, loss=None, kl=None, grad_logp=None, stream=None):
+    """Clipped policy loss of each sequence with kl_coef times its KL estimate to a reference model: (loss float32
+    [n_seqs], kl float32 [n_seqs] or None without ``ref_logp``, gradient of grad_scale * loss.sum() with respect to
+    ``logp``, or None without ``want_grad``). ``old_logp`` None: the tokens were sampled by this very policy."""
+    import torch
+    n, n_seqs = _check_tokens(logp, seq_offsets, mask, old_logp=old_logp, ref_logp=ref_logp, grad_logp=grad_logp)
+    f32, dev = (torch.float32,), logp.device
+    _vector("advantages", advantages, f32, n_seqs, dev)
+    with _Launch(dev, stream) as on:
+        loss = on.empty(n_seqs, torch.float32) if loss is None else _vector("loss", loss, f32, n_seqs, dev)
+        if kl is not None:
+            _vector("kl", kl, f32, n_seqs, dev)
+        elif ref_logp is not None:
+            kl = on.empty(n_seqs, torch.float32)
+        if grad_logp is None and want_grad:
+            grad_logp = on.empty(n, torch.float32)
+        work = on.workspace("tree_ens_policy_workspace", n, n_seqs)
+        on.call("tree_ens_policy_loss", _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(),
+                n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef), float(grad_scale), int(flags),
+                _ptr(loss), _ptr(kl), _ptr(grad_logp), _ptr(work), work.numel() if work is not None else 0)
+    return loss, kl, grad_logp
 
 
 def tree_ens_info(h) -> dict:

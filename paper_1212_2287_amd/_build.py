@@ -22,7 +22,7 @@ HIP_FLAGS = [
 
 
 SCORE_MODES = 6  # modes of score.hip (score.hpp)
-HIP_SOURCES = ("tree_ens", "uniform", "term", "topk")
+HIP_SOURCES = ("tree_ens", "uniform", "term", "topk", "logp", "losses")
 
 
 def _hipcc() -> str:

@@ -1,0 +1,362 @@
+"""GPU preference loss, group advantages and policy loss through the C ABI, against the float64 oracle.
+
+Tolerances, with u = 2^-24: differences of log-probabilities are rounded once, exp and log1p are off by at most
+8u, sums are held in double and rounded once. A margin is off by u (sum of its terms + itself); a pair's loss and
+slope by the two margins' errors (both have slope <= 1) plus 16u."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import losses as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_1212_2287_amd as T
+    T.load_library()
+    return T
+
+
+def _dev(a):
+    import torch
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _close(got, want, tol, what):
+    got = got.double().cpu().numpy()
+    assert got.shape == np.shape(want), what
+    fine = np.isfinite(want)
+    assert np.array_equal(got[~fine], want[~fine], equal_nan=True), what
+    err = np.abs(got - want)[fine] / (np.broadcast_to(tol, np.shape(want))[fine] + 1e-37)
+    assert (err <= 1).all(), (what, float(err.max()), int(err.argmax()))
+
+
+# lengths of the sequences
+LENGTHS = {
+    "none": [], "one": [1], "empty": [0, 0, 0], "pair": [3, 2], "edges": [0, 1, 2, 63, 64, 65, 0, 127, 128, 129, 255, 256, 257, 0],
+    "short": list(np.random.default_rng(1).integers(0, 9, 700)), "mixed": list(np.random.default_rng(2).integers(1, 700, 300)),
+    "tile": [2047, 1, 2048, 2049, 4096, 3, 6145, 0, 5], "long": [100_003, 7, 0, 40_000], "single": [262_147],
+    "skewed": [1] * 500 + [90_001] + [2] * 500, "many": list(np.random.default_rng(3).integers(0, 40, 20_000)),
+    "ordinary": list(np.random.default_rng(4).integers(1, 1200, 2_000)),
+}
+
+
+def _tokens(name, seed=0, masked=True):
+    rng = np.random.default_rng([seed, len(name)])
+    lens = np.array(LENGTHS[name], np.int64)
+    seqs = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    n = int(seqs[-1])
+    lp = -rng.exponential(size=n).astype(np.float32)
+    ref = (lp + rng.normal(0, 0.3, n)).astype(np.float32)
+    mask = None
+    if masked:
+        mask = rng.random(n) < 0.7
+        for s in rng.integers(0, max(len(lens), 1), len(lens) // 10):  # sequences of which nothing counts
+            mask[seqs[s]:seqs[s + 1]] = False
+    return rng, seqs, lp, ref, mask
+
+
+def _groups(rng, n_seqs, sizes):
+    """Group offsets of the given sizes in turn, as many as there are sequences."""
+    ends = []
+    at = 0
+    while at < n_seqs:
+        at = min(n_seqs, at + int(sizes[len(ends) % len(sizes)]))
+        ends.append(at)
+    return np.concatenate([[0], ends]).astype(np.int64)
+
+
+def _check_preference(T, seqs, lp, ref, mask, scores, groups, beta, smoothing, grad_scale, mean, what):
+    flags = T.TREE_ENS_SEQ_MEAN if mean else 0
+    args = (_dev(lp), _dev(seqs), _dev(scores), _dev(groups))
+    more = dict(ref_logp=_dev(ref), mask=_dev(mask), beta=beta, smoothing=smoothing, grad_scale=grad_scale, flags=flags)
+    loss, h, grad = T.tree_ens_preference_loss(*args, **more)
+    beta, smoothing, grad_scale = (float(np.float32(v)) for v in (beta, smoothing, grad_scale))
+    want = O.preference_loss(lp, seqs, scores, groups, ref, mask, beta, smoothing, grad_scale, mean)
+    size = O.margins(np.abs(lp if ref is None else lp.astype(np.float64) - ref), seqs, None, mask, abs(beta), mean)[0]
+    tol_h = 2 * U * (size + np.abs(want[1]))
+    _close(h, want[1], tol_h, what + " margins")
+    tol_loss, tol_grad, w = np.zeros(len(groups) - 1), np.zeros(len(seqs) - 1), np.abs(O.margins(lp, seqs, ref, mask, beta, mean)[1])
+    for g, (a, b) in enumerate(zip(groups[:-1], groups[1:])):
+        s = scores[a:b]
+        pairs = max(int((s[:, None] > s[None, :]).sum()), 1)
+        worst, span = 2 * tol_h[a:b].max(initial=0), np.ptp(want[1][a:b]) if b > a else 0.0
+        each = worst + U * span + 16 * U
+        tol_loss[g] = each + 8 * U * want[0][g] + 2 * U * abs(smoothing) * span
+        met = (s[:, None] > s[None, :]).sum(1) + (s[:, None] < s[None, :]).sum(1)
+        tol_grad[a:b] = abs(grad_scale) * w[a:b] * met / pairs * (each + 8 * U)
+    _close(loss, want[0], tol_loss, what + " loss")
+    per_token = np.repeat(tol_grad, np.diff(seqs)) + 4 * U * np.abs(want[2])
+    _close(grad, want[2], per_token, what + " gradient")
+    only = T.tree_ens_preference_loss(*args, **more, want_grad=False)
+    assert only[2] is None and bool((only[0] == loss).all()) and bool((only[1] == h).all())
+    again = T.tree_ens_preference_loss(*args, **more)
+    assert all(bool((x == y).all()) for x, y in zip(again, (loss, h, grad)))
+
+
+@pytest.mark.parametrize("sizes", [[2], [1, 5, 0, 17, 64], [130, 7], [1500]])
+@pytest.mark.parametrize("name", [k for k in LENGTHS if k not in ("none",)])
+def test_preference_loss(T, name, sizes):
+    print("[preference]", name, sizes, flush=True)
+    for k, (mean, masked, smoothing) in enumerate([(False, True, 0.0), (True, False, 0.1), (True, True, 0.3)]):
+        rng, seqs, lp, ref, mask = _tokens(name, k, masked)
+        n_seqs = len(seqs) - 1
+        groups = _groups(rng, n_seqs, sizes)
+        scores = np.round(rng.normal(size=n_seqs) * 4).astype(np.float32) / 4  # equal scores among them
+        scores[rng.random(n_seqs) < 0.05] = np.nan
+        _check_preference(T, seqs, lp, ref if k else None, mask, scores, groups, 0.1 if k else 0.01, smoothing, 0.25, mean,
+                          f"{name} {sizes} {k}")
+
+
+def test_preference_loss_of_far_margins(T):
+    """Margins hundreds apart: losses of thousands one way, of next to nothing the other."""
+    lp = np.array([-1.0, -900.0, -2.0, -30.0, -0.5, -20.0], np.float32)
+    seqs = np.arange(7)
+    scores = np.array([1, 0, 0, 1, 2, 1], np.float32)
+    for beta in (1.0, 4.0):
+        _check_preference(T, seqs, lp, None, None, scores, np.array([0, 2, 4, 6]), beta, 0.0, 1.0, False, "far")
+
+
+def test_masked_tokens_may_hold_anything(T):
+    rng, seqs, lp, ref, mask = _tokens("mixed")
+    old = (lp - rng.normal(0, 0.05, len(lp))).astype(np.float32)
+    bad = [np.nan, np.inf, -np.inf]
+    dirty = [a.copy() for a in (lp, ref, old)]
+    for k, a in enumerate(dirty):
+        a[~mask] = np.resize(bad[k:] + bad[:k], int((~mask).sum()))
+    groups, n_seqs = _groups(rng, len(seqs) - 1, [9]), len(seqs) - 1
+    scores = rng.normal(size=n_seqs).astype(np.float32)
+    for mean in (0, T.TREE_ENS_SEQ_MEAN):
+        a, b = (T.tree_ens_preference_loss(_dev(x), _dev(seqs), _dev(scores), _dev(groups), ref_logp=_dev(y), mask=_dev(mask),
+                                           flags=mean) for x, y in ((lp, ref), dirty[:2]))
+        assert all(bool((x == y).all()) for x, y in zip(a, b))
+        a, b = (T.tree_ens_policy_loss(_dev(x), _dev(z), _dev(scores), _dev(seqs), ref_logp=_dev(y), mask=_dev(mask),
+                                       kl_coef=0.1, flags=mean) for x, y, z in ((lp, ref, old), dirty))
+        assert all(bool((x == y).all()) for x, y in zip(a, b))
+
+
+def _check_policy(T, seqs, lp, old, ref, mask, adv, low, high, kl_coef, grad_scale, mean, what):
+    args = (_dev(lp), _dev(old), _dev(adv), _dev(seqs))
+    more = dict(ref_logp=_dev(ref), mask=_dev(mask), clip_low=low, clip_high=high, kl_coef=kl_coef, grad_scale=grad_scale,
+                flags=T.TREE_ENS_SEQ_MEAN if mean else 0)
+    loss, kl, grad = T.tree_ens_policy_loss(*args, **more)
+    low, high = 1 - float(np.float32(1) - np.float32(low)), float(np.float32(1) + np.float32(high)) - 1
+    kl_coef, grad_scale = float(np.float32(kl_coef)), float(np.float32(grad_scale))
+    want = O.policy_loss(lp, old, adv, seqs, ref, mask, low, high, kl_coef, grad_scale, mean)
+    n = len(lp)
+    use = np.ones(n, bool) if mask is None else mask
+    d = np.zeros(n) if old is None else lp.astype(np.float64) - old
+    q = np.zeros(n) if ref is None else ref.astype(np.float64) - lp
+    A = np.abs(np.repeat(adv, np.diff(seqs))).astype(np.float64)
+    e_ratio = U * (8 + 2 * np.abs(d)) * np.exp(d)
+    e_kl = 16 * U * (np.expm1(q) - q) + U * np.abs(q * np.expm1(q)) + np.where(np.abs(q) >= 0.5, 8 * U * (np.exp(q) + np.abs(q)), 0)
+    e_up = e_kl + 4 * U * (np.abs(q) + np.abs(np.expm1(q)))
+
+    def total(v):
+        c = np.concatenate([[0.0], np.cumsum(np.where(use, v, 0.0))])
+        return c[seqs[1:]] - c[seqs[:-1]]
+    share = 1.0 / np.maximum(total(np.ones(n)), 1) if mean else np.ones(len(seqs) - 1)
+    gain = A * np.exp(np.abs(d))
+    _close(loss, want[0], share * total(A * e_ratio + 4 * U * gain + abs(kl_coef) * e_kl) + 4 * U * np.abs(want[0]), what + " loss")
+    if ref is None:
+        assert kl is None
+    else:
+        _close(kl, want[1], share * total(e_kl) + 4 * U * np.abs(want[1]), what + " kl")
+    per = abs(grad_scale) * np.repeat(share, np.diff(seqs)) * (A * e_ratio + abs(kl_coef) * e_up + 4 * U * (gain + np.abs(kl_coef * np.expm1(q))))
+    _close(grad, want[2], per, what + " gradient")
+    only = T.tree_ens_policy_loss(*args, **more, want_grad=False)
+    assert only[2] is None and bool((only[0] == loss).all())
+    again = T.tree_ens_policy_loss(*args, **more)
+    assert bool((again[0] == loss).all()) and bool((again[2] == grad).all())
+
+
+@pytest.mark.parametrize("name", list(LENGTHS))
+def test_policy_loss(T, name):
+    print("[policy]", name, flush=True)
+    for k, (mean, masked) in enumerate([(False, False), (True, True), (True, False), (False, True)]):
+        rng, seqs, lp, ref, mask = _tokens(name, k, masked)
+        n = len(lp)
+        r = rng.normal(0, 0.2, n)
+        for edge in (np.log(0.8), np.log(1.25)):  # the gradient jumps at a clip's edge
+            r = np.where(np.abs(r - edge) < 1e-3, edge + 2e-3, r)
+        old = (lp - r).astype(np.float32)
+        ref[rng.random(n) < 0.02] += 1.0
+        adv = rng.normal(size=len(seqs) - 1).astype(np.float32)
+        adv[rng.random(len(adv)) < 0.1] = 0.0
+        _check_policy(T, seqs, lp, old, ref if k != 2 else None, mask, adv, 0.2, 0.25, 0.05 if k != 2 else 0.0, 0.5, mean,
+                      f"{name} {k}")
+
+
+def test_policy_loss_on_the_edge_and_far_off(T):
+    """Ratios exactly 1 with a clip of nothing count as inside; ratios that overflow are clipped for a positive
+    advantage and for an advantage of 0; on-policy tokens have ratio 1."""
+    lp = np.array([-1.0, -1.0, 0.0, 0.0, -200.0, -0.5], np.float32)
+    old = np.array([-1.0, -1.0, -200.0, -200.0, 0.0, -0.5], np.float32)
+    seqs = np.arange(7)
+    adv = np.array([2.0, -2.0, 1.0, 0.0, -3.0, 0.0], np.float32)
+    _check_policy(T, seqs, lp, old, None, None, adv, 0.0, 0.0, 0.0, 1.0, False, "edge")
+    _check_policy(T, seqs, lp, None, lp - np.float32(0.125), None, adv, 0.2, 0.2, 0.5, 1.0, True, "on policy")
+    loss, _, grad = T.tree_ens_policy_loss(_dev(lp[2:3]), _dev(old[2:3]), _dev(np.array([-1.0], np.float32)), _dev(np.array([0, 1])))
+    assert float(loss) == np.inf and float(grad) == np.inf
+    loss, _, grad = T.tree_ens_policy_loss(_dev(np.array([np.nan], np.float32)), _dev(old[:1]), _dev(adv[:1]), _dev(np.array([0, 1])))
+    assert np.isnan(float(loss)) and np.isnan(float(grad))
+
+
+@pytest.mark.parametrize("sizes", [[1], [2], [16], [0, 1, 63, 64, 65, 200], [1025, 3], [5000], [70_000]])
+def test_group_advantage(T, sizes):
+    rng = np.random.default_rng(len(sizes))
+    n = max(3000, 2 * max(sizes))
+    groups = _groups(rng, n, sizes)
+    scores = (5 + 0.1 * rng.normal(size=n)).astype(np.float32)
+    scores[groups[1]:groups[2]] = 2.5  # a group without spread
+    for flags in (0, T.TREE_ENS_CENTER_ONLY):
+        got = T.tree_ens_group_advantage(_dev(scores), _dev(groups), eps=1e-3, flags=flags)
+        want = O.group_advantage(scores, groups, float(np.float32(1e-3)), bool(flags))
+        # the sums are double: the result is rounded once (twice if the mean is)
+        _close(got, want, 4 * U * np.abs(want) + 1e-12, f"{sizes} {flags}")
+    x = _dev(scores)
+    T.tree_ens_group_advantage(x, _dev(groups), eps=1e-3, flags=T.TREE_ENS_CENTER_ONLY, advantages=x)
+    assert bool((x == got).all())
+
+
+def test_group_advantage_of_special_scores(T):
+    scores = np.array([1.0, np.nan, 2.0, 1.0, np.inf, 3.0, 3.0, 7.0], np.float32)
+    got = T.tree_ens_group_advantage(_dev(scores), _dev(np.array([0, 3, 5, 7]))).cpu().numpy()
+    assert np.isnan(got[:5]).all() and got[5:].tolist() == [0.0, 0.0, 0.0]
+
+
+def test_ill_formed_offsets_stay_inside(T):
+    """Offsets beyond the tokens are clamped; tokens and sequences outside every segment get zeros."""
+    rng, _, lp, ref, _ = _tokens("mixed")
+    lp, ref = lp[:1000], ref[:1000]
+    seqs = np.array([100, 200, 450, 450, 2000, 2000])
+    groups = np.array([1, 3, 9])
+    scores = np.arange(5).astype(np.float32)
+    loss, h, grad = T.tree_ens_preference_loss(_dev(lp), _dev(seqs), _dev(scores), _dev(groups), ref_logp=_dev(ref))
+    want = O.preference_loss(lp, seqs, scores, groups, ref, beta=float(np.float32(0.1)))
+    _close(loss, want[0], 1e-5, "loss")
+    _close(h, want[1], 1e-4, "margins")
+    _close(grad, want[2], 1e-6, "gradient")
+    assert not bool(grad[:200].any())
+    adv = T.tree_ens_group_advantage(_dev(scores), _dev(groups))
+    assert float(adv[0]) == 0.0 and bool((adv[1:3] != 0).all())
+    pol = T.tree_ens_policy_loss(_dev(lp), None, _dev(scores), _dev(seqs))
+    _close(pol[2], O.policy_loss(lp, None, scores, seqs)[2], 1e-6, "policy gradient")
+    # offsets that decrease: whatever comes out, nothing outside is touched
+    odd = np.array([500, 20, 900, -7, 10**15, 3])
+    guard = _dev(np.full(1000 + 64, 7.0, np.float32))
+    T.tree_ens_policy_loss(_dev(lp), None, _dev(scores), _dev(odd), grad_logp=guard[32:1032])
+    T.tree_ens_preference_loss(_dev(lp), _dev(odd), _dev(scores), _dev(np.array([3, 0, 10**15, -2])), grad_logp=guard[32:1032])
+    assert bool((guard[:32] == 7).all()) and bool((guard[1032:] == 7).all())
+
+
+def test_nothing_to_learn_from(T):
+    import torch
+    none, zero = torch.empty(0, device="cuda"), _dev(np.zeros(1, np.int64))
+    loss, h, grad = T.tree_ens_preference_loss(none, zero, none, zero)
+    assert loss.numel() == h.numel() == grad.numel() == 0
+    tokens = torch.ones(300, device="cuda")
+    out = torch.full((300,), 5.0, device="cuda")
+    T.tree_ens_preference_loss(tokens, zero, none, zero, grad_logp=out)
+    assert not bool(out.any())
+    out.fill_(5.0)
+    T.tree_ens_policy_loss(tokens, None, none, zero, grad_logp=out)
+    assert not bool(out.any())
+    assert T.tree_ens_group_advantage(none, zero).numel() == 0
+    out.fill_(5.0)
+    T.tree_ens_group_advantage(tokens, zero, advantages=out)
+    assert not bool(out.any())
+    out.fill_(5.0)  # sequences, but no group: margins, and a gradient of zeros
+    _, h, _ = T.tree_ens_preference_loss(tokens, _dev(np.array([0, 100, 300])), _dev(np.ones(2, np.float32)), zero, beta=0.5, grad_logp=out)
+    assert h.tolist() == [50.0, 100.0] and not bool(out.any())
+
+
+def test_gradients_by_differences(T):
+    """The GPU's gradients against differences of the GPU's own losses summed in float64: a step of 0.05 along a
+    random direction through 200 tokens has an error of order step^2."""
+    import torch
+    rng = np.random.default_rng(11)
+    seqs, groups = np.arange(0, 201, 10), np.array([0, 8, 20])
+    lp, ref = -rng.exponential(size=200), -rng.exponential(size=200)
+    scores = rng.normal(size=20).astype(np.float32)
+    u = rng.normal(size=200)
+
+    def pref(e, **kw):
+        return T.tree_ens_preference_loss(_dev((lp + e * u).astype(np.float32)), _dev(seqs), _dev(scores), _dev(groups),
+                                          ref_logp=_dev(ref.astype(np.float32)), smoothing=0.05, flags=T.TREE_ENS_SEQ_MEAN, **kw)
+    slope = (pref(0.05)[0].double().sum() - pref(-0.05)[0].double().sum()) / 0.1
+    assert abs(float(slope) - float((pref(0.0)[2].double().cpu() * torch.from_numpy(u)).sum())) < 1e-4
+
+    def policy(e):
+        return T.tree_ens_policy_loss(_dev((lp + e * u).astype(np.float32)), _dev((lp - 0.05 * u).astype(np.float32)), _dev(scores),
+                                      _dev(seqs), ref_logp=_dev(ref.astype(np.float32)), clip_low=1.0, clip_high=9.0, kl_coef=0.2)
+    slope = (policy(0.01)[0].double().sum() - policy(-0.01)[0].double().sum()) / 0.02
+    got = float((policy(0.0)[2].double().cpu() * torch.from_numpy(u)).sum())
+    assert abs(float(slope) - got) < 1e-3 * (1 + abs(got))
+
+
+def test_another_stream_and_graph(T):
+    import torch
+    rng, seqs, lp, ref, mask = _tokens("ordinary")
+    n_seqs = len(seqs) - 1
+    groups = _groups(rng, n_seqs, [30])
+    a = [_dev(x) for x in (lp, seqs, rng.normal(size=n_seqs).astype(np.float32), groups, ref, mask)]
+    out = [torch.empty(len(groups) - 1, device="cuda"), torch.empty(n_seqs, device="cuda"), torch.empty(len(lp), device="cuda"),
+           torch.empty(n_seqs, device="cuda"), torch.empty(n_seqs, device="cuda"), torch.empty(len(lp), device="cuda")]
+
+    def step(stream=None):
+        T.tree_ens_preference_loss(a[0], a[1], a[2], a[3], ref_logp=a[4], mask=a[5], flags=T.TREE_ENS_SEQ_MEAN, loss=out[0],
+                                   margins=out[1], grad_logp=out[2], stream=stream)
+        adv = T.tree_ens_group_advantage(a[2], a[3], stream=stream)
+        T.tree_ens_policy_loss(a[0], a[4], adv, a[1], ref_logp=a[4], mask=a[5], kl_coef=0.1, flags=T.TREE_ENS_SEQ_MEAN,
+                               loss=out[3], kl=out[4], grad_logp=out[5], stream=stream)
+        return adv
+    step()
+    want = [o.clone() for o in out]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(out, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        adv = step()
+    for k in range(3):
+        a[0].copy_(torch.from_numpy(-np.random.default_rng(k).exponential(size=len(lp))).float())
+        step()
+        want = [o.clone() for o in out]
+        for o in out:
+            o.fill_(-7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, want)), k
+    assert adv.numel() == n_seqs
+
+
+def test_argument_errors(T):
+    import torch
+    lp, seqs = torch.zeros(8, device="cuda"), _dev(np.array([0, 3, 8]))
+    scores, groups = torch.zeros(2, device="cuda"), _dev(np.array([0, 2]))
+    with pytest.raises(TypeError, match="scores"):
+        T.tree_ens_preference_loss(lp, seqs, scores[:1], groups)
+    with pytest.raises(TypeError, match="seq_offsets"):
+        T.tree_ens_preference_loss(lp, seqs.int(), scores, groups)
+    with pytest.raises(TypeError, match="mask"):
+        T.tree_ens_preference_loss(lp, seqs, scores, groups, mask=lp)
+    with pytest.raises(TypeError, match="ref_logp"):
+        T.tree_ens_preference_loss(lp, seqs, scores, groups, ref_logp=lp[:4])
+    with pytest.raises(TypeError, match="logp"):
+        T.tree_ens_preference_loss(lp.double(), seqs, scores, groups)
+    with pytest.raises(T.TreeEnsError) as ei:
+        T.tree_ens_preference_loss(lp, seqs, scores, groups, smoothing=1.0)
+    assert ei.value.code == T.TREE_ENS_E_ARG
+    with pytest.raises(TypeError, match="advantages"):
+        T.tree_ens_policy_loss(lp, None, scores[:1].expand(2), seqs)
+    with pytest.raises(T.TreeEnsError):
+        T.tree_ens_policy_loss(lp, None, scores, seqs, kl_coef=0.1)
+    with pytest.raises(T.TreeEnsError):
+        T.tree_ens_group_advantage(scores, groups, eps=0.0)
