@@ -286,3 +286,48 @@ def test_argument_errors(T):
     logp, _, _ = T.tree_ens_token_logp(empty, td[:0])
     assert logp.shape == (0,)
     assert T.tree_ens_token_logp_backward(empty, td[:0], torch.empty(0, 2, device="cuda"), g[:0]).shape == (0, 8)
+
+
+@pytest.mark.parametrize("dtype,n,V,pad", [
+    ("bf16", 9_000, 203, 0), ("bf16", 8_200, 2_000, 0), ("f32", 8_001, 1_000, 3),   # 16 threads a row
+    ("f16", 2_500, 3_001, 0), ("f32", 20_000, 1_100, 0), ("bf16", 50, 400, 0),      # a wave
+    ("bf16", 700, 40_003, 0), ("f32", 20, 1_500, 0), ("f32", 4_100, 17_001, 1),     # 256 threads
+    ("bf16", 300, 8_001, 0), ("f16", 130, 60_000, 0),                               # 1,024 threads
+    ("bf16", 128, 33_000, 0), ("f32", 2, 200_001, 0), ("f16", 64, 100_001, 7),      # shares of a row
+])
+def test_every_way_to_split_the_rows(T, dtype, n, V, pad):
+    """Rows enough (or few enough) for each way the passes are split, 40 of them against the oracle."""
+    print("[logp]", dtype, n, V, pad, flush=True)
+    import torch
+    d, td, _, t = _logits(dtype, n, V, pad, seed=5)
+    pick = np.unique(np.concatenate([[0, n - 1], np.random.default_rng(n).integers(0, n, 38)]))
+    x = d[torch.from_numpy(pick).cuda()].double().cpu().numpy()
+    want = O.token_logp(x, t[pick], 0.8)
+    for entropy in (True, False):
+        got = T.tree_ens_token_logp(d, td, scale=0.8, want_entropy=entropy)
+        at = [a.cpu()[pick] for a in (got[0], got[1] if entropy else torch.from_numpy(_full(want[1], pick, n)), got[2])]
+        _check_forward(at, want, V, f"{dtype} {n} x {V}")
+        again = T.tree_ens_token_logp(d, td, scale=0.8, want_entropy=entropy)
+        assert torch.equal(got[0], again[0]) and torch.equal(got[2], again[2])
+    rng = np.random.default_rng(1)
+    g, h = rng.normal(size=n).astype(np.float32), rng.normal(size=n).astype(np.float32)
+    _, entropy, stats = T.tree_ens_token_logp(d, td, scale=0.8, want_entropy=True)
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for k, more in enumerate(({}, dict(entropy=entropy, grad_entropy=dev(h)))):
+        out = T.tree_ens_token_logp_backward(d, td, stats, dev(g), scale=0.8, **more)
+        ref = O.token_logp_grad(x, t[pick], g[pick], h[pick] if k else None, 0.8)
+        # the statistics are the kernel's: they carry its own rounding
+        slack = _forward_tolerance(V, *want)
+        tol = _grad_tolerance(ref, x, t[pick], g[pick], h[pick] * k, 0.8, dtype, want[2], want[1])
+        p = np.exp(0.8 * (x - x.max(1, keepdims=True)) - want[2][:, 1:])
+        tol = tol + 0.8 * p * (np.abs(g[pick]) * slack[2] + k * np.abs(h[pick]) * (slack[1] + slack[2] * (2 + want[1] + np.abs(want[2][:, 1]))))[:, None] * 2
+        err = np.abs(out[torch.from_numpy(pick).cuda()].double().cpu().numpy() - ref) / tol
+        assert (err <= 1).all(), float(err.max())
+        dead = torch.from_numpy((t < 0)).cuda()
+        assert not bool(out[dead].any())
+
+
+def _full(values, pick, n):
+    out = np.zeros(n)
+    out[pick] = values
+    return out
