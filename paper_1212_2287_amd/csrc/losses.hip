@@ -30,14 +30,15 @@ __device__ __forceinline__ Span span_of(const int64_t *offsets, int64_t i, int64
     return {a, min(max(offsets[i + 1], a), n)};
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
+template <typename T> __device__ __forceinline__ T wave_sum(T v) {
     for (int off = kWave / 2; off; off >>= 1)
         v += __shfl_xor(v, off);
     return v;
 }
 
 // Sum over the workgroup, in a fixed order, for every thread.
-__device__ __forceinline__ double block_sum(double v, double *part) {
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double part[kWaves];
     v = wave_sum(v);
     __syncthreads(); // part may still be read for the sum before
     if (threadIdx.x % kWave == 0)
@@ -76,110 +77,154 @@ struct Tokens {
 // ---------------------------------------------------------------------------------------------
 // Tiles of tokens
 //
-// Sums over sequences of any lengths read the tokens in tiles of equal size, eight neighbours a thread,
+// Sums over sequences of any lengths read the tokens in tiles of equal size, neighbours a thread,
 // so no workgroup waits for a long sequence. A thread finds the sequence of its first token by search
 // and walks on; what a sequence leaves open at a thread's end is carried to the next one by a segmented
 // scan over the workgroup. A sequence inside one tile has its sum stored by the tile; one that goes on
 // leaves the tile's `tail` where it begins and `head` in every later tile, added up afterwards in order.
 // ---------------------------------------------------------------------------------------------
-constexpr int kEach = 8;
+constexpr int kEach = 16;
 constexpr int kTile = kThreads * kEach;
 
-struct Pair {
-    double a, b;
+template <typename B> struct Pair {
+    double a;
+    B b;
 };
-__device__ __forceinline__ Pair operator+(Pair x, Pair y) { return {x.a + y.a, x.b + y.b}; }
+template <typename B> __device__ __forceinline__ Pair<B> operator+(Pair<B> x, Pair<B> y) { return {x.a + y.a, x.b + y.b}; }
 
 // Two sums per sequence and two per tile.
-struct Sums {
-    Pair *inside; // [n_seqs], of sequences inside one tile
-    Pair *head;   // [tiles]
-    Pair *tail;   // [tiles]
+template <typename B> struct Sums {
+    Pair<B> *inside; // [n_seqs], of sequences inside one tile
+    Pair<B> *head;   // [tiles]
+    Pair<B> *tail;   // [tiles]
 };
 
-// The last s in [-1, n_seqs] with offsets[s] <= t (-1: none), by 64 pivots at a time. Offsets that
-// decrease give some index of the range.
-__device__ __forceinline__ int64_t sequence_at(const int64_t *offsets, int64_t n_seqs, int64_t t) {
-    int64_t lo = -1, hi = n_seqs + 1; // offsets[lo] <= t < offsets[hi]
-    while (hi - lo > 1) {
-        const int64_t step = (hi - lo + kWave) / (kWave + 1), p = lo + (threadIdx.x % kWave + 1) * step;
-        lo += __popcll(__ballot(p < hi && offsets[p] <= t)) * step;
-        hi = min(hi, lo + step);
+// The sequences of a tile's first and last token: the last s in [-1, n_seqs] with offsets[s] <= the
+// token (-1: none), by one wave with 64 pivots at a time. Offsets that decrease give some indices of the
+// range.
+__device__ __forceinline__ int2 sequences_of(const int64_t *offsets, int n_seqs, int64_t first, int64_t last) {
+    unsigned lo[2] = {0, 0}, hi[2] = {unsigned(n_seqs) + 2, unsigned(n_seqs) + 2}; // from -1 on
+    const unsigned lane = threadIdx.x % kWave + 1;
+    while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1) { // offsets[lo - 1] <= the token < offsets[hi - 1]
+        unsigned step[2];
+        bool before[2] = {false, false};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            step[e] = (hi[e] - lo[e] + kWave) / (kWave + 1);
+            // in 64 bits: the pivots beyond hi may pass 32
+            const uint64_t p = lo[e] + uint64_t(lane) * step[e];
+            if (p < hi[e])
+                before[e] = offsets[p - 1] <= (e ? last : first);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            lo[e] += unsigned(__popcll(__ballot(before[e]))) * step[e];
+            hi[e] = step[e] < hi[e] - lo[e] ? lo[e] + step[e] : hi[e];
+        }
     }
-    return lo;
+    return make_int2(int(lo[0]) - 1, int(lo[1]) - 1);
 }
 
-// The sequence of a token, while the token moves on inside a tile. -1 and n_seqs stand for the tokens
-// before the first and after the last sequence.
+// The sequence of a token, while the token moves on inside a tile. Positions count from the tile's
+// first token, sequences from that token's; those without one (before the first, after the last
+// sequence) have indices outside [0, n_seqs) too.
+constexpr int kStaged = 512; // offsets of a tile that are held in LDS
 struct Walk {
     const int64_t *offsets;
-    int64_t n_seqs, n, last, s, end; // last: the sequence of the tile's last token
-    __device__ __forceinline__ bool inside() const { return s >= 0 && s < n_seqs; }
-    __device__ __forceinline__ int64_t start() const { return s < 0 ? 0 : max(offsets[s], int64_t(0)); }
-    __device__ __forceinline__ int64_t end_of(int64_t i) const { return i < n_seqs ? min(offsets[i + 1], n) : n; }
+    const int *staged; // offsets of the tile's sequences, within [-1, count]
+    int64_t n_seqs, first, s0;
+    int last, count; // last: the sequence of the tile's last token
+    bool goes_on;    // past the tile
+    int s, end;
+    __device__ __forceinline__ int64_t sequence() const { return s0 + s; }
+    __device__ __forceinline__ bool inside() const { return sequence() >= 0 && sequence() < n_seqs; }
+    __device__ __forceinline__ int fetch(int i) const { // where sequence i begins
+        if (s0 + i < 0)
+            return first == 0 ? 0 : -1;
+        if (s0 + i > n_seqs)
+            return count;
+        return int(max(int64_t(-1), min(max(offsets[s0 + i], int64_t(0)) - first, int64_t(count))));
+    }
+    __device__ __forceinline__ int start_of(int i) const { return i < kStaged ? staged[i] : fetch(i); }
     // s: a sequence at or before that of t
-    __device__ __forceinline__ void place(int64_t t) {
-        int64_t lo = s, hi = last;
+    __device__ __forceinline__ void place(int t) {
+        int lo = s, hi = last;
         while (lo < hi) {
-            const int64_t mid = lo + (hi - lo + 1) / 2;
-            if (offsets[mid] <= t)
+            const int mid = lo + (hi - lo + 1) / 2;
+            if (start_of(mid) <= t)
                 lo = mid;
             else
                 hi = mid - 1;
         }
         s = lo;
-        end = end_of(s);
+        end = s < last ? start_of(s + 1) : goes_on ? INT32_MAX : count;
     }
 };
 
-__device__ __forceinline__ Walk walk_from(const Tokens &in, int64_t first, int64_t count) {
-    Walk w{in.offsets, in.n_seqs, in.n, 0, 0, 0};
-    w.s = sequence_at(in.offsets, in.n_seqs, first);
-    w.last = sequence_at(in.offsets, in.n_seqs, first + count - 1);
+// Called by every thread of the workgroup; `q`: the sequences of the tile's first and last token.
+__device__ __forceinline__ Walk walk_of(const Tokens &in, int64_t first, int64_t count, int2 q, int *staged) {
+    Walk w{in.offsets, staged, in.n_seqs, first, q.x, max(q.y - q.x, 0), int(count), true, 0, 0};
+    const int64_t at = w.s0 + w.last;
+    if (at >= 0 && at < in.n_seqs)
+        w.goes_on = min(in.offsets[at + 1], in.n) > first + count;
+    __syncthreads(); // the tile before has been walked
+    for (int i = threadIdx.x; i <= w.last && i < kStaged; i += kThreads)
+        staged[i] = w.fetch(i);
+    __syncthreads();
     return w;
 }
 
 typedef float float4_ __attribute__((ext_vector_type(4), aligned(4)));
-typedef unsigned char byte8_ __attribute__((ext_vector_type(8), aligned(1)));
+typedef unsigned unsigned_ __attribute__((aligned(1)));
 
 // A thread's tokens [t, t + count) of an array.
-__device__ __forceinline__ void load_tokens(const float *p, int64_t t, int count, float (&x)[kEach]) {
-    if (count == kEach) {
-        const float4_ a = *reinterpret_cast<const float4_ *>(p + t), b = *reinterpret_cast<const float4_ *>(p + t + 4);
+template <int E> __device__ __forceinline__ void load_tokens(const float *p, int64_t t, int count, float (&x)[E]) {
+    if (count == E) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] = a[k];
-            x[k + 4] = b[k];
+        for (int v = 0; v < E; v += 4) {
+            const float4_ a = *reinterpret_cast<const float4_ *>(p + t + v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x[v + k] = a[k];
         }
         return;
     }
 #pragma unroll
-    for (int k = 0; k < kEach; ++k)
+    for (int k = 0; k < E; ++k)
         x[k] = k < count ? p[t + k] : 0.0f;
 }
 
-__device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, const float (&x)[kEach]) {
-    if (count == kEach) {
-        *reinterpret_cast<float4_ *>(p + t) = float4_{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<float4_ *>(p + t + 4) = float4_{x[4], x[5], x[6], x[7]};
+template <int E> __device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, const float (&x)[E]) {
+    if (count == E) {
+#pragma unroll
+        for (int v = 0; v < E; v += 4)
+            *reinterpret_cast<float4_ *>(p + t + v) = float4_{x[v], x[v + 1], x[v + 2], x[v + 3]};
         return;
     }
 #pragma unroll
-    for (int k = 0; k < kEach; ++k)
+    for (int k = 0; k < E; ++k)
         if (k < count)
             p[t + k] = x[k];
 }
 
+// Bit k: byte k of x is not 0.
+__device__ __forceinline__ unsigned nonzero_bytes(unsigned x) {
+    const unsigned high = (((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u;
+    return ((high >> 7) * 0x10204080u) >> 28;
+}
+
 // Bit k: token t + k counts.
-__device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, int count) {
+template <int E> __device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, int count) {
+    if (count <= 0)
+        return 0u;
+    const unsigned all = (1u << count) - 1;
+    if (!mask)
+        return all;
     unsigned bits = 0;
-    if (!mask || count <= 0)
-        return count <= 0 ? 0u : (1u << count) - 1;
-    if (count == kEach) {
-        const byte8_ m = *reinterpret_cast<const byte8_ *>(mask + t);
+    if (count == E) {
 #pragma unroll
-        for (int k = 0; k < kEach; ++k)
-            bits |= unsigned(m[k] != 0) << k;
+        for (int v = 0; v < E; v += 4)
+            bits |= nonzero_bytes(*reinterpret_cast<const unsigned_ *>(mask + t + v)) << v;
         return bits;
     }
     for (int k = 0; k < count; ++k)
@@ -187,75 +232,95 @@ __device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, in
     return bits;
 }
 
-__device__ __forceinline__ Pair shuffle_up(Pair x, int by) { return {__shfl_up(x.a, by), __shfl_up(x.b, by)}; }
+// Lanes' values moved by a DPP control; 0 where no lane is the source.
+template <int kControl, int kRows> __device__ __forceinline__ int moved(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xf, false);
+}
+template <int kControl, int kRows> __device__ __forceinline__ double moved(double x) {
+    const long long u = __double_as_longlong(x);
+    const unsigned lo = unsigned(moved<kControl, kRows>(int(u))), hi = unsigned(moved<kControl, kRows>(int(u >> 32)));
+    return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
+}
 
-// Adds up value(k) of the tile's tokens by sequence and stores the sums. enter() is called when the
-// walk has come to another sequence, before the value of its first token is asked for.
-template <typename Enter, typename Value>
-__device__ __forceinline__ void sum_tile(const Sums &out, int64_t tile, int64_t n, Walk w, Enter &&enter, Value &&value) {
-    __shared__ Pair part[kWaves];
-    __shared__ bool closed[kWaves];
-    const int64_t first = tile * kTile, t = first + threadIdx.x * kEach;
-    const int count = int(max(int64_t(0), min(int64_t(kEach), n - t)));
-    Pair open{0.0, 0.0}, head{0.0, 0.0}; // of the sequence being walked; of the one that the thread began in
-    bool ended = false;                  // some sequence ended in this thread
-    int64_t head_s = -1;                 // the one that the thread began in, if it ends here
-    bool head_before = false;            // and began before the tile
+// One step of an inclusive scan over the wave that starts again wherever a sequence ended.
+template <int kControl, int kRows, typename B> __device__ __forceinline__ void scan_step(Pair<B> &run, int &stop) {
+    const Pair<B> p{moved<kControl, kRows>(run.a), moved<kControl, kRows>(run.b)};
+    const int q = moved<kControl, kRows>(stop);
+    if (!stop)
+        run = p + run;
+    stop |= q;
+}
+
+// Adds up the tile's tokens by sequence: x and, counted, y (one of them per token if it has none).
+// Stores the sums. Tokens that do not count hold 0.
+template <typename B, typename Y>
+__device__ __forceinline__ void sum_tile(const Sums<B> &out, int64_t tile, Walk w, float (&x)[kEach], Y &&y) {
+    __shared__ Pair<B> part[kWaves];
+    __shared__ int closed[kWaves];
+    const int t = threadIdx.x * kEach, count = min(kEach, w.count - t);
+    Pair<B> open{0, 0}, head{0, 0}; // of the sequence being walked; of the one that the thread began in
+    int ended = 0;                  // some sequence ended in this thread
+    int64_t head_s = -1;            // the one that the thread began in, if it ends here
+    bool head_before = false;       // and began before the tile
     if (count > 0) {
         w.place(t);
-        enter(w);
-        bool own = w.start() >= t; // the walked sequence began in this thread
-        const bool before = w.start() < first;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            if (k < count) {
-                if (t + k >= w.end) {
-                    w.s += 1;
-                    w.place(t + k);
-                    enter(w);
-                }
-                const Pair v = value(k);
-                open = open + v;
-                if (t + k + 1 >= w.end) {
-                    if (w.inside()) {
-                        if (own) {
-                            out.inside[w.s] = open;
-                        } else {
-                            head = open;
-                            head_s = w.s;
-                            head_before = before;
-                        }
-                    }
-                    open = {0.0, 0.0};
-                    ended = own = true;
+        const int start = w.start_of(w.s);
+        bool own = start >= t; // the walked sequence began in this thread
+        const auto close = [&] {
+            if (w.inside()) {
+                if (own) {
+                    out.inside[w.sequence()] = open;
+                } else {
+                    head = open;
+                    head_s = w.sequence();
+                    head_before = start < 0;
                 }
             }
-        }
-    }
-    // inclusive scan of what is open, restarted wherever a sequence ended
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    Pair run = open;
-    bool stop = ended;
+            open = {0, 0};
+            ended = 1;
+            own = true;
+        };
+        int k = 0;
+        while (t + count > w.end) { // some tokens are the next sequence's
+            const int to = w.end - t;
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const Pair p = shuffle_up(run, off);
-        const bool q = __shfl_up(int(stop), off);
-        if (lane >= off && !stop) {
-            run = run + p;
-            stop = q;
+            for (int i = 0; i < kEach; ++i) {
+                open.a += i < to ? x[i] : 0.0f;
+                x[i] = i < to ? 0.0f : x[i];
+            }
+            open.b = y(k, to);
+            close();
+            k = to;
+            w.s += 1;
+            w.place(t + to);
         }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            open.a += x[i];
+        open.b = y(k, count);
+        if (t + count == w.end)
+            close();
     }
-    __syncthreads(); // the tile before has been read
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    Pair<B> run = open;
+    int stop = ended;
+    scan_step<0x111, 0xf>(run, stop); // row_shr 1, 2, 4, 8: within 16 lanes
+    scan_step<0x112, 0xf>(run, stop);
+    scan_step<0x114, 0xf>(run, stop);
+    scan_step<0x118, 0xf>(run, stop);
+    scan_step<0x142, 0xa>(run, stop); // row_bcast 15: into the second and fourth 16
+    scan_step<0x143, 0xc>(run, stop); // row_bcast 31: into the upper 32
+    __syncthreads();                  // the tile before has been read
     if (lane == kWave - 1) {
         part[wave] = run;
         closed[wave] = stop;
     }
     __syncthreads();
-    Pair carry = shuffle_up(run, 1);
-    bool stopped = __shfl_up(int(stop), 1);
+    Pair<B> carry{__shfl_up(run.a, 1), __shfl_up(run.b, 1)};
+    int stopped = __shfl_up(stop, 1);
     if (lane == 0) {
-        carry = {0.0, 0.0};
-        stopped = false;
+        carry = {0, 0};
+        stopped = 0;
     }
     for (int k = wave - 1; k >= 0 && !stopped; --k) {
         carry = part[k] + carry;
@@ -263,22 +328,19 @@ __device__ __forceinline__ void sum_tile(const Sums &out, int64_t tile, int64_t 
     }
     if (head_s >= 0)
         (head_before ? out.head[tile] : out.inside[head_s]) = carry + head;
-    if (threadIdx.x == kThreads - 1) { // a sequence that goes on in the next tile
-        const int64_t end = min(first + kTile, n);
-        w.s = w.last;
-        if (w.inside() && w.end_of(w.s) > end)
-            (w.start() < first ? out.head : out.tail)[tile] = ended ? open : carry + open;
-    }
+    w.s = w.last;
+    if (threadIdx.x == kThreads - 1 && w.goes_on && w.inside())
+        (w.start_of(w.s) < 0 ? out.head : out.tail)[tile] = ended ? open : carry + open;
 }
 
 // The sums of a sequence, from the tiles.
-__device__ __forceinline__ Pair joined(const Sums &in, int64_t s, Span q) {
+template <typename B> __device__ __forceinline__ Pair<B> joined(const Sums<B> &in, int64_t s, Span q) {
     if (q.a == q.b)
-        return {0.0, 0.0};
+        return {0, 0};
     const int64_t first = q.a / kTile, last = (q.b - 1) / kTile;
     if (first == last)
         return in.inside[s];
-    Pair sum = in.tail[first];
+    Pair<B> sum = in.tail[first];
 #pragma unroll 4
     for (int64_t k = first + 1; k <= last; ++k)
         sum = sum + in.head[k];
@@ -289,19 +351,31 @@ __device__ __forceinline__ Pair joined(const Sums &in, int64_t s, Span q) {
 // Preference loss
 // ---------------------------------------------------------------------------------------------
 
-// Sums of a sequence's log ratios, and how many count.
-__global__ void __launch_bounds__(kThreads) ratio_tile_kernel(Tokens in, Sums out) {
+// Sums of a sequence's log ratios, and how many count; and the tiles' sequences, for spread_tile_kernel.
+__global__ void __launch_bounds__(kThreads) ratio_tile_kernel(Tokens in, Sums<int> out, int2 *bounds) {
+    __shared__ int staged[kStaged];
     const int64_t tiles = (in.n + kTile - 1) / kTile;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t first = tile * kTile, t = first + threadIdx.x * kEach;
-        const int count = int(max(int64_t(0), min(int64_t(kEach), in.n - t)));
+        const int64_t first = tile * kTile, size = min(int64_t(kTile), in.n - first), t = first + threadIdx.x * kEach;
+        const int count = int(min(int64_t(kEach), in.n - t));
         float x[kEach], r[kEach] = {};
         load_tokens(in.logp, t, count, x);
         if (in.ref)
             load_tokens(in.ref, t, count, r);
-        const unsigned use = load_mask(in.mask, t, count);
-        sum_tile(out, tile, in.n, walk_from(in, first, min(int64_t(kTile), in.n - first)), [](const Walk &) {},
-                 [&](int k) { return use >> k & 1u ? Pair{double(x[k] - r[k]), 1.0} : Pair{0.0, 0.0}; });
+        const unsigned use = load_mask<kEach>(in.mask, t, count);
+        __shared__ int2 found;
+        if (threadIdx.x < kWave) {
+            const int2 q = sequences_of(in.offsets, int(in.n_seqs), first, first + size - 1);
+            if (threadIdx.x == 0)
+                bounds[tile] = found = q;
+        }
+        __syncthreads();
+        const int2 q = found;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            x[k] = use >> k & 1u ? x[k] - r[k] : 0.0f;
+        sum_tile(out, tile, walk_of(in, first, size, q, staged), x,
+                 [&](int k, int to) { return __popc(use & (2u << (to - 1)) - (1u << k)); });
     }
 }
 
@@ -314,148 +388,405 @@ struct Preference {
     float *loss, *margins, *weights; // weights: dh / dlogp of a counted token, then the loss's gradient
 };
 
-// Margins and weights of the sequences [a, b), by the threads of a workgroup.
-__device__ __forceinline__ void join_margins(const Tokens &in, const Sums &sums, const Preference &p, int64_t a, int64_t b, bool alone) {
-    for (int64_t s = a + threadIdx.x; s < b; s += kThreads) {
-        const Pair v = joined(sums, s, span_of(in.offsets, s, in.n));
-        const double w = p.mean ? double(p.beta) / fmax(v.b, 1.0) : double(p.beta);
-        p.margins[s] = float(w * v.a);
-        p.weights[s] = alone ? 0.0f : float(w); // alone: in no group
+constexpr int kFour = 4; // neighbours that a lane takes of a sequence that is its wave's
+
+// Sum of a sequence's log ratios and how many count, by a wave.
+__device__ __forceinline__ Pair<int> ratios_of(const Tokens &in, Span q) {
+    double sum = 0.0;
+    int counted = 0;
+#pragma unroll 2
+    for (int64_t t = q.a + threadIdx.x % kWave * kFour; t < q.b; t += kWave * kFour) {
+        const int count = int(min(int64_t(kFour), q.b - t));
+        float x[kFour], r[kFour] = {};
+        load_tokens(in.logp, t, count, x);
+        if (in.ref)
+            load_tokens(in.ref, t, count, r);
+        const unsigned use = load_mask<kFour>(in.mask, t, count);
+#pragma unroll
+        for (int k = 0; k < kFour; ++k)
+            sum += use >> k & 1u ? x[k] - r[k] : 0.0f;
+        counted += __popc(use);
+    }
+    return {wave_sum(sum), wave_sum(counted)};
+}
+
+// The gradient at a sequence's tokens, by a wave.
+__device__ __forceinline__ void spread(const Tokens &in, Span q, float weight, float *grad) {
+    for (int64_t t = q.a + threadIdx.x % kWave * kFour; t < q.b; t += kWave * kFour) {
+        const int count = int(min(int64_t(kFour), q.b - t));
+        const unsigned use = load_mask<kFour>(in.mask, t, count);
+        float d[kFour];
+#pragma unroll
+        for (int k = 0; k < kFour; ++k)
+            d[k] = use >> k & 1u ? weight : 0.0f;
+        store_tokens(grad, t, count, d);
     }
 }
 
-// softplus(-d) = max(-d, 0) + log1p(e) and sigmoid(-d) of e = exp(-|d|).
-struct Logistic {
-    float softplus, sigmoid;
-};
-__device__ __forceinline__ Logistic logistic(float d) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504088896340736f * fabsf(d));
-    const float u = 1.0f + e, r = __builtin_amdgcn_rcpf(u);
-    // log1p(e) = log u + log(1 + rest / u), with the rest that u was rounded by
-    const float l = fmaf(e - (u - 1.0f), r, 0.69314718055994530942f * __builtin_amdgcn_logf(u));
-    return {(d < 0.0f ? -d : 0.0f) + l, d >= 0.0f ? e * r : r};
+__device__ __forceinline__ void spread_zero(float *grad, int64_t a, int64_t b) {
+    for (int64_t t = a + threadIdx.x % kWave; t < b; t += kWave)
+        grad[t] = 0.0f;
 }
 
-// Loss of a group, and weights times the loss's gradient with respect to the margins. With d the
-// margin of a pair, l = softplus(-d) + smoothing d and dl/dd = smoothing - sigmoid(-d). Every candidate
-// meets every other one, so each pair is met twice and nothing is added atomically.
-__global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Sums sums, Preference p) {
-    __shared__ double part[kWaves];
-    __shared__ float2 other[kThreads]; // (margin, score) of the candidates that are met
-    __shared__ float slopes[kThreads];
+constexpr int kHeld = 512; // candidates of a group that are held in LDS
+
+// What the pairs that a thread met add up to: softplus(-d), d and 1.
+struct Met {
+    float loss, lead;
+    int pairs;
+};
+// The same over threads, with the smoothing.
+struct Loss {
+    double sum, pairs;
+    // Margins that are infinite have no smoothed loss that is finite, but may have a plain one.
+    __device__ __forceinline__ void add(const Met &m, float smoothing, double weight) {
+        sum += weight * (smoothing > 0.0f ? m.loss + double(smoothing) * m.lead : double(m.loss));
+        pairs += weight * m.pairs;
+    }
+};
+
+// One pair: dl/dh of the candidate `me`, and with kLoss the pair's loss. Candidates are (margin, score),
+// margins and losses in units of ln 2 here. With d the margin by which the better one leads and e =
+// exp(-|d|): l = softplus(-d) + smoothing d, softplus(-d) = max(-d, 0) + log1p(e), dl/dd = smoothing -
+// sigmoid(-d).
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLn2 = 0.693147180559945309417;
+template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 other, float smoothing, Met &met) {
+    const bool ahead = me.y > other.y, behind = me.y < other.y;
+    const float lead = me.x - other.x;
+    const float e = __builtin_amdgcn_exp2f(-fabsf(lead));
+    const float u = 1.0f + e, r = __builtin_amdgcn_rcpf(u);
+    if (kLoss) {
+        const float d = ahead ? lead : -lead;
+        // log1p(e) = log u + log(1 + rest / u), with the rest that u was rounded by
+        float l = __builtin_amdgcn_logf(u) + fmaxf(-d, 0.0f);
+        l = fmaf((e - (u - 1.0f)) * r, kLog2e, l);
+        met.loss += ahead || behind ? l : 0.0f;
+        met.lead += ahead || behind ? d : 0.0f;
+        met.pairs += ahead || behind;
+    }
+    const float dl = smoothing - ((lead >= 0.0f) == ahead ? e * r : r);
+    return ahead ? dl : behind ? -dl : 0.0f;
+}
+
+// The n <= kHeld candidates of a group lie twice in a row, so that i + k needs no remainder. In step k
+// candidate i meets i + k (modulo n), for its own slope alone, so nothing is added atomically; the first
+// half of the steps meets every pair once and takes its loss. One thread takes candidate i in every
+// `shares`-th step from 1 + share on; returns its slope.
+__device__ __forceinline__ float meet_held(const float2 *held, int n, int i, int share, int shares, float smoothing, Loss &loss) {
+    const float2 me = held[i], *other = held + i;
+    Met met{0.0f, 0.0f, 0}, unused = met;
+    float slope = 0.0f;
+    int k = 1 + share;
+#pragma unroll 4
+    for (; k <= (n - 1) / 2; k += shares)
+        slope += meet<true>(me, other[k], smoothing, met);
+    if (2 * k == n) { // opposite each other: the lower one takes the loss
+        slope += meet<true>(me, other[k], smoothing, i < k ? met : unused);
+        k += shares;
+    }
+#pragma unroll 4
+    for (; k < n; k += shares)
+        slope += meet<false>(me, other[k], smoothing, met);
+    loss.add(met, smoothing, 1.0);
+    return slope;
+}
+
+// One thread's candidate against the kHeld or fewer of a larger group that are held: every pair is met
+// twice.
+__device__ __forceinline__ float meet_window(float2 me, const float2 *held, int fit, int share, int shares, float smoothing, Loss &loss) {
+    Met met{0.0f, 0.0f, 0};
+    float slope = 0.0f;
+#pragma unroll 4
+    for (int j = share; j < fit; j += shares)
+        slope += meet<true>(me, held[j], smoothing, met);
+    loss.add(met, smoothing, 0.5);
+    return slope;
+}
+
+// Loss of a group, and weights times the loss's gradient with respect to the margins, by a workgroup.
+// kFused: it also sums the sequences' tokens first and writes their gradients last, instead of the tile
+// kernels.
+template <bool kFused>
+__global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Sums<int> sums, Preference p, float *grad) {
+    __shared__ float2 held[2 * kHeld];
+    __shared__ float slopes[kWaves][kHeld];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     for (int64_t g = blockIdx.x; g < max(p.n_groups, int64_t(1)); g += gridDim.x) {
         Span q{in.n_seqs, in.n_seqs}; // without groups, every sequence is before the first one
         if (p.n_groups > 0)
             q = span_of(p.groups, g, in.n_seqs);
-        if (g == 0)
-            join_margins(in, sums, p, 0, q.a, true);
-        if (g == p.n_groups - 1)
-            join_margins(in, sums, p, q.b, in.n_seqs, true);
-        if (p.n_groups == 0)
-            return;
-        join_margins(in, sums, p, q.a, q.b, false);
-        __syncthreads();
-        // as many candidates at a time as fit, each by the same number of threads
+        // sequences outside every group go with the first and the last one; their gradient is 0
+        const int64_t lo = g == 0 ? 0 : q.a, hi = g >= p.n_groups - 1 ? in.n_seqs : q.b;
         const int64_t n = q.b - q.a;
-        const int rows = int(max(int64_t(1), min(n, int64_t(kThreads)))), shares = kThreads / rows;
-        const int row = threadIdx.x % rows, share = threadIdx.x / rows;
-        double total = 0.0, pairs = 0.0;
-        for (int64_t i0 = 0; i0 < n; i0 += rows) {
-            const int64_t i = i0 + row;
-            const bool mine = i < n && share < shares;
-            const float h = mine ? p.margins[q.a + i] : 0.0f, r = mine ? p.scores[q.a + i] : 0.0f;
-            float slope = 0.0f;
-            for (int64_t j0 = 0; j0 < n; j0 += kThreads) {
-                __syncthreads();
-                if (j0 + threadIdx.x < n)
-                    other[threadIdx.x] = make_float2(p.margins[q.a + j0 + threadIdx.x], p.scores[q.a + j0 + threadIdx.x]);
-                __syncthreads();
-                if (!mine)
-                    continue;
-                const int met = int(min(int64_t(kThreads), n - j0));
-                float sum = 0.0f;
-                int found = 0;
-                for (int j = share; j < met; j += shares) {
-                    const float2 o = other[j];
-                    const bool ahead = r > o.y, behind = r < o.y;
-                    if (!ahead && !behind)
-                        continue;
-                    const float d = ahead ? h - o.x : o.x - h;
-                    const Logistic l = logistic(d);
-                    const float dl = p.smoothing - l.sigmoid;
-                    slope += ahead ? dl : -dl;
-                    if (ahead) {
-                        sum += l.softplus;
-                        if (p.smoothing > 0.0f)
-                            sum = fmaf(p.smoothing, d, sum);
-                        ++found;
-                    }
-                }
-                total += sum;
-                pairs += found;
+        __syncthreads(); // held may still be read for the group before
+        const auto take = [&](int64_t s, Pair<int> v) {
+            const double w = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
+            const float h = float(w * v.a);
+            p.margins[s] = h;
+            p.weights[s] = s < q.a || s >= q.b ? 0.0f : float(w);
+            if (n <= kHeld && s >= q.a && s < q.b)
+                held[s - q.a] = held[s - q.a + n] = make_float2(h * kLog2e, p.scores[s]);
+        };
+        if constexpr (kFused) {
+            for (int64_t s = lo + wave; s < hi; s += kWaves) {
+                const Pair<int> v = ratios_of(in, span_of(in.offsets, s, in.n));
+                if (lane == 0)
+                    take(s, v);
             }
-            if (p.grad_scale != 0.0f) { // raw slopes; the number of pairs is not known yet
-                __syncthreads();
-                slopes[threadIdx.x] = slope;
-                __syncthreads();
-                if (threadIdx.x < rows && i < n) {
-                    double sum = slope;
-                    for (int k = 1; k < shares; ++k)
-                        sum += slopes[k * rows + row];
-                    p.weights[q.a + i] = float(p.weights[q.a + i] * sum);
+        } else {
+            for (int64_t s = lo + threadIdx.x; s < hi; s += kThreads)
+                take(s, joined(sums, s, span_of(in.offsets, s, in.n)));
+        }
+        __syncthreads();
+        Loss loss{0.0, 0.0};
+        if (n <= kHeld) {
+            // waves take steps in turn and leave their slopes in rows of their own
+            for (int i = lane; i < n; i += kWave)
+                slopes[wave][i] = meet_held(held, int(n), i, wave, kWaves, p.smoothing, loss);
+            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += kThreads) {
+                double sum = slopes[0][i];
+                for (int w = 1; w < kWaves; ++w)
+                    sum += slopes[w][i];
+                p.weights[q.a + i] = float(p.weights[q.a + i] * sum);
+            }
+        } else {
+            for (int64_t i0 = 0; i0 < n; i0 += kThreads) {
+                const int64_t i = q.a + i0 + threadIdx.x;
+                const float2 me = i < q.b ? make_float2(p.margins[i] * kLog2e, p.scores[i]) : make_float2(0.0f, 0.0f);
+                double sum = 0.0;
+                for (int64_t j0 = q.a; j0 < q.b; j0 += kHeld) {
+                    const int fit = int(min(int64_t(kHeld), q.b - j0));
+                    __syncthreads();
+                    for (int j = threadIdx.x; j < fit; j += kThreads)
+                        held[j] = make_float2(p.margins[j0 + j] * kLog2e, p.scores[j0 + j]);
+                    __syncthreads();
+                    if (i < q.b)
+                        sum += meet_window(me, held, fit, 0, 1, p.smoothing, loss);
                 }
+                if (i < q.b)
+                    p.weights[i] = float(p.weights[i] * sum);
             }
         }
-        total = block_sum(total, part);
-        pairs = block_sum(pairs, part);
-        if (threadIdx.x == 0)
-            p.loss[g] = float(total / fmax(pairs, 1.0));
-        const double by = double(p.grad_scale) / fmax(pairs, 1.0);
-        for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
-            p.weights[i] = float(p.weights[i] * by);
+        loss.sum = block_sum(loss.sum);
+        loss.pairs = block_sum(loss.pairs);
+        const double share = 1.0 / fmax(loss.pairs, 1.0);
+        if (threadIdx.x == 0 && p.n_groups > 0)
+            p.loss[g] = float(loss.sum * (kLn2 * share));
         __syncthreads();
+        if constexpr (kFused) {
+            if (!grad)
+                continue;
+            for (int64_t s = lo + wave; s < hi; s += kWaves) {
+                const Span t = span_of(in.offsets, s, in.n);
+                spread(in, t, float(p.weights[s] * (p.grad_scale * share)), grad);
+                if (s == 0)
+                    spread_zero(grad, 0, t.a);
+                if (s == in.n_seqs - 1)
+                    spread_zero(grad, t.b, in.n);
+            }
+        } else {
+            for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
+                p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
+        }
+    }
+}
+
+// Margins and weights, a thread a sequence, where pairs_part_kernel needs them all before it starts.
+__global__ void __launch_bounds__(kThreads) join_kernel(Tokens in, Sums<int> sums, Preference p) {
+    for (int64_t s = blockIdx.x * int64_t(kThreads) + threadIdx.x; s < in.n_seqs; s += int64_t(gridDim.x) * kThreads) {
+        const Pair<int> v = joined(sums, s, span_of(in.offsets, s, in.n));
+        const double w = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
+        p.margins[s] = float(w * v.a);
+        p.weights[s] = float(w);
+    }
+}
+
+constexpr int kHeldPart = 2048;
+
+// One of `parts` shares of a group's candidates, against all of the group. As many threads take a
+// candidate as there are, each every so many steps of it.
+__global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Preference p, int parts, Loss *partial) {
+    __shared__ float2 held[2 * kHeldPart];
+    __shared__ float slopes[kThreads];
+    const unsigned items = unsigned(p.n_groups) * unsigned(parts); // fewer than sequences
+    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+        const unsigned g = item / unsigned(parts), part = item - g * unsigned(parts);
+        const Span q = span_of(p.groups, g, n_seqs);
+        const unsigned n = unsigned(q.b - q.a), chunk = (n + unsigned(parts) - 1) / unsigned(parts);
+        const int64_t from = min(int64_t(part) * chunk, int64_t(n)), to = min(from + chunk, int64_t(n));
+        Loss loss{0.0, 0.0};
+        // rows of even size, as few as fit
+        const int turns = int((to - from + kThreads - 1) / kThreads), each = turns ? int((to - from + turns - 1) / turns) : 0;
+        for (int64_t i0 = from; i0 < to; i0 += each) {
+            const int rows = int(min(int64_t(each), to - i0)), shares = kThreads / rows;
+            const int row = threadIdx.x % rows, share = threadIdx.x / rows;
+            const int64_t i = i0 + row;
+            const float2 me = make_float2(p.margins[q.a + i] * kLog2e, p.scores[q.a + i]);
+            double slope = 0.0;
+            if (n <= kHeldPart) {
+                if (i0 == from)
+                    for (int j = threadIdx.x; j < n; j += kThreads)
+                        held[j] = held[j + n] = make_float2(p.margins[q.a + j] * kLog2e, p.scores[q.a + j]);
+                __syncthreads();
+                if (share < shares)
+                    slope = meet_held(held, int(n), int(i), share, shares, p.smoothing, loss);
+            } else {
+                for (int64_t j0 = 0; j0 < n; j0 += kHeldPart) {
+                    const int fit = int(min(int64_t(kHeldPart), n - j0));
+                    __syncthreads();
+                    for (int j = threadIdx.x; j < fit; j += kThreads)
+                        held[j] = make_float2(p.margins[q.a + j0 + j] * kLog2e, p.scores[q.a + j0 + j]);
+                    __syncthreads();
+                    if (share < shares)
+                        slope += meet_window(me, held, fit, share, shares, p.smoothing, loss);
+                }
+            }
+            slopes[threadIdx.x] = float(slope);
+            __syncthreads();
+            if (threadIdx.x < rows) {
+                for (int k = 1; k < shares; ++k)
+                    slope += slopes[k * rows + row];
+                p.weights[q.a + i] = float(p.weights[q.a + i] * slope);
+            }
+            __syncthreads(); // slopes are free
+        }
+        loss.sum = block_sum(loss.sum);
+        loss.pairs = block_sum(loss.pairs);
+        if (threadIdx.x == 0)
+            partial[item] = loss;
+        __syncthreads(); // held and slopes are free
+    }
+}
+
+// What pairs_part_kernel leaves: a group's loss, and weights by its number of pairs. A wave takes a group.
+__global__ void __launch_bounds__(kThreads) pairs_finish_kernel(int64_t n_seqs, Preference p, int parts, const Loss *partial) {
+    for (int64_t g = blockIdx.x * int64_t(kWaves) + threadIdx.x / kWave; g < p.n_groups; g += int64_t(gridDim.x) * kWaves) {
+        const int lane = threadIdx.x % kWave;
+        const Span q = span_of(p.groups, g, n_seqs);
+        Loss loss{0.0, 0.0};
+        for (int k = lane; k < parts; k += kWave) {
+            loss.sum += partial[g * parts + k].sum;
+            loss.pairs += partial[g * parts + k].pairs;
+        }
+        loss.sum = wave_sum(loss.sum);
+        loss.pairs = wave_sum(loss.pairs);
+        const double share = 1.0 / fmax(loss.pairs, 1.0);
+        if (lane == 0)
+            p.loss[g] = float(loss.sum * (kLn2 * share));
+        for (int64_t i = q.a + lane; i < q.b; i += kWave)
+            p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
+        // sequences outside every group
+        if (g == 0)
+            for (int64_t i = lane; i < q.a; i += kWave)
+                p.weights[i] = 0.0f;
+        if (g == p.n_groups - 1)
+            for (int64_t i = q.b + lane; i < n_seqs; i += kWave)
+                p.weights[i] = 0.0f;
+    }
+}
+
+// Groups of a few candidates: eight lanes take one. Larger ones among them are met from memory.
+constexpr int kFew = 8;
+__global__ void __launch_bounds__(kThreads) pairs_few_kernel(Tokens in, Sums<int> sums, Preference p) {
+    constexpr int kGroups = kThreads / kFew;
+    const int lane = threadIdx.x % kFew;
+    for (int64_t g0 = blockIdx.x * int64_t(kGroups); g0 < p.n_groups; g0 += int64_t(gridDim.x) * kGroups) {
+        const int64_t g = g0 + threadIdx.x / kFew;
+        if (g >= p.n_groups)
+            continue;
+        const Span q = span_of(p.groups, g, in.n_seqs);
+        const int64_t lo = g == 0 ? 0 : q.a, hi = g == p.n_groups - 1 ? in.n_seqs : q.b;
+        for (int64_t s = lo + lane; s < hi; s += kFew) {
+            const bool member = s >= q.a && s < q.b;
+            const Pair<int> v = joined(sums, s, span_of(in.offsets, s, in.n));
+            const double by = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
+            p.margins[s] = float(by * v.a);
+            p.weights[s] = member ? float(by) : 0.0f;
+        }
+        __threadfence_block(); // the group's lanes are of one wave
+        Loss loss{0.0, 0.0};
+        for (int64_t i = q.a + lane; i < q.b; i += kFew) {
+            const float2 me = make_float2(p.margins[i] * kLog2e, p.scores[i]);
+            Met met{0.0f, 0.0f, 0};
+            float slope = 0.0f;
+#pragma unroll 2
+            for (int64_t j = q.a; j < q.b; ++j)
+                slope += meet<true>(me, make_float2(p.margins[j] * kLog2e, p.scores[j]), p.smoothing, met);
+            loss.add(met, p.smoothing, 0.5);
+            p.weights[i] = float(p.weights[i] * slope);
+        }
+        for (int off = kFew / 2; off; off >>= 1) {
+            loss.sum += __shfl_xor(loss.sum, off);
+            loss.pairs += __shfl_xor(loss.pairs, off);
+        }
+        const double share = 1.0 / fmax(loss.pairs, 1.0);
+        if (lane == 0)
+            p.loss[g] = float(loss.sum * (kLn2 * share));
+        for (int64_t i = q.a + lane; i < q.b; i += kFew)
+            p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
+    }
+}
+
+// Stores a tile of kEach neighbours a thread, through LDS so that a wave's stores are neighbours.
+__device__ __forceinline__ void store_tile(float *out, int64_t first, int size, const float (&d)[kEach]) {
+    constexpr int kPad = kEach + 4; // rows of other banks
+    __shared__ float rows[kThreads * kPad];
+    __syncthreads(); // the tile before has been stored
+#pragma unroll
+    for (int v = 0; v < kEach; v += 4)
+        *reinterpret_cast<float4 *>(rows + threadIdx.x * kPad + v) = make_float4(d[v], d[v + 1], d[v + 2], d[v + 3]);
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kEach; v += 4) {
+        const int t = v * kThreads + threadIdx.x * 4;
+        const float4 q = *reinterpret_cast<const float4 *>(rows + t / kEach * kPad + t % kEach);
+        if (t + 4 <= size)
+            *reinterpret_cast<float4_ *>(out + first + t) = float4_{q.x, q.y, q.z, q.w};
+        else
+            for (int k = 0; t + k < size; ++k)
+                out[first + t + k] = rows[t / kEach * kPad + t % kEach + k];
     }
 }
 
 // grad[t] = the sequence's weight at its counted tokens.
-__global__ void __launch_bounds__(kThreads) spread_tile_kernel(Tokens in, const float *weights, float *grad) {
+__global__ void __launch_bounds__(kThreads) spread_tile_kernel(Tokens in, const int2 *bounds, const float *weights, float *grad) {
+    __shared__ int staged[kStaged];
     const int64_t tiles = (in.n + kTile - 1) / kTile;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t first = tile * kTile, t = first + threadIdx.x * kEach;
-        const int count = int(max(int64_t(0), min(int64_t(kEach), in.n - t)));
-        const unsigned use = load_mask(in.mask, t, count);
-        Walk w = walk_from(in, first, min(int64_t(kTile), in.n - first));
-        if (count <= 0)
-            continue;
-        w.place(t);
-        float x = w.inside() ? weights[w.s] : 0.0f, d[kEach];
+        const int64_t first = tile * kTile;
+        const int size = int(min(int64_t(kTile), in.n - first)), t = threadIdx.x * kEach, count = min(kEach, size - t);
+        const unsigned use = load_mask<kEach>(in.mask, first + t, count);
+        Walk w = walk_of(in, first, size, bounds[tile], staged);
+        float d[kEach] = {};
+        for (int k = 0; k < count;) {
+            w.place(t + k);
+            const float x = w.inside() ? weights[w.sequence()] : 0.0f;
+            const int to = min(w.end - t, count);
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            if (k < count && t + k >= w.end) {
-                w.s += 1;
-                w.place(t + k);
-                x = w.inside() ? weights[w.s] : 0.0f;
-            }
-            d[k] = use >> k & 1u ? x : 0.0f;
+            for (int i = 0; i < kEach; ++i)
+                d[i] = i >= k && use >> i & 1u ? x : d[i];
+            k = to;
+            w.s += 1;
         }
-        store_tokens(grad, t, count, d);
+        store_tile(grad, first, size, d);
     }
 }
 
 __global__ void __launch_bounds__(kThreads)
 advantage_kernel(const float *scores, int64_t n, const int64_t *groups, int64_t n_groups, float eps, bool center,
                  float *out) {
-    __shared__ double part[kWaves];
     for (int64_t g = blockIdx.x; g < n_groups; g += gridDim.x) {
         const Span q = span_of(groups, g, n);
         const double count = fmax(double(q.b - q.a), 1.0);
         double sum = 0.0, squares = 0.0;
         for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
             sum += scores[i];
-        const double mean = block_sum(sum, part) / count;
+        const double mean = block_sum(sum) / count;
         for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
             squares += (scores[i] - mean) * (scores[i] - mean);
-        const double std = sqrt(block_sum(squares, part) / count);
+        const double std = sqrt(block_sum(squares) / count);
         const double by = center ? 1.0 : 1.0 / (std + eps);
         for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
             out[i] = float((scores[i] - mean) * by);
@@ -487,7 +818,6 @@ struct Policy {
 };
 
 __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p) {
-    __shared__ double part[kWaves];
     for (int64_t s = blockIdx.x; s < in.n_seqs; s += gridDim.x) {
         const Span q = span_of(in.offsets, s, in.n);
         const float a = p.advantages[s];
@@ -496,7 +826,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p) {
             double count = 0.0;
             for (int64_t t = q.a + threadIdx.x; t < q.b; t += kThreads)
                 count += in.counts(t) ? 1.0 : 0.0;
-            share = 1.0 / fmax(block_sum(count, part), 1.0);
+            share = 1.0 / fmax(block_sum(count), 1.0);
         }
         const float w = float(p.grad_scale * share);
         double loss = 0.0, kl = 0.0;
@@ -518,8 +848,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p) {
             if (p.grad)
                 p.grad[t] = w * d;
         }
-        loss = block_sum(loss, part);
-        kl = block_sum(kl, part);
+        loss = block_sum(loss);
+        kl = block_sum(kl);
         if (threadIdx.x == 0) {
             p.loss[s] = float(share * (loss + p.kl_coef * kl));
             if (p.kl)
@@ -572,14 +902,52 @@ int64_t tiles_of(int64_t n_tokens) { return (n_tokens + kTile - 1) / kTile; }
 
 // Two sums per sequence and tile, 16 bytes each.
 int64_t sums_bytes(int64_t n_tokens, int64_t n_seqs) { return 16 * (n_seqs + 2 * tiles_of(n_tokens)); }
+int64_t bounds_bytes(int64_t n_tokens) { return 8 * tiles_of(n_tokens); }
 
-Sums sums_at(void *workspace, int64_t n_tokens, int64_t n_seqs) {
-    Pair *p = static_cast<Pair *>(workspace);
+template <typename B> Sums<B> sums_at(void *workspace, int64_t n_tokens, int64_t n_seqs) {
+    static_assert(sizeof(Pair<B>) == 16, "as sums_bytes counts");
+    Pair<B> *p = static_cast<Pair<B> *>(workspace);
     return {p, p + n_seqs, p + n_seqs + tiles_of(n_tokens)};
 }
 
-int64_t preference_bytes(int64_t n_tokens, int64_t n_seqs) {
-    return sums_bytes(n_tokens, n_seqs) + (n_seqs * 4 + 15) / 16 * 16;
+// Which kernels meet the pairs, by the mean sizes of groups and sequences. Measured (us of the whole loss;
+// groups x candidates x tokens; pairs_kernel fused / tile kernels with pairs_few_kernel / with pairs_kernel /
+// with pairs_part_kernel):
+//   64 x 2 x 250: 7.1 / 14.9 / 15.6; 512 x 2 x 500: 10.2 / 16.0 / 16.5; 512 x 8 x 500: 18.9 / 19.7 / 20.4;
+//   4,096 x 2 x 500: 39 / 23.9 / 34; 50,000 x 2 x 30: 272 / 29 / 153; 2 x 2 x 60,000: 451 / 12.9 / 14.2;
+//   5,000 x 8 x 20: 47 / 25.6 / 37; 512 x 16 x 500: 44 / 41 / 25.2; 2,000 x 40 x 100: - / - / 48 / 58;
+//   909 x 110 x 143: - / - / 79 / 75; 100 x 300 x 100: - / - / 137 / 45; 9,090 x 110 x 10: - / - / 190 / 210.
+enum class Pairs { kFused, kFew, kGroup, kParts };
+struct PreferencePlan {
+    Pairs by;
+    int parts;
+};
+
+PreferencePlan preference_plan(int64_t n_tokens, int64_t n_seqs, int64_t n_groups) {
+    if (n_groups == 0 || n_seqs == 0)
+        return {Pairs::kGroup, 1};
+    const double seqs = double(n_seqs) / double(n_groups), tokens = double(n_tokens) / double(n_seqs);
+    if (seqs <= 8.0 && n_seqs <= 4096 && tokens <= 1024.0)
+        return {Pairs::kFused, 1};
+    if (seqs <= 8.0)
+        return {Pairs::kFew, 1};
+    if (seqs >= 96.0 && n_groups <= 2048) // workgroups for the whole card, but eight candidates at least for each
+        return {Pairs::kParts, int(std::min(std::ceil(2048.0 / double(n_groups)), std::ceil(seqs / 8.0)))};
+    return {Pairs::kGroup, 1};
+}
+
+// Where a preference loss keeps what its kernels hand on.
+struct PreferenceSpace {
+    int64_t sums, bounds, weights, partial, bytes;
+};
+PreferenceSpace preference_space(int64_t n_tokens, int64_t n_seqs, int64_t n_groups) {
+    const PreferencePlan plan = preference_plan(n_tokens, n_seqs, n_groups);
+    const auto round = [](int64_t b) { return (b + 15) / 16 * 16; };
+    PreferenceSpace p{0, sums_bytes(n_tokens, n_seqs), 0, 0, 0};
+    p.weights = p.bounds + round(bounds_bytes(n_tokens));
+    p.partial = p.weights + round(4 * n_seqs);
+    p.bytes = p.partial + (plan.by == Pairs::kParts ? n_groups * plan.parts * int64_t(sizeof(Loss)) : 0);
+    return p;
 }
 
 } // namespace
@@ -593,7 +961,7 @@ int tree_ens_preference_workspace(int64_t n_tokens, int64_t n_seqs, int64_t n_gr
     *bytes = 0;
     if (int rc = check_counts(n_tokens, n_seqs, n_groups))
         return rc;
-    *bytes = preference_bytes(n_tokens, n_seqs);
+    *bytes = preference_space(n_tokens, n_seqs, n_groups).bytes;
     return TREE_ENS_OK;
 }
 
@@ -616,25 +984,41 @@ int tree_ens_preference_loss(void *stream, const float *logp, const float *ref_l
     if (misaligned(ref_logp, 4) || misaligned(scores, 4) || misaligned(group_offsets, 8) || misaligned(loss, 4) ||
         misaligned(margins, 4) || misaligned(grad_logp, 4))
         return set_error(TREE_ENS_E_ARG, "a pointer is misaligned for its type");
-    if (int rc = check_workspace(workspace, workspace_bytes, preference_bytes(n_tokens, n_seqs)))
+    const PreferenceSpace space = preference_space(n_tokens, n_seqs, n_groups);
+    if (int rc = check_workspace(workspace, workspace_bytes, space.bytes))
         return rc;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Tokens in{logp, ref_logp, mask, n_tokens, seq_offsets, n_seqs};
-    const Sums sums = sums_at(workspace, n_tokens, n_seqs);
-    float *weights = reinterpret_cast<float *>(static_cast<char *>(workspace) + sums_bytes(n_tokens, n_seqs));
+    char *const at = static_cast<char *>(workspace);
+    const Sums<int> sums = sums_at<int>(at + space.sums, n_tokens, n_seqs);
+    int2 *bounds = reinterpret_cast<int2 *>(at + space.bounds);
+    float *weights = reinterpret_cast<float *>(at + space.weights);
+    Loss *partial = reinterpret_cast<Loss *>(at + space.partial);
     const Preference p{scores, group_offsets, n_groups, beta, smoothing, grad_scale, (flags & TREE_ENS_SEQ_MEAN) != 0,
                        loss, margins, weights};
+    const PreferencePlan plan = preference_plan(n_tokens, n_seqs, n_groups);
+    const bool fused = plan.by == Pairs::kFused;
+    const auto blocks = [](int64_t items, int64_t per_block) { return dim3(blocks_for((items + per_block - 1) / per_block)); };
     (void)hipGetLastError();
-    if (n_seqs > 0 && n_tokens > 0)
-        hipLaunchKernelGGL(ratio_tile_kernel, dim3(blocks_for(tiles_of(n_tokens))), dim3(kThreads), 0, s, in, sums);
-    if (n_seqs > 0 || n_groups > 0)
-        hipLaunchKernelGGL(pairs_kernel, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, sums, p);
-    if (grad_logp && n_tokens > 0) {
+    if (!fused && n_seqs > 0 && n_tokens > 0)
+        hipLaunchKernelGGL(ratio_tile_kernel, blocks(n_tokens, kTile), dim3(kThreads), 0, s, in, sums, bounds);
+    if (fused) {
+        hipLaunchKernelGGL(pairs_kernel<true>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, sums, p, grad_logp);
+    } else if (plan.by == Pairs::kFew) {
+        hipLaunchKernelGGL(pairs_few_kernel, blocks(n_groups, kThreads / kFew), dim3(kThreads), 0, s, in, sums, p);
+    } else if (plan.by == Pairs::kParts) {
+        hipLaunchKernelGGL(join_kernel, blocks(n_seqs, kThreads), dim3(kThreads), 0, s, in, sums, p);
+        hipLaunchKernelGGL(pairs_part_kernel, dim3(blocks_for(n_groups * plan.parts)), dim3(kThreads), 0, s, n_seqs, p, plan.parts,
+                           partial);
+        hipLaunchKernelGGL(pairs_finish_kernel, blocks(n_groups, kWaves), dim3(kThreads), 0, s, n_seqs, p, plan.parts, partial);
+    } else if (n_seqs > 0 || n_groups > 0) {
+        hipLaunchKernelGGL(pairs_kernel<false>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, sums, p, nullptr);
+    }
+    if (!fused && grad_logp && n_tokens > 0) {
         if (n_seqs > 0)
-            hipLaunchKernelGGL(spread_tile_kernel, dim3(blocks_for(tiles_of(n_tokens))), dim3(kThreads), 0, s, in, weights, grad_logp);
+            hipLaunchKernelGGL(spread_tile_kernel, blocks(n_tokens, kTile), dim3(kThreads), 0, s, in, bounds, weights, grad_logp);
         else
-            hipLaunchKernelGGL(zero_kernel, dim3(blocks_for((n_tokens + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
-                               grad_logp, n_tokens);
+            hipLaunchKernelGGL(zero_kernel, blocks(n_tokens, kThreads), dim3(kThreads), 0, s, grad_logp, n_tokens);
     }
     return launched("preference loss");
 }

@@ -360,3 +360,25 @@ def test_argument_errors(T):
         T.tree_ens_policy_loss(lp, None, scores, seqs, kl_coef=0.1)
     with pytest.raises(T.TreeEnsError):
         T.tree_ens_group_advantage(scores, groups, eps=0.0)
+
+
+@pytest.mark.parametrize("groups,sizes,length", [
+    (300, [2], (1, 60)), (700, [1, 2, 6], (0, 30)),            # one kernel
+    (6_000, [2], (1, 40)), (900, [8, 1, 40, 3], (0, 20)),      # few candidates a group, larger ones among them
+    (120, [40, 90, 3], (0, 60)), (1, [64], (1, 9)),            # a workgroup a group
+    (9, [700, 300, 511, 512, 513], (0, 12)), (2, [1030], (1, 5)), (1, [2100], (1, 3)), (4, [97], (0, 4_000)),  # parts of one
+    (30, [600, 2, 31, 1], (0, 9)),                             # groups that differ widely
+])
+def test_every_way_to_meet_the_pairs(T, groups, sizes, length):
+    rng = np.random.default_rng([groups, len(sizes)])
+    goff = np.concatenate([[0], np.cumsum(np.resize(sizes, groups))]).astype(np.int64)
+    n_seqs = int(goff[-1])
+    seqs = np.concatenate([[0], np.cumsum(rng.integers(length[0], length[1] + 1, n_seqs))]).astype(np.int64)
+    n = int(seqs[-1])
+    lp = -rng.exponential(size=n).astype(np.float32)
+    ref = (lp + rng.normal(0, 0.3, n)).astype(np.float32)
+    mask = rng.random(n) < 0.8
+    scores = (np.round(rng.normal(size=n_seqs) * 8) / 8).astype(np.float32)
+    scores[rng.random(n_seqs) < 0.01] = np.nan
+    for smoothing, mean in ((0.0, False), (0.2, True)):
+        _check_preference(T, seqs, lp, ref, mask, scores, goff, 0.2, smoothing, 1.0, mean, f"{groups} of {sizes}")
