@@ -9,6 +9,7 @@
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "status.hpp"
 #include "tree_ens.h"
@@ -50,16 +51,6 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-// Zero what lies before the first and after the last of n segments (all of it without any).
-__device__ __forceinline__ void zero_outside(float *out, int64_t size, const int64_t *offsets, int64_t i, int64_t n, Span s) {
-    if (i == 0)
-        for (int64_t t = threadIdx.x; t < s.a; t += kThreads)
-            out[t] = 0.0f;
-    if (i == n - 1)
-        for (int64_t t = s.b + threadIdx.x; t < size; t += kThreads)
-            out[t] = 0.0f;
-}
-
 __global__ void __launch_bounds__(kThreads) zero_kernel(float *out, int64_t size) {
     for (int64_t t = blockIdx.x * int64_t(kThreads) + threadIdx.x; t < size; t += int64_t(gridDim.x) * kThreads)
         out[t] = 0.0f;
@@ -71,140 +62,30 @@ struct Tokens {
     int64_t n;
     const int64_t *offsets;
     int64_t n_seqs;
-    __device__ __forceinline__ bool counts(int64_t t) const { return !mask || mask[t]; }
 };
-
-// ---------------------------------------------------------------------------------------------
-// Tiles of tokens
-//
-// Sums over sequences of any lengths read the tokens in tiles of equal size, neighbours a thread,
-// so no workgroup waits for a long sequence. A thread finds the sequence of its first token by search
-// and walks on; what a sequence leaves open at a thread's end is carried to the next one by a segmented
-// scan over the workgroup. A sequence inside one tile has its sum stored by the tile; one that goes on
-// leaves the tile's `tail` where it begins and `head` in every later tile, added up afterwards in order.
-// ---------------------------------------------------------------------------------------------
-constexpr int kEach = 16;
-constexpr int kTile = kThreads * kEach;
 
 template <typename B> struct Pair {
     double a;
     B b;
 };
-template <typename B> __device__ __forceinline__ Pair<B> operator+(Pair<B> x, Pair<B> y) { return {x.a + y.a, x.b + y.b}; }
-
-// Two sums per sequence and two per tile.
-template <typename B> struct Sums {
-    Pair<B> *inside; // [n_seqs], of sequences inside one tile
-    Pair<B> *head;   // [tiles]
-    Pair<B> *tail;   // [tiles]
-};
-
-// The sequences of a tile's first and last token: the last s in [-1, n_seqs] with offsets[s] <= the
-// token (-1: none), by one wave with 64 pivots at a time. Offsets that decrease give some indices of the
-// range.
-__device__ __forceinline__ int2 sequences_of(const int64_t *offsets, int n_seqs, int64_t first, int64_t last) {
-    unsigned lo[2] = {0, 0}, hi[2] = {unsigned(n_seqs) + 2, unsigned(n_seqs) + 2}; // from -1 on
-    const unsigned lane = threadIdx.x % kWave + 1;
-    while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1) { // offsets[lo - 1] <= the token < offsets[hi - 1]
-        unsigned step[2];
-        bool before[2] = {false, false};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            step[e] = (hi[e] - lo[e] + kWave) / (kWave + 1);
-            // in 64 bits: the pivots beyond hi may pass 32
-            const uint64_t p = lo[e] + uint64_t(lane) * step[e];
-            if (p < hi[e])
-                before[e] = offsets[p - 1] <= (e ? last : first);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            lo[e] += unsigned(__popcll(__ballot(before[e]))) * step[e];
-            hi[e] = step[e] < hi[e] - lo[e] ? lo[e] + step[e] : hi[e];
-        }
-    }
-    return make_int2(int(lo[0]) - 1, int(lo[1]) - 1);
-}
-
-// The sequence of a token, while the token moves on inside a tile. Positions count from the tile's
-// first token, sequences from that token's; those without one (before the first, after the last
-// sequence) have indices outside [0, n_seqs) too.
-constexpr int kStaged = 512; // offsets of a tile that are held in LDS
-struct Walk {
-    const int64_t *offsets;
-    const int *staged; // offsets of the tile's sequences, within [-1, count]
-    int64_t n_seqs, first, s0;
-    int last, count; // last: the sequence of the tile's last token
-    bool goes_on;    // past the tile
-    int s, end;
-    __device__ __forceinline__ int64_t sequence() const { return s0 + s; }
-    __device__ __forceinline__ bool inside() const { return sequence() >= 0 && sequence() < n_seqs; }
-    __device__ __forceinline__ int fetch(int i) const { // where sequence i begins
-        if (s0 + i < 0)
-            return first == 0 ? 0 : -1;
-        if (s0 + i > n_seqs)
-            return count;
-        return int(max(int64_t(-1), min(max(offsets[s0 + i], int64_t(0)) - first, int64_t(count))));
-    }
-    __device__ __forceinline__ int start_of(int i) const { return i < kStaged ? staged[i] : fetch(i); }
-    // s: a sequence at or before that of t
-    __device__ __forceinline__ void place(int t) {
-        int lo = s, hi = last;
-        while (lo < hi) {
-            const int mid = lo + (hi - lo + 1) / 2;
-            if (start_of(mid) <= t)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        s = lo;
-        end = s < last ? start_of(s + 1) : goes_on ? INT32_MAX : count;
-    }
-};
-
-// Called by every thread of the workgroup; `q`: the sequences of the tile's first and last token.
-__device__ __forceinline__ Walk walk_of(const Tokens &in, int64_t first, int64_t count, int2 q, int *staged) {
-    Walk w{in.offsets, staged, in.n_seqs, first, q.x, max(q.y - q.x, 0), int(count), true, 0, 0};
-    const int64_t at = w.s0 + w.last;
-    if (at >= 0 && at < in.n_seqs)
-        w.goes_on = min(in.offsets[at + 1], in.n) > first + count;
-    __syncthreads(); // the tile before has been walked
-    for (int i = threadIdx.x; i <= w.last && i < kStaged; i += kThreads)
-        staged[i] = w.fetch(i);
-    __syncthreads();
-    return w;
-}
 
 typedef float float4_ __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned unsigned_ __attribute__((aligned(1)));
 
-// A thread's tokens [t, t + count) of an array.
-template <int E> __device__ __forceinline__ void load_tokens(const float *p, int64_t t, int count, float (&x)[E]) {
-    if (count == E) {
-#pragma unroll
-        for (int v = 0; v < E; v += 4) {
-            const float4_ a = *reinterpret_cast<const float4_ *>(p + t + v);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                x[v + k] = a[k];
-        }
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < E; ++k)
-        x[k] = k < count ? p[t + k] : 0.0f;
-}
+constexpr int kFour = 4; // neighbouring tokens that a thread takes at a time
 
-template <int E> __device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, const float (&x)[E]) {
-    if (count == E) {
+// Tokens [t, t + 4) of an array of n, 0 beyond its end.
+__device__ __forceinline__ void load_tokens(const float *p, int64_t t, int64_t n, float (&x)[kFour]) {
+    if (t + kFour <= n) {
+        const float4_ a = *reinterpret_cast<const float4_ *>(p + t);
 #pragma unroll
-        for (int v = 0; v < E; v += 4)
-            *reinterpret_cast<float4_ *>(p + t + v) = float4_{x[v], x[v + 1], x[v + 2], x[v + 3]};
+        for (int k = 0; k < kFour; ++k)
+            x[k] = a[k];
         return;
     }
 #pragma unroll
-    for (int k = 0; k < E; ++k)
-        if (k < count)
-            p[t + k] = x[k];
+    for (int k = 0; k < kFour; ++k)
+        x[k] = t + k < n ? p[t + k] : 0.0f;
 }
 
 // Bit k: byte k of x is not 0.
@@ -213,172 +94,122 @@ __device__ __forceinline__ unsigned nonzero_bytes(unsigned x) {
     return ((high >> 7) * 0x10204080u) >> 28;
 }
 
-// Bit k: token t + k counts.
-template <int E> __device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, int count) {
-    if (count <= 0)
-        return 0u;
-    const unsigned all = (1u << count) - 1;
+// A byte for each of the four tokens, not 0 where it counts; tokens beyond the end of the array count as
+// the caller says.
+__device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, int64_t n) {
     if (!mask)
-        return all;
-    unsigned bits = 0;
-    if (count == E) {
-#pragma unroll
-        for (int v = 0; v < E; v += 4)
-            bits |= nonzero_bytes(*reinterpret_cast<const unsigned_ *>(mask + t + v)) << v;
-        return bits;
+        return ~0u;
+    if (t + kFour <= n)
+        return *reinterpret_cast<const unsigned_ *>(mask + t);
+    unsigned x = 0;
+    for (int k = 0; t + k < n; ++k)
+        x |= unsigned(mask[t + k]) << (8 * k);
+    return x;
+}
+
+__device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, const float (&x)[kFour]) {
+    if (count == kFour) {
+        *reinterpret_cast<float4_ *>(p + t) = float4_{x[0], x[1], x[2], x[3]};
+        return;
     }
-    for (int k = 0; k < count; ++k)
-        bits |= unsigned(mask[t + k] != 0) << k;
-    return bits;
-}
-
-// Lanes' values moved by a DPP control; 0 where no lane is the source.
-template <int kControl, int kRows> __device__ __forceinline__ int moved(int x) {
-    return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xf, false);
-}
-template <int kControl, int kRows> __device__ __forceinline__ double moved(double x) {
-    const long long u = __double_as_longlong(x);
-    const unsigned lo = unsigned(moved<kControl, kRows>(int(u))), hi = unsigned(moved<kControl, kRows>(int(u >> 32)));
-    return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
-}
-
-// One step of an inclusive scan over the wave that starts again wherever a sequence ended.
-template <int kControl, int kRows, typename B> __device__ __forceinline__ void scan_step(Pair<B> &run, int &stop) {
-    const Pair<B> p{moved<kControl, kRows>(run.a), moved<kControl, kRows>(run.b)};
-    const int q = moved<kControl, kRows>(stop);
-    if (!stop)
-        run = p + run;
-    stop |= q;
-}
-
-// Adds up the tile's tokens by sequence: x and, counted, y (one of them per token if it has none).
-// Stores the sums. Tokens that do not count hold 0.
-template <typename B, typename Y>
-__device__ __forceinline__ void sum_tile(const Sums<B> &out, int64_t tile, Walk w, float (&x)[kEach], Y &&y) {
-    __shared__ Pair<B> part[kWaves];
-    __shared__ int closed[kWaves];
-    const int t = threadIdx.x * kEach, count = min(kEach, w.count - t);
-    Pair<B> open{0, 0}, head{0, 0}; // of the sequence being walked; of the one that the thread began in
-    int ended = 0;                  // some sequence ended in this thread
-    int64_t head_s = -1;            // the one that the thread began in, if it ends here
-    bool head_before = false;       // and began before the tile
-    if (count > 0) {
-        w.place(t);
-        const int start = w.start_of(w.s);
-        bool own = start >= t; // the walked sequence began in this thread
-        const auto close = [&] {
-            if (w.inside()) {
-                if (own) {
-                    out.inside[w.sequence()] = open;
-                } else {
-                    head = open;
-                    head_s = w.sequence();
-                    head_before = start < 0;
-                }
-            }
-            open = {0, 0};
-            ended = 1;
-            own = true;
-        };
-        int k = 0;
-        while (t + count > w.end) { // some tokens are the next sequence's
-            const int to = w.end - t;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                open.a += i < to ? x[i] : 0.0f;
-                x[i] = i < to ? 0.0f : x[i];
-            }
-            open.b = y(k, to);
-            close();
-            k = to;
-            w.s += 1;
-            w.place(t + to);
+    for (int k = 0; k < kFour; ++k)
+        if (k < count)
+            p[t + k] = x[k];
+}
+
+// ---------------------------------------------------------------------------------------------
+// Sequences, by groups of threads
+//
+// kGroup neighbouring threads take a sequence, four neighbouring tokens a thread at a time. Sequences
+// much longer than the group is made for are left to the whole workgroup afterwards, so that none keeps
+// a few lanes busy alone. A workgroup's sequence may be one of `parts` parts of it.
+// ---------------------------------------------------------------------------------------------
+constexpr int kTurns = 16; // a group takes at most so many times four tokens a thread
+
+template <int kN> struct Lanes {
+    int id;
+    // Sum over the group, in a fixed order, for each of its threads.
+    template <typename T> __device__ __forceinline__ T sum(T v) const {
+        if constexpr (kN == kThreads)
+            return T(block_sum(double(v)));
+        for (int off = kN / 2; off; off >>= 1)
+            v += __shfl_xor(v, off);
+        return v;
+    }
+    // For this thread's fours of a span, kAhead at a time: load(k, t) for each, then use(k, t, count).
+    template <int kAhead, typename Load, typename Use> __device__ __forceinline__ void each(Span q, Load &&load, Use &&use) const {
+        constexpr int kStep = kN * kFour;
+        for (int64_t t0 = q.a + id * kFour; t0 < q.b; t0 += kAhead * kStep) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (t0 + k * kStep < q.b)
+                    load(k, t0 + k * kStep);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (t0 + k * kStep < q.b)
+                    use(k, t0 + k * kStep, int(min(int64_t(kFour), q.b - t0 - k * kStep)));
         }
-#pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            open.a += x[i];
-        open.b = y(k, count);
-        if (t + count == w.end)
-            close();
     }
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    Pair<B> run = open;
-    int stop = ended;
-    scan_step<0x111, 0xf>(run, stop); // row_shr 1, 2, 4, 8: within 16 lanes
-    scan_step<0x112, 0xf>(run, stop);
-    scan_step<0x114, 0xf>(run, stop);
-    scan_step<0x118, 0xf>(run, stop);
-    scan_step<0x142, 0xa>(run, stop); // row_bcast 15: into the second and fourth 16
-    scan_step<0x143, 0xc>(run, stop); // row_bcast 31: into the upper 32
-    __syncthreads();                  // the tile before has been read
-    if (lane == kWave - 1) {
-        part[wave] = run;
-        closed[wave] = stop;
-    }
-    __syncthreads();
-    Pair<B> carry{__shfl_up(run.a, 1), __shfl_up(run.b, 1)};
-    int stopped = __shfl_up(stop, 1);
-    if (lane == 0) {
-        carry = {0, 0};
-        stopped = 0;
-    }
-    for (int k = wave - 1; k >= 0 && !stopped; --k) {
-        carry = part[k] + carry;
-        stopped = closed[k];
-    }
-    if (head_s >= 0)
-        (head_before ? out.head[tile] : out.inside[head_s]) = carry + head;
-    w.s = w.last;
-    if (threadIdx.x == kThreads - 1 && w.goes_on && w.inside())
-        (w.start_of(w.s) < 0 ? out.head : out.tail)[tile] = ended ? open : carry + open;
+};
+
+// Which of `count` tokens count, as bits.
+__device__ __forceinline__ unsigned counted_bits(unsigned mask, int count) { return nonzero_bytes(mask) & ((1u << count) - 1); }
+
+// Part `part` of `parts` of a span, in whole fours.
+__device__ __forceinline__ Span part_of(Span q, int part, int parts) {
+    const int64_t each = ((q.b - q.a + parts - 1) / parts + kFour - 1) / kFour * kFour;
+    const int64_t a = min(q.a + part * each, q.b);
+    return {a, min(a + each, q.b)};
 }
 
-// The sums of a sequence, from the tiles.
-template <typename B> __device__ __forceinline__ Pair<B> joined(const Sums<B> &in, int64_t s, Span q) {
-    if (q.a == q.b)
-        return {0, 0};
-    const int64_t first = q.a / kTile, last = (q.b - 1) / kTile;
-    if (first == last)
-        return in.inside[s];
-    Pair<B> sum = in.tail[first];
-#pragma unroll 4
-    for (int64_t k = first + 1; k <= last; ++k)
-        sum = sum + in.head[k];
-    return sum;
+// Calls body(lanes, s, span, part) for every sequence; parts > 1 with whole workgroups only.
+template <int kGroup, typename Body> __device__ __forceinline__ void for_sequences(const Tokens &in, int parts, Body &&body) {
+    constexpr int kSeqs = kThreads / kGroup;
+    if constexpr (kSeqs == 1) {
+        const Lanes<kThreads> lanes{int(threadIdx.x)};
+        for (int64_t item = blockIdx.x; item < in.n_seqs * parts; item += gridDim.x) {
+            const int64_t s = parts > 1 ? item / parts : item;
+            const int part = int(item - s * parts);
+            const Span q = span_of(in.offsets, s, in.n);
+            body(lanes, s, parts > 1 ? part_of(q, part, parts) : q, part);
+        }
+    } else {
+        for (int64_t s0 = blockIdx.x * int64_t(kSeqs); s0 < in.n_seqs; s0 += int64_t(gridDim.x) * kSeqs) {
+            const int64_t s = s0 + threadIdx.x / kGroup;
+            Span q{0, 0};
+            if (s < in.n_seqs)
+                q = span_of(in.offsets, s, in.n);
+            const bool rest = q.b - q.a > kGroup * kFour * kTurns;
+            if (s < in.n_seqs && !rest)
+                body(Lanes<kGroup>{int(threadIdx.x % kGroup)}, s, q, 0);
+            if (!__syncthreads_or(rest))
+                continue;
+            for (int64_t i = s0; i < min(s0 + kSeqs, in.n_seqs); ++i) {
+                const Span r = span_of(in.offsets, i, in.n);
+                if (r.b - r.a > kGroup * kFour * kTurns)
+                    body(Lanes<kThreads>{int(threadIdx.x)}, i, r, 0);
+            }
+        }
+    }
+}
+
+// Zero the gradient of tokens before the first and after the last sequence, by the first workgroups.
+__device__ __forceinline__ void zero_outside(const Tokens &in, float *grad) {
+    const unsigned blocks = min(gridDim.x, 64u);
+    if (blockIdx.x >= blocks)
+        return;
+    const int64_t a = span_of(in.offsets, 0, in.n).a, b = span_of(in.offsets, in.n_seqs - 1, in.n).b;
+    const int64_t at = blockIdx.x * int64_t(kThreads) + threadIdx.x, step = int64_t(blocks) * kThreads;
+    for (int64_t t = at; t < a; t += step)
+        grad[t] = 0.0f;
+    for (int64_t t = b + at; t < in.n; t += step)
+        grad[t] = 0.0f;
 }
 
 // ---------------------------------------------------------------------------------------------
 // Preference loss
 // ---------------------------------------------------------------------------------------------
-
-// Sums of a sequence's log ratios, and how many count; and the tiles' sequences, for spread_tile_kernel.
-__global__ void __launch_bounds__(kThreads) ratio_tile_kernel(Tokens in, Sums<int> out, int2 *bounds) {
-    __shared__ int staged[kStaged];
-    const int64_t tiles = (in.n + kTile - 1) / kTile;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t first = tile * kTile, size = min(int64_t(kTile), in.n - first), t = first + threadIdx.x * kEach;
-        const int count = int(min(int64_t(kEach), in.n - t));
-        float x[kEach], r[kEach] = {};
-        load_tokens(in.logp, t, count, x);
-        if (in.ref)
-            load_tokens(in.ref, t, count, r);
-        const unsigned use = load_mask<kEach>(in.mask, t, count);
-        __shared__ int2 found;
-        if (threadIdx.x < kWave) {
-            const int2 q = sequences_of(in.offsets, int(in.n_seqs), first, first + size - 1);
-            if (threadIdx.x == 0)
-                bounds[tile] = found = q;
-        }
-        __syncthreads();
-        const int2 q = found;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k)
-            x[k] = use >> k & 1u ? x[k] - r[k] : 0.0f;
-        sum_tile(out, tile, walk_of(in, first, size, q, staged), x,
-                 [&](int k, int to) { return __popc(use & (2u << (to - 1)) - (1u << k)); });
-    }
-}
-
 struct Preference {
     const float *scores;
     const int64_t *groups;
@@ -386,46 +217,88 @@ struct Preference {
     float beta, smoothing, grad_scale;
     bool mean;
     float *loss, *margins, *weights; // weights: dh / dlogp of a counted token, then the loss's gradient
+    // The margin and weight of a sequence with this sum of log ratios and so many counted tokens.
+    __device__ __forceinline__ void take(int64_t s, Pair<int> v) const {
+        const double w = mean ? double(beta) / max(v.b, 1) : double(beta);
+        margins[s] = float(w * v.a);
+        weights[s] = float(w);
+    }
 };
 
-constexpr int kFour = 4; // neighbours that a lane takes of a sequence that is its wave's
-
-// Sum of a sequence's log ratios and how many count, by a wave.
-__device__ __forceinline__ Pair<int> ratios_of(const Tokens &in, Span q) {
+// Sum of a span's log ratios and how many count, over a group's threads.
+template <int kN> __device__ __forceinline__ Pair<int> ratios_of(const Tokens &in, Lanes<kN> lanes, Span q) {
+    constexpr int kAhead = 4;
     double sum = 0.0;
     int counted = 0;
-#pragma unroll 2
-    for (int64_t t = q.a + threadIdx.x % kWave * kFour; t < q.b; t += kWave * kFour) {
-        const int count = int(min(int64_t(kFour), q.b - t));
-        float x[kFour], r[kFour] = {};
-        load_tokens(in.logp, t, count, x);
-        if (in.ref)
-            load_tokens(in.ref, t, count, r);
-        const unsigned use = load_mask<kFour>(in.mask, t, count);
+    float x[kAhead][kFour], r[kAhead][kFour] = {};
+    unsigned mask[kAhead];
+    lanes.template each<kAhead>(
+        q,
+        [&](int k, int64_t t) {
+            load_tokens(in.logp, t, in.n, x[k]);
+            if (in.ref)
+                load_tokens(in.ref, t, in.n, r[k]);
+            mask[k] = load_mask(in.mask, t, in.n);
+        },
+        [&](int k, int64_t, int count) {
+            const unsigned use = counted_bits(mask[k], count);
 #pragma unroll
-        for (int k = 0; k < kFour; ++k)
-            sum += use >> k & 1u ? x[k] - r[k] : 0.0f;
-        counted += __popc(use);
-    }
-    return {wave_sum(sum), wave_sum(counted)};
+            for (int i = 0; i < kFour; ++i)
+                sum += use >> i & 1u ? x[k][i] - r[k][i] : 0.0f;
+            counted += __popc(use);
+        });
+    return {lanes.sum(sum), lanes.sum(counted)};
 }
 
-// The gradient at a sequence's tokens, by a wave.
-__device__ __forceinline__ void spread(const Tokens &in, Span q, float weight, float *grad) {
-    for (int64_t t = q.a + threadIdx.x % kWave * kFour; t < q.b; t += kWave * kFour) {
-        const int count = int(min(int64_t(kFour), q.b - t));
-        const unsigned use = load_mask<kFour>(in.mask, t, count);
-        float d[kFour];
+// The gradient at a span's tokens.
+template <int kN> __device__ __forceinline__ void spread(const Tokens &in, Lanes<kN> lanes, Span q, float weight, float *grad) {
+    constexpr int kAhead = 4;
+    unsigned mask[kAhead];
+    lanes.template each<kAhead>(
+        q, [&](int k, int64_t t) { mask[k] = load_mask(in.mask, t, in.n); },
+        [&](int k, int64_t t, int count) {
+            const unsigned use = counted_bits(mask[k], count);
+            float d[kFour];
 #pragma unroll
-        for (int k = 0; k < kFour; ++k)
-            d[k] = use >> k & 1u ? weight : 0.0f;
-        store_tokens(grad, t, count, d);
+            for (int i = 0; i < kFour; ++i)
+                d[i] = use >> i & 1u ? weight : 0.0f;
+            store_tokens(grad, t, count, d);
+        });
+}
+
+// Margins and weights, or with several parts what each adds to them.
+template <int kGroup>
+__global__ void __launch_bounds__(kThreads) margin_kernel(Tokens in, Preference p, int parts, Pair<int> *partial) {
+    for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
+        const Pair<int> v = ratios_of(in, lanes, q);
+        if (lanes.id != 0)
+            return;
+        if (parts > 1)
+            partial[s * parts + part] = v;
+        else
+            p.take(s, v);
+    });
+}
+
+// Margins and weights from the parts, a wave a sequence.
+__global__ void __launch_bounds__(kThreads) margin_join_kernel(int64_t n_seqs, Preference p, int parts, const Pair<int> *partial) {
+    const Lanes<kWave> lanes{int(threadIdx.x % kWave)};
+    for (int64_t s = blockIdx.x * int64_t(kWaves) + threadIdx.x / kWave; s < n_seqs; s += int64_t(gridDim.x) * kWaves) {
+        Pair<int> v{0.0, 0};
+        for (int k = lanes.id; k < parts; k += kWave) {
+            v.a += partial[s * parts + k].a;
+            v.b += partial[s * parts + k].b;
+        }
+        v = {lanes.sum(v.a), lanes.sum(v.b)};
+        if (lanes.id == 0)
+            p.take(s, v);
     }
 }
 
-__device__ __forceinline__ void spread_zero(float *grad, int64_t a, int64_t b) {
-    for (int64_t t = a + threadIdx.x % kWave; t < b; t += kWave)
-        grad[t] = 0.0f;
+// grad[t] = the sequence's weight at its counted tokens.
+template <int kGroup> __global__ void __launch_bounds__(kThreads) spread_kernel(Tokens in, const float *weights, int parts, float *grad) {
+    for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int) { spread(in, lanes, q, weights[s], grad); });
+    zero_outside(in, grad);
 }
 
 constexpr int kHeld = 512; // candidates of a group that are held in LDS
@@ -504,45 +377,47 @@ __device__ __forceinline__ float meet_window(float2 me, const float2 *held, int 
     return slope;
 }
 
+// Sequences outside every group have no gradient: those before the first and after the last group, for the
+// kernels that meet the pairs.
+__device__ __forceinline__ void clear_outside(const Preference &p, int64_t n_seqs, int64_t g, Span q, int id, int step) {
+    if (g == 0)
+        for (int64_t s = id; s < q.a; s += step)
+            p.weights[s] = 0.0f;
+    if (g == p.n_groups - 1)
+        for (int64_t s = q.b + id; s < n_seqs; s += step)
+            p.weights[s] = 0.0f;
+}
+
 // Loss of a group, and weights times the loss's gradient with respect to the margins, by a workgroup.
 // kFused: it also sums the sequences' tokens first and writes their gradients last, instead of the tile
 // kernels.
 template <bool kFused>
-__global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Sums<int> sums, Preference p, float *grad) {
+__global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p, float *grad) {
     __shared__ float2 held[2 * kHeld];
     __shared__ float slopes[kWaves][kHeld];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    for (int64_t g = blockIdx.x; g < max(p.n_groups, int64_t(1)); g += gridDim.x) {
-        Span q{in.n_seqs, in.n_seqs}; // without groups, every sequence is before the first one
-        if (p.n_groups > 0)
-            q = span_of(p.groups, g, in.n_seqs);
-        // sequences outside every group go with the first and the last one; their gradient is 0
-        const int64_t lo = g == 0 ? 0 : q.a, hi = g >= p.n_groups - 1 ? in.n_seqs : q.b;
+    const int wave = threadIdx.x / kWave;
+    const Lanes<kWave> lanes{int(threadIdx.x % kWave)};
+    for (int64_t g = blockIdx.x; g < p.n_groups; g += gridDim.x) {
+        const Span q = span_of(p.groups, g, in.n_seqs);
         const int64_t n = q.b - q.a;
-        __syncthreads(); // held may still be read for the group before
-        const auto take = [&](int64_t s, Pair<int> v) {
-            const double w = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
-            const float h = float(w * v.a);
-            p.margins[s] = h;
-            p.weights[s] = s < q.a || s >= q.b ? 0.0f : float(w);
-            if (n <= kHeld && s >= q.a && s < q.b)
-                held[s - q.a] = held[s - q.a + n] = make_float2(h * kLog2e, p.scores[s]);
-        };
+        // fused, sequences outside every group go with the first and the last one
+        const int64_t lo = g == 0 ? 0 : q.a, hi = g == p.n_groups - 1 ? in.n_seqs : q.b;
         if constexpr (kFused) {
             for (int64_t s = lo + wave; s < hi; s += kWaves) {
-                const Pair<int> v = ratios_of(in, span_of(in.offsets, s, in.n));
-                if (lane == 0)
-                    take(s, v);
+                const Pair<int> v = ratios_of(in, lanes, span_of(in.offsets, s, in.n));
+                if (lanes.id == 0)
+                    p.take(s, v);
             }
-        } else {
-            for (int64_t s = lo + threadIdx.x; s < hi; s += kThreads)
-                take(s, joined(sums, s, span_of(in.offsets, s, in.n)));
+            __syncthreads();
         }
-        __syncthreads();
+        clear_outside(p, in.n_seqs, g, q, threadIdx.x, kThreads);
         Loss loss{0.0, 0.0};
         if (n <= kHeld) {
+            for (int i = threadIdx.x; i < n; i += kThreads)
+                held[i] = held[i + n] = make_float2(p.margins[q.a + i] * kLog2e, p.scores[q.a + i]);
+            __syncthreads();
             // waves take steps in turn and leave their slopes in rows of their own
-            for (int i = lane; i < n; i += kWave)
+            for (int i = lanes.id; i < n; i += kWave)
                 slopes[wave][i] = meet_held(held, int(n), i, wave, kWaves, p.smoothing, loss);
             __syncthreads();
             for (int i = threadIdx.x; i < n; i += kThreads) {
@@ -572,35 +447,20 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Sums<int> su
         loss.sum = block_sum(loss.sum);
         loss.pairs = block_sum(loss.pairs);
         const double share = 1.0 / fmax(loss.pairs, 1.0);
-        if (threadIdx.x == 0 && p.n_groups > 0)
+        if (threadIdx.x == 0)
             p.loss[g] = float(loss.sum * (kLn2 * share));
         __syncthreads();
-        if constexpr (kFused) {
-            if (!grad)
-                continue;
-            for (int64_t s = lo + wave; s < hi; s += kWaves) {
-                const Span t = span_of(in.offsets, s, in.n);
-                spread(in, t, float(p.weights[s] * (p.grad_scale * share)), grad);
-                if (s == 0)
-                    spread_zero(grad, 0, t.a);
-                if (s == in.n_seqs - 1)
-                    spread_zero(grad, t.b, in.n);
-            }
-        } else {
-            for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
-                p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
-        }
+        for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
+            p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
+        __syncthreads(); // held and slopes are free, weights are there
+        if constexpr (kFused)
+            if (grad)
+                for (int64_t s = lo + wave; s < hi; s += kWaves)
+                    spread(in, lanes, span_of(in.offsets, s, in.n), p.weights[s], grad);
     }
-}
-
-// Margins and weights, a thread a sequence, where pairs_part_kernel needs them all before it starts.
-__global__ void __launch_bounds__(kThreads) join_kernel(Tokens in, Sums<int> sums, Preference p) {
-    for (int64_t s = blockIdx.x * int64_t(kThreads) + threadIdx.x; s < in.n_seqs; s += int64_t(gridDim.x) * kThreads) {
-        const Pair<int> v = joined(sums, s, span_of(in.offsets, s, in.n));
-        const double w = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
-        p.margins[s] = float(w * v.a);
-        p.weights[s] = float(w);
-    }
+    if constexpr (kFused)
+        if (grad)
+            zero_outside(in, grad);
 }
 
 constexpr int kHeldPart = 2048;
@@ -677,35 +537,21 @@ __global__ void __launch_bounds__(kThreads) pairs_finish_kernel(int64_t n_seqs, 
             p.loss[g] = float(loss.sum * (kLn2 * share));
         for (int64_t i = q.a + lane; i < q.b; i += kWave)
             p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
-        // sequences outside every group
-        if (g == 0)
-            for (int64_t i = lane; i < q.a; i += kWave)
-                p.weights[i] = 0.0f;
-        if (g == p.n_groups - 1)
-            for (int64_t i = q.b + lane; i < n_seqs; i += kWave)
-                p.weights[i] = 0.0f;
+        clear_outside(p, n_seqs, g, q, lane, kWave);
     }
 }
 
 // Groups of a few candidates: eight lanes take one. Larger ones among them are met from memory.
 constexpr int kFew = 8;
-__global__ void __launch_bounds__(kThreads) pairs_few_kernel(Tokens in, Sums<int> sums, Preference p) {
+__global__ void __launch_bounds__(kThreads) pairs_few_kernel(int64_t n_seqs, Preference p) {
     constexpr int kGroups = kThreads / kFew;
     const int lane = threadIdx.x % kFew;
     for (int64_t g0 = blockIdx.x * int64_t(kGroups); g0 < p.n_groups; g0 += int64_t(gridDim.x) * kGroups) {
         const int64_t g = g0 + threadIdx.x / kFew;
         if (g >= p.n_groups)
             continue;
-        const Span q = span_of(p.groups, g, in.n_seqs);
-        const int64_t lo = g == 0 ? 0 : q.a, hi = g == p.n_groups - 1 ? in.n_seqs : q.b;
-        for (int64_t s = lo + lane; s < hi; s += kFew) {
-            const bool member = s >= q.a && s < q.b;
-            const Pair<int> v = joined(sums, s, span_of(in.offsets, s, in.n));
-            const double by = p.mean ? double(p.beta) / max(v.b, 1) : double(p.beta);
-            p.margins[s] = float(by * v.a);
-            p.weights[s] = member ? float(by) : 0.0f;
-        }
-        __threadfence_block(); // the group's lanes are of one wave
+        const Span q = span_of(p.groups, g, n_seqs);
+        clear_outside(p, n_seqs, g, q, lane, kFew);
         Loss loss{0.0, 0.0};
         for (int64_t i = q.a + lane; i < q.b; i += kFew) {
             const float2 me = make_float2(p.margins[i] * kLog2e, p.scores[i]);
@@ -729,51 +575,9 @@ __global__ void __launch_bounds__(kThreads) pairs_few_kernel(Tokens in, Sums<int
     }
 }
 
-// Stores a tile of kEach neighbours a thread, through LDS so that a wave's stores are neighbours.
-__device__ __forceinline__ void store_tile(float *out, int64_t first, int size, const float (&d)[kEach]) {
-    constexpr int kPad = kEach + 4; // rows of other banks
-    __shared__ float rows[kThreads * kPad];
-    __syncthreads(); // the tile before has been stored
-#pragma unroll
-    for (int v = 0; v < kEach; v += 4)
-        *reinterpret_cast<float4 *>(rows + threadIdx.x * kPad + v) = make_float4(d[v], d[v + 1], d[v + 2], d[v + 3]);
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < kEach; v += 4) {
-        const int t = v * kThreads + threadIdx.x * 4;
-        const float4 q = *reinterpret_cast<const float4 *>(rows + t / kEach * kPad + t % kEach);
-        if (t + 4 <= size)
-            *reinterpret_cast<float4_ *>(out + first + t) = float4_{q.x, q.y, q.z, q.w};
-        else
-            for (int k = 0; t + k < size; ++k)
-                out[first + t + k] = rows[t / kEach * kPad + t % kEach + k];
-    }
-}
-
-// grad[t] = the sequence's weight at its counted tokens.
-__global__ void __launch_bounds__(kThreads) spread_tile_kernel(Tokens in, const int2 *bounds, const float *weights, float *grad) {
-    __shared__ int staged[kStaged];
-    const int64_t tiles = (in.n + kTile - 1) / kTile;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t first = tile * kTile;
-        const int size = int(min(int64_t(kTile), in.n - first)), t = threadIdx.x * kEach, count = min(kEach, size - t);
-        const unsigned use = load_mask<kEach>(in.mask, first + t, count);
-        Walk w = walk_of(in, first, size, bounds[tile], staged);
-        float d[kEach] = {};
-        for (int k = 0; k < count;) {
-            w.place(t + k);
-            const float x = w.inside() ? weights[w.sequence()] : 0.0f;
-            const int to = min(w.end - t, count);
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                d[i] = i >= k && use >> i & 1u ? x : d[i];
-            k = to;
-            w.s += 1;
-        }
-        store_tile(grad, first, size, d);
-    }
-}
-
+// ---------------------------------------------------------------------------------------------
+// Advantages and policy loss
+// ---------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kThreads)
 advantage_kernel(const float *scores, int64_t n, const int64_t *groups, int64_t n_groups, float eps, bool center,
                  float *out) {
@@ -790,15 +594,22 @@ advantage_kernel(const float *scores, int64_t n, const int64_t *groups, int64_t 
         const double by = center ? 1.0 : 1.0 / (std + eps);
         for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
             out[i] = float((scores[i] - mean) * by);
-        zero_outside(out, n, groups, g, n_groups, q);
+        // candidates outside every group
+        if (g == 0)
+            for (int64_t i = threadIdx.x; i < q.a; i += kThreads)
+                out[i] = 0.0f;
+        if (g == n_groups - 1)
+            for (int64_t i = q.b + threadIdx.x; i < n; i += kThreads)
+                out[i] = 0.0f;
     }
 }
+
+// exp(x), off by 2^-24 (2 + |x|) of itself.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // exp(q) - q - 1: the sum of q^k / k! from k = 2 where the difference would cancel. Below 1/2 the
 // terms up to k = 9 leave out less than 2e-9 of it.
 __device__ __forceinline__ float exp_less_tangent(float q) {
-    if (!(fabsf(q) < 0.5f))
-        return expf(q) - q - 1.0f;
     float s = 1.0f / 362880.0f;
     s = fmaf(s, q, 1.0f / 40320.0f);
     s = fmaf(s, q, 1.0f / 5040.0f);
@@ -807,7 +618,7 @@ __device__ __forceinline__ float exp_less_tangent(float q) {
     s = fmaf(s, q, 1.0f / 24.0f);
     s = fmaf(s, q, 1.0f / 6.0f);
     s = fmaf(s, q, 0.5f);
-    return s * q * q;
+    return fabsf(q) < 0.5f ? s * q * q : exp_of(q) - q - 1.0f;
 }
 
 struct Policy {
@@ -815,48 +626,129 @@ struct Policy {
     float low, high, kl_coef, grad_scale;
     bool mean;
     float *loss, *kl, *grad;
+    // The sums of a sequence's gains and of exp(q) - q - 1.
+    __device__ __forceinline__ void take(int64_t s, Pair<double> v, double share) const {
+        loss[s] = float(share * (v.a + kl_coef * v.b));
+        if (kl)
+            kl[s] = float(share * v.b);
+    }
 };
 
-__global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p) {
-    for (int64_t s = blockIdx.x; s < in.n_seqs; s += gridDim.x) {
-        const Span q = span_of(in.offsets, s, in.n);
+// Of one token: the ratio, k = exp(q) - q - 1 and dk/dq = exp(q) - 1.
+struct Terms {
+    float ratio, k, up;
+};
+__device__ __forceinline__ Terms terms_of(const Tokens &in, const Policy &p, float logp, float old, float ref) {
+    const float d = p.old_logp ? logp - old : 0.0f, q = in.ref ? ref - logp : 0.0f; // without them: 0, whatever logp is
+    const float k = exp_less_tangent(q);
+    return {exp_of(d), k, k + q};
+}
+// The clipped gain's share in the loss, and the gradient of the token's loss. Comparisons pass a NaN
+// ratio unchanged.
+__device__ __forceinline__ float policy_of(const Policy &p, const Terms &x, float a, float &slope) {
+    const float edge = a >= 0.0f ? p.high : p.low;
+    const bool clipped = a >= 0.0f ? x.ratio > edge : x.ratio < edge;
+    slope = (clipped ? 0.0f : -a * x.ratio) - p.kl_coef * x.up;
+    return -(clipped ? edge : x.ratio) * a;
+}
+
+// How many of a span's tokens count.
+template <int kN> __device__ __forceinline__ int counted_of(const Tokens &in, Lanes<kN> lanes, Span q) {
+    constexpr int kAhead = 4;
+    int count = 0;
+    unsigned mask[kAhead];
+    lanes.template each<kAhead>(
+        q, [&](int k, int64_t t) { mask[k] = load_mask(in.mask, t, in.n); },
+        [&](int k, int64_t, int some) { count += __popc(counted_bits(mask[k], some)); });
+    return lanes.sum(count);
+}
+
+// How many tokens of each part of a sequence count, for the mean over masked sequences in parts.
+__global__ void __launch_bounds__(kThreads) count_kernel(Tokens in, int parts, int *counts) {
+    for_sequences<kThreads>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
+        const int count = counted_of(in, lanes, q);
+        if (lanes.id == 0)
+            counts[s * parts + part] = count;
+    });
+}
+
+// What a sequence's loss is multiplied by, for the threads that take it (or the part q of it).
+template <int kN>
+__device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, Lanes<kN> lanes, int64_t s, Span q, int parts, const int *counts) {
+    if (!p.mean)
+        return 1.0;
+    if (!in.mask) {
+        const Span all = span_of(in.offsets, s, in.n);
+        return 1.0 / double(max(all.b - all.a, int64_t(1)));
+    }
+    if (parts == 1)
+        return 1.0 / max(counted_of(in, lanes, q), 1);
+    double count = 0.0; // of all parts
+    for (int k = lanes.id; k < parts; k += kN)
+        count += counts[s * parts + k];
+    return 1.0 / fmax(lanes.sum(count), 1.0);
+}
+
+template <int kGroup>
+__global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, int parts, const int *counts, Pair<double> *partial) {
+    for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
         const float a = p.advantages[s];
-        double share = 1.0;
-        if (p.mean) {
-            double count = 0.0;
-            for (int64_t t = q.a + threadIdx.x; t < q.b; t += kThreads)
-                count += in.counts(t) ? 1.0 : 0.0;
-            share = 1.0 / fmax(block_sum(count), 1.0);
-        }
+        const double share = share_of(in, p, lanes, s, q, parts, counts);
         const float w = float(p.grad_scale * share);
         double loss = 0.0, kl = 0.0;
-        for (int64_t t = q.a + threadIdx.x; t < q.b; t += kThreads) {
-            float d = 0.0f;
-            if (in.counts(t)) {
-                const float lp = in.logp[t];
-                const float ratio = p.old_logp ? expf(lp - p.old_logp[t]) : 1.0f;
-                // comparisons that a NaN ratio passes unchanged
-                const bool clipped = a >= 0.0f ? ratio > p.high : ratio < p.low;
-                loss -= (clipped ? (a >= 0.0f ? p.high : p.low) : ratio) * a;
-                d = clipped ? 0.0f : -a * ratio;
-                if (in.ref) {
-                    const float x = in.ref[t] - lp, k = exp_less_tangent(x);
-                    kl += k;
-                    d -= p.kl_coef * (k + x);
+        constexpr int kAhead = 2;
+        float x[kAhead][kFour], old[kAhead][kFour] = {}, ref[kAhead][kFour] = {};
+        unsigned mask[kAhead];
+        lanes.template each<kAhead>(
+            q,
+            [&](int k, int64_t t) {
+                load_tokens(in.logp, t, in.n, x[k]);
+                if (p.old_logp)
+                    load_tokens(p.old_logp, t, in.n, old[k]);
+                if (in.ref)
+                    load_tokens(in.ref, t, in.n, ref[k]);
+                mask[k] = load_mask(in.mask, t, in.n);
+            },
+            [&](int k, int64_t t, int count) {
+                const unsigned use = counted_bits(mask[k], count);
+                float d[kFour];
+#pragma unroll
+                for (int i = 0; i < kFour; ++i) {
+                    const Terms m = terms_of(in, p, x[k][i], old[k][i], ref[k][i]);
+                    const float gain = policy_of(p, m, a, d[i]);
+                    const bool counts_ = use >> i & 1u;
+                    loss += counts_ ? gain : 0.0f;
+                    kl += counts_ ? m.k : 0.0f;
+                    d[i] = counts_ ? w * d[i] : 0.0f;
                 }
-            }
-            if (p.grad)
-                p.grad[t] = w * d;
+                if (p.grad)
+                    store_tokens(p.grad, t, count, d);
+            });
+        const Pair<double> v{lanes.sum(loss), lanes.sum(kl)};
+        if (lanes.id != 0)
+            return;
+        if (parts > 1)
+            partial[s * parts + part] = v;
+        else
+            p.take(s, v, share);
+    });
+    if (p.grad)
+        zero_outside(in, p.grad);
+}
+
+// Losses from the parts, a wave a sequence.
+__global__ void __launch_bounds__(kThreads) policy_join_kernel(Tokens in, Policy p, int parts, const int *counts, const Pair<double> *partial) {
+    const Lanes<kWave> lanes{int(threadIdx.x % kWave)};
+    for (int64_t s = blockIdx.x * int64_t(kWaves) + threadIdx.x / kWave; s < in.n_seqs; s += int64_t(gridDim.x) * kWaves) {
+        Pair<double> v{0.0, 0.0};
+        for (int k = lanes.id; k < parts; k += kWave) {
+            v.a += partial[s * parts + k].a;
+            v.b += partial[s * parts + k].b;
         }
-        loss = block_sum(loss);
-        kl = block_sum(kl);
-        if (threadIdx.x == 0) {
-            p.loss[s] = float(share * (loss + p.kl_coef * kl));
-            if (p.kl)
-                p.kl[s] = float(share * kl);
-        }
-        if (p.grad)
-            zero_outside(p.grad, in.n, in.offsets, s, in.n_seqs, q);
+        v = {lanes.sum(v.a), lanes.sum(v.b)};
+        const double share = share_of(in, p, lanes, s, Span{0, 0}, parts, counts);
+        if (lanes.id == 0)
+            p.take(s, v, share);
     }
 }
 
@@ -865,6 +757,8 @@ using treeens::set_error;
 bool misaligned(const void *p, unsigned a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
 unsigned blocks_for(int64_t n) { return unsigned(std::min(std::max<int64_t>(n, 1), kMaxBlocks)); }
+
+dim3 blocks_of(int64_t items, int64_t per_block) { return dim3(blocks_for((items + per_block - 1) / per_block)); }
 
 int launched(const char *what) {
     const hipError_t e = hipGetLastError();
@@ -898,17 +792,43 @@ int check_tokens(const float *logp, int64_t n_tokens, const int64_t *seq_offsets
     return TREE_ENS_OK;
 }
 
-int64_t tiles_of(int64_t n_tokens) { return (n_tokens + kTile - 1) / kTile; }
-
-// Two sums per sequence and tile, 16 bytes each.
-int64_t sums_bytes(int64_t n_tokens, int64_t n_seqs) { return 16 * (n_seqs + 2 * tiles_of(n_tokens)); }
-int64_t bounds_bytes(int64_t n_tokens) { return 8 * tiles_of(n_tokens); }
-
-template <typename B> Sums<B> sums_at(void *workspace, int64_t n_tokens, int64_t n_seqs) {
-    static_assert(sizeof(Pair<B>) == 16, "as sums_bytes counts");
-    Pair<B> *p = static_cast<Pair<B> *>(workspace);
-    return {p, p + n_seqs, p + n_seqs + tiles_of(n_tokens)};
+// How sequences are shared out: threads for each, or parts of it. By their mean length, and more threads
+// where the sequences are too few for 2,000 waves, 8 to a CU. Measured on the policy loss (us; sequences x mean
+// tokens: 8 / 16 / 32 / 64 / 256 threads):
+//   200,000 x 24: 35 / 45 / 77 / 144 / 483; 99,000 x 49: 29 / 32 / 44 / 76 / 241; 50,000 x 98: 31 / 28 / 31 / 45 /
+//   127; 30,000 x 195: 48 / 31 / 29 / 34 / 81; 20,000 x 325: - / - / 31 / 31 / 58; 10,000 x 818: - / - / 43 / 33 / 39;
+//   4,096 x 2,030: - / - / 54 / 41 / 31; 4,000 x 24: 5.7 / 4.9 / 4.4 / 5.5 / 11.5; 2,000 x 81: 9.7 / 6.4 / 5.0 / 4.5 / 7.4.
+// In parts of a thousand tokens or more where long sequences are few (1 / 2 / 4 / 8 / 64 parts): 512 x 23,600:
+// 120 / 72 / 55 / 48 / -; 4 x 61,400: 122 / 62 / 35 / 18 / 7.2; 256 x 3,200: 15.2 / 13.4 / 11.5 / 12.5 / -; 2,048 x
+// 1,600: 18 / 22 / 29 / 46 / -.
+struct SequencePlan {
+    int group, parts;
+};
+SequencePlan sequence_plan(int64_t n_tokens, int64_t n_seqs) {
+    const double seqs = double(std::max<int64_t>(n_seqs, 1)), tokens = double(n_tokens) / seqs;
+    SequencePlan plan{tokens <= 64.0 ? 8 : tokens <= 144.0 ? 16 : tokens <= 320.0 ? 32 : tokens <= 1024.0 ? kWave : kThreads, 1};
+    while (plan.group < kThreads && seqs * plan.group < 2000.0 * kWave)
+        plan.group = plan.group == kWave ? kThreads : 2 * plan.group;
+    if (plan.group == kThreads && n_seqs <= 1024)
+        plan.parts = int(std::max(1.0, std::min(4096.0 / seqs, tokens / 1024.0)));
+    return plan;
 }
+
+// Calls f with a std::integral_constant of the group's size.
+template <typename F> void with_group(int group, F &&f) {
+    if (group == 8)
+        f(std::integral_constant<int, 8>());
+    else if (group == 16)
+        f(std::integral_constant<int, 16>());
+    else if (group == 32)
+        f(std::integral_constant<int, 32>());
+    else if (group == kWave)
+        f(std::integral_constant<int, kWave>());
+    else
+        f(std::integral_constant<int, kThreads>());
+}
+
+int64_t round_up(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 // Which kernels meet the pairs, by the mean sizes of groups and sequences. Measured (us of the whole loss;
 // groups x candidates x tokens; pairs_kernel fused / tile kernels with pairs_few_kernel / with pairs_kernel /
@@ -927,7 +847,7 @@ PreferencePlan preference_plan(int64_t n_tokens, int64_t n_seqs, int64_t n_group
     if (n_groups == 0 || n_seqs == 0)
         return {Pairs::kGroup, 1};
     const double seqs = double(n_seqs) / double(n_groups), tokens = double(n_tokens) / double(n_seqs);
-    if (seqs <= 8.0 && n_seqs <= 4096 && tokens <= 1024.0)
+    if (seqs <= 8.0 && n_seqs <= 2048 && tokens <= 512.0)
         return {Pairs::kFused, 1};
     if (seqs <= 8.0)
         return {Pairs::kFew, 1};
@@ -938,16 +858,27 @@ PreferencePlan preference_plan(int64_t n_tokens, int64_t n_seqs, int64_t n_group
 
 // Where a preference loss keeps what its kernels hand on.
 struct PreferenceSpace {
-    int64_t sums, bounds, weights, partial, bytes;
+    int64_t weights, losses, sums, bytes;
 };
 PreferenceSpace preference_space(int64_t n_tokens, int64_t n_seqs, int64_t n_groups) {
-    const PreferencePlan plan = preference_plan(n_tokens, n_seqs, n_groups);
-    const auto round = [](int64_t b) { return (b + 15) / 16 * 16; };
-    PreferenceSpace p{0, sums_bytes(n_tokens, n_seqs), 0, 0, 0};
-    p.weights = p.bounds + round(bounds_bytes(n_tokens));
-    p.partial = p.weights + round(4 * n_seqs);
-    p.bytes = p.partial + (plan.by == Pairs::kParts ? n_groups * plan.parts * int64_t(sizeof(Loss)) : 0);
+    const PreferencePlan pairs = preference_plan(n_tokens, n_seqs, n_groups);
+    const SequencePlan seqs = sequence_plan(n_tokens, n_seqs);
+    PreferenceSpace p{0, round_up(4 * n_seqs), 0, 0};
+    p.sums = p.losses + (pairs.by == Pairs::kParts ? n_groups * pairs.parts * int64_t(sizeof(Loss)) : 0);
+    p.bytes = p.sums + (seqs.parts > 1 ? n_seqs * seqs.parts * int64_t(sizeof(Pair<int>)) : 0);
     return p;
+}
+
+// Where a policy loss does, if it goes in parts.
+struct PolicySpace {
+    int64_t counts, bytes;
+};
+PolicySpace policy_space(int64_t n_tokens, int64_t n_seqs) {
+    const int64_t parts = sequence_plan(n_tokens, n_seqs).parts;
+    if (parts == 1)
+        return {0, 0};
+    const int64_t sums = n_seqs * parts * int64_t(sizeof(Pair<double>));
+    return {sums, sums + 4 * n_seqs * parts};
 }
 
 } // namespace
@@ -990,35 +921,44 @@ int tree_ens_preference_loss(void *stream, const float *logp, const float *ref_l
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Tokens in{logp, ref_logp, mask, n_tokens, seq_offsets, n_seqs};
     char *const at = static_cast<char *>(workspace);
-    const Sums<int> sums = sums_at<int>(at + space.sums, n_tokens, n_seqs);
-    int2 *bounds = reinterpret_cast<int2 *>(at + space.bounds);
     float *weights = reinterpret_cast<float *>(at + space.weights);
-    Loss *partial = reinterpret_cast<Loss *>(at + space.partial);
+    Loss *losses = reinterpret_cast<Loss *>(at + space.losses);
+    Pair<int> *sums = reinterpret_cast<Pair<int> *>(at + space.sums);
     const Preference p{scores, group_offsets, n_groups, beta, smoothing, grad_scale, (flags & TREE_ENS_SEQ_MEAN) != 0,
                        loss, margins, weights};
-    const PreferencePlan plan = preference_plan(n_tokens, n_seqs, n_groups);
-    const bool fused = plan.by == Pairs::kFused;
-    const auto blocks = [](int64_t items, int64_t per_block) { return dim3(blocks_for((items + per_block - 1) / per_block)); };
+    const PreferencePlan pairs = preference_plan(n_tokens, n_seqs, n_groups);
+    const SequencePlan seqs = sequence_plan(n_tokens, n_seqs);
+    const bool fused = pairs.by == Pairs::kFused;
     (void)hipGetLastError();
-    if (!fused && n_seqs > 0 && n_tokens > 0)
-        hipLaunchKernelGGL(ratio_tile_kernel, blocks(n_tokens, kTile), dim3(kThreads), 0, s, in, sums, bounds);
-    if (fused) {
-        hipLaunchKernelGGL(pairs_kernel<true>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, sums, p, grad_logp);
-    } else if (plan.by == Pairs::kFew) {
-        hipLaunchKernelGGL(pairs_few_kernel, blocks(n_groups, kThreads / kFew), dim3(kThreads), 0, s, in, sums, p);
-    } else if (plan.by == Pairs::kParts) {
-        hipLaunchKernelGGL(join_kernel, blocks(n_seqs, kThreads), dim3(kThreads), 0, s, in, sums, p);
-        hipLaunchKernelGGL(pairs_part_kernel, dim3(blocks_for(n_groups * plan.parts)), dim3(kThreads), 0, s, n_seqs, p, plan.parts,
-                           partial);
-        hipLaunchKernelGGL(pairs_finish_kernel, blocks(n_groups, kWaves), dim3(kThreads), 0, s, n_seqs, p, plan.parts, partial);
-    } else if (n_seqs > 0 || n_groups > 0) {
-        hipLaunchKernelGGL(pairs_kernel<false>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, sums, p, nullptr);
+    if (n_seqs > 0 && !fused) {
+        with_group(seqs.group, [&](auto group) {
+            hipLaunchKernelGGL(margin_kernel<decltype(group)::value>, blocks_of(n_seqs * seqs.parts, kThreads / seqs.group),
+                               dim3(kThreads), 0, s, in, p, seqs.parts, sums);
+        });
+        if (seqs.parts > 1)
+            hipLaunchKernelGGL(margin_join_kernel, blocks_of(n_seqs, kWaves), dim3(kThreads), 0, s, n_seqs, p, seqs.parts, sums);
     }
-    if (!fused && grad_logp && n_tokens > 0) {
-        if (n_seqs > 0)
-            hipLaunchKernelGGL(spread_tile_kernel, blocks(n_tokens, kTile), dim3(kThreads), 0, s, in, bounds, weights, grad_logp);
+    if (n_groups == 0) {
+        // no pair, no gradient
+    } else if (fused) {
+        hipLaunchKernelGGL(pairs_kernel<true>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, p, grad_logp);
+    } else if (pairs.by == Pairs::kFew) {
+        hipLaunchKernelGGL(pairs_few_kernel, blocks_of(n_groups, kThreads / kFew), dim3(kThreads), 0, s, n_seqs, p);
+    } else if (pairs.by == Pairs::kParts) {
+        hipLaunchKernelGGL(pairs_part_kernel, dim3(blocks_for(n_groups * pairs.parts)), dim3(kThreads), 0, s, n_seqs, p,
+                           pairs.parts, losses);
+        hipLaunchKernelGGL(pairs_finish_kernel, blocks_of(n_groups, kWaves), dim3(kThreads), 0, s, n_seqs, p, pairs.parts, losses);
+    } else {
+        hipLaunchKernelGGL(pairs_kernel<false>, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, in, p, nullptr);
+    }
+    if (grad_logp && n_tokens > 0 && !fused) {
+        if (n_seqs > 0 && n_groups > 0)
+            with_group(seqs.group, [&](auto group) {
+                hipLaunchKernelGGL(spread_kernel<decltype(group)::value>, blocks_of(n_seqs * seqs.parts, kThreads / seqs.group),
+                                   dim3(kThreads), 0, s, in, weights, seqs.parts, grad_logp);
+            });
         else
-            hipLaunchKernelGGL(zero_kernel, blocks(n_tokens, kThreads), dim3(kThreads), 0, s, grad_logp, n_tokens);
+            hipLaunchKernelGGL(zero_kernel, blocks_of(n_tokens, kThreads), dim3(kThreads), 0, s, grad_logp, n_tokens);
     }
     return launched("preference loss");
 }
@@ -1054,7 +994,10 @@ int tree_ens_policy_workspace(int64_t n_tokens, int64_t n_seqs, int64_t *bytes) 
     if (!bytes)
         return set_error(TREE_ENS_E_ARG, "bytes is NULL");
     *bytes = 0;
-    return check_counts(n_tokens, n_seqs, 0);
+    if (int rc = check_counts(n_tokens, n_seqs, 0))
+        return rc;
+    *bytes = policy_space(n_tokens, n_seqs).bytes;
+    return TREE_ENS_OK;
 }
 
 int tree_ens_policy_loss(void *stream, const float *logp, const float *old_logp, const float *ref_logp,
@@ -1079,18 +1022,30 @@ int tree_ens_policy_loss(void *stream, const float *logp, const float *old_logp,
     if (misaligned(old_logp, 4) || misaligned(ref_logp, 4) || misaligned(advantages, 4) || misaligned(loss, 4) ||
         misaligned(kl, 4) || misaligned(grad_logp, 4))
         return set_error(TREE_ENS_E_ARG, "a pointer is misaligned for its type");
-    (void)workspace;
-    (void)workspace_bytes;
+    const PolicySpace space = policy_space(n_tokens, n_seqs);
+    if (int rc = check_workspace(workspace, workspace_bytes, space.bytes))
+        return rc;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const Tokens in{logp, ref_logp, mask, n_tokens, seq_offsets, n_seqs};
     const Policy p{old_logp, advantages, 1.0f - clip_low, 1.0f + clip_high, kl_coef, grad_scale,
                    (flags & TREE_ENS_SEQ_MEAN) != 0, loss, kl, grad_logp};
+    const SequencePlan seqs = sequence_plan(n_tokens, n_seqs);
+    Pair<double> *sums = static_cast<Pair<double> *>(workspace);
+    int *counts = reinterpret_cast<int *>(static_cast<char *>(workspace) + space.counts);
     (void)hipGetLastError();
-    if (n_seqs > 0)
-        hipLaunchKernelGGL(policy_kernel, dim3(blocks_for(n_seqs)), dim3(kThreads), 0, s, in, p);
-    else if (grad_logp && n_tokens > 0)
-        hipLaunchKernelGGL(zero_kernel, dim3(blocks_for((n_tokens + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
-                           grad_logp, n_tokens);
+    if (n_seqs == 0) {
+        if (grad_logp && n_tokens > 0)
+            hipLaunchKernelGGL(zero_kernel, blocks_of(n_tokens, kThreads), dim3(kThreads), 0, s, grad_logp, n_tokens);
+        return launched("policy loss");
+    }
+    if (seqs.parts > 1 && p.mean && mask)
+        hipLaunchKernelGGL(count_kernel, blocks_of(n_seqs * seqs.parts, 1), dim3(kThreads), 0, s, in, seqs.parts, counts);
+    with_group(seqs.group, [&](auto group) {
+        hipLaunchKernelGGL(policy_kernel<decltype(group)::value>, blocks_of(n_seqs * seqs.parts, kThreads / seqs.group),
+                           dim3(kThreads), 0, s, in, p, seqs.parts, counts, sums);
+    });
+    if (seqs.parts > 1)
+        hipLaunchKernelGGL(policy_join_kernel, blocks_of(n_seqs, kWaves), dim3(kThreads), 0, s, in, p, seqs.parts, counts, sums);
     return launched("policy loss");
 }
 

@@ -382,3 +382,35 @@ def test_every_way_to_meet_the_pairs(T, groups, sizes, length):
     scores[rng.random(n_seqs) < 0.01] = np.nan
     for smoothing, mean in ((0.0, False), (0.2, True)):
         _check_preference(T, seqs, lp, ref, mask, scores, goff, 0.2, smoothing, 1.0, mean, f"{groups} of {sizes}")
+
+
+@pytest.mark.parametrize("repeat", [1, 40_000])
+def test_impossible_tokens_without_old_or_reference_policy(T, repeat):
+    """log-probabilities of -inf: without the old policy's the ratio is 1, without a reference the KL term is 0."""
+    lp = np.tile(np.array([-1.0, -np.inf, -2.0, -0.5], np.float32), repeat)
+    old = np.tile(np.array([-1.0, -3.0, -2.5, -0.5], np.float32), repeat)
+    seqs = np.arange(0, 4 * repeat + 1, 2)
+    adv = np.resize(np.array([1.0, -1.0], np.float32), 2 * repeat)
+    for o in (None, old):
+        loss, kl, grad = T.tree_ens_policy_loss(_dev(lp), _dev(o), _dev(adv), _dev(seqs), clip_low=0.5, clip_high=0.5)
+        with np.errstate(invalid="ignore"):
+            want = O.policy_loss(lp, o, adv, seqs, clip_low=0.5, clip_high=0.5)
+        _close(loss, want[0], 1e-5, "loss")
+        _close(grad, want[2], 1e-5, "gradient")
+        assert kl is None
+
+
+@pytest.mark.parametrize("seqs_,length", [(3, (0, 50)), (2_000, (40, 60)), (30_000, (0, 5)), (50, (3_000, 20_000)), (3, (200_000, 300_000))])
+def test_every_way_to_take_the_tokens_of_a_policy_loss(T, seqs_, length):
+    rng = np.random.default_rng(seqs_)
+    seqs = np.concatenate([[0], np.cumsum(rng.integers(length[0], length[1] + 1, seqs_))]).astype(np.int64)
+    n = int(seqs[-1])
+    lp = -rng.exponential(size=n).astype(np.float32)
+    r = rng.normal(0, 0.2, n)
+    for edge in (np.log(0.8), np.log(1.25)):
+        r = np.where(np.abs(r - edge) < 1e-3, edge + 2e-3, r)
+    old, ref = (lp - r).astype(np.float32), (lp + rng.normal(0, 0.3, n)).astype(np.float32)
+    adv, mask = rng.normal(size=seqs_).astype(np.float32), rng.random(n) < 0.6
+    for mean in (False, True):
+        for m in (None, mask):
+            _check_policy(T, seqs, lp, old, ref, m, adv, 0.2, 0.25, 0.05, 0.5, mean, f"{seqs_} {length} {mean}")
