@@ -378,12 +378,12 @@ def tree_ens_predict_topk(h, X, group_offsets, k: int, scores=None, top_idx=None
 # ----------------------------------------------------------------------------------------------
 # learning from scores
 # ----------------------------------------------------------------------------------------------
-def _vector(name, t, dtype, n, device):
-    """Check a contiguous device vector of n entries (any number if n is None) of a type."""
+def _vector(name, t, dtypes, n, device):
+    """Check a contiguous device vector of n entries (any number if n is None)."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda" or t.dtype not in dtype or t.dim() != 1 or \
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != 1 or \
             not t.is_contiguous() or (device is not None and t.device != device):
-        raise TypeError(f"{name} must be a contiguous {str(dtype[0])[6:]} vector on the device")
+        raise TypeError(f"{name} must be a contiguous {str(dtypes[0])[6:]} vector on the device")
     if n is not None and t.shape[0] != n:
         raise TypeError(f"{name} must have {n} entries, not {t.shape[0]}")
     return t
@@ -393,54 +393,58 @@ def _ptr(t):
     return t.data_ptr() if t is not None and t.numel() else None
 
 
-class _Launch:
-    """One call's device and stream: memory it allocates belongs to the stream the work runs on."""
+def _elsewhere(device, stream):
+    """A context in which ``stream`` is torch's current stream on ``device``, or None where it is already: the call
+    then runs inside it, so that memory it allocates belongs to the stream its work runs on."""
+    import torch
+    if stream is None:
+        return torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device)
+    return torch.cuda.stream(stream)
 
-    def __init__(self, device, stream):
-        import torch
-        self.device = device
-        self.guards = []
-        if stream is not None and not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device)
-        if stream is not None:
-            self.guards.append(torch.cuda.stream(stream))  # makes its device current too
-        elif torch.cuda.current_device() != device.index:
-            self.guards.append(torch.cuda.device(device))
 
-    def __enter__(self):
-        for g in self.guards:
-            g.__enter__()
-        return self
+def _workspace(device, fn, *sizes):
+    """(tensor or None, pointer, bytes) that the function of these sizes needs."""
+    import torch
+    need = ctypes.c_int64()
+    _check(getattr(load_library(), fn)(*sizes, ctypes.byref(need)), fn)
+    if not need.value:
+        return None, None, 0
+    t = torch.empty(need.value, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), need.value
 
-    def __exit__(self, *exc):
-        for g in reversed(self.guards):
-            g.__exit__(*exc)
 
-    def empty(self, shape, dtype):
-        import torch
-        return torch.empty(shape, dtype=dtype, device=self.device)
+def _enqueue(device, fn, *args):
+    rc = getattr(load_library(), fn)(_stream_of_device(device), *args)
+    if rc != TREE_ENS_OK:
+        _check(rc, fn)
 
-    def workspace(self, fn, *sizes):
-        import torch
-        need = ctypes.c_int64()
-        _check(getattr(load_library(), fn)(*sizes, ctypes.byref(need)), fn)
-        return self.empty(need.value, torch.uint8) if need.value else None
 
-    def call(self, fn, *args):
-        _check(getattr(load_library(), fn)(_stream_of(self, None), *args), fn)
+def _stream_of_device(device):
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _check_logits(logits, targets):
     """(dtype code, n_tokens, n_vocab, row stride) of device logits [n_tokens, n_vocab]."""
     import torch
     codes = {torch.float32: TREE_ENS_F32, torch.bfloat16: TREE_ENS_BF16, torch.float16: TREE_ENS_F16}
-    if not isinstance(logits, torch.Tensor) or logits.device.type != "cuda" or logits.dtype not in codes or \
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dtype not in codes or \
             logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise TypeError("logits must be a CUDA (HIP) float32, bfloat16 or float16 [n_tokens, n_vocab] tensor with "
                         "contiguous rows")
     n, v = logits.shape
     _vector("targets", targets, (torch.int64,), n, logits.device)
     return codes[logits.dtype], n, v, logits.stride(0) if n > 1 else v
+
+
+def _check_stats(stats, n, device):
+    import torch
+    if not isinstance(stats, torch.Tensor) or stats.dtype != torch.float32 or stats.shape != (n, 2) or \
+            not stats.is_contiguous() or stats.device != device:
+        raise TypeError("stats must be a contiguous float32 [n_tokens, 2] tensor on the logits' device")
 
 
 def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool = False, logp=None, entropy=None,
@@ -450,20 +454,26 @@ def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool 
     [n_tokens, 2] for the gradient). Rows of ``logits`` may lie any stride apart."""
     import torch
     code, n, v, stride = _check_logits(logits, targets)
-    f32, dev = (torch.float32,), logits.device
-    with _Launch(dev, stream) as on:
-        logp = on.empty(n, torch.float32) if logp is None else _vector("logp", logp, f32, n, dev)
-        if entropy is not None:
-            _vector("entropy", entropy, f32, n, dev)
-        elif want_entropy:
-            entropy = on.empty(n, torch.float32)
-        if stats is None:
-            stats = on.empty((n, 2), torch.float32)
-        elif stats.dtype != torch.float32 or stats.shape != (n, 2) or not stats.is_contiguous() or stats.device != dev:
-            raise TypeError("stats must be a contiguous float32 [n_tokens, 2] tensor on the logits' device")
-        work = on.workspace("tree_ens_token_logp_workspace", code, n, v)
-        on.call("tree_ens_token_logp", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale), _ptr(logp),
-                _ptr(entropy), _ptr(stats), _ptr(work), work.numel() if work is not None else 0)
+    f32, dev = torch.float32, logits.device
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_token_logp(logits, targets, scale, want_entropy, logp, entropy, stats)
+    if logp is None:
+        logp = torch.empty(n, dtype=f32, device=dev)
+    else:
+        _vector("logp", logp, (f32,), n, dev)
+    if entropy is not None:
+        _vector("entropy", entropy, (f32,), n, dev)
+    elif want_entropy:
+        entropy = torch.empty(n, dtype=f32, device=dev)
+    if stats is None:
+        stats = torch.empty((n, 2), dtype=f32, device=dev)
+    else:
+        _check_stats(stats, n, dev)
+    _keep, work, size = _workspace(dev, "tree_ens_token_logp_workspace", code, n, v)
+    _enqueue(dev, "tree_ens_token_logp", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale), _ptr(logp),
+             _ptr(entropy), _ptr(stats), work, size)
     return logp, entropy, stats
 
 
@@ -473,42 +483,52 @@ def tree_ens_token_logp_backward(logits, targets, stats, grad_logp, scale: float
     (``entropy`` as the forward gave it; both or neither). ``grad_logits`` may be ``logits`` itself."""
     import torch
     code, n, v, stride = _check_logits(logits, targets)
-    f32, dev = (torch.float32,), logits.device
-    if not isinstance(stats, torch.Tensor) or stats.dtype != torch.float32 or stats.shape != (n, 2) or \
-            not stats.is_contiguous() or stats.device != dev:
-        raise TypeError("stats must be the forward's float32 [n_tokens, 2] tensor")
-    _vector("grad_logp", grad_logp, f32, n, dev)
-    for name, t in (("entropy", entropy), ("grad_entropy", grad_entropy)):
-        if t is not None:
-            _vector(name, t, f32, n, dev)
+    f32, dev = torch.float32, logits.device
+    _check_stats(stats, n, dev)
+    _vector("grad_logp", grad_logp, (f32,), n, dev)
     if (entropy is None) != (grad_entropy is None):
         raise TypeError("entropy and grad_entropy are given together")
-    if grad_logits is not None and (grad_logits.dtype != logits.dtype or grad_logits.shape != logits.shape or
-                                    (v > 1 and grad_logits.stride(1) != 1) or grad_logits.device != dev):
+    if entropy is not None:
+        _vector("entropy", entropy, (f32,), n, dev)
+        _vector("grad_entropy", grad_entropy, (f32,), n, dev)
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_token_logp_backward(logits, targets, stats, grad_logp, scale, entropy, grad_entropy, grad_logits)
+    if grad_logits is None:
+        grad_logits = torch.empty((n, v), dtype=logits.dtype, device=dev)
+    elif not isinstance(grad_logits, torch.Tensor) or grad_logits.dtype != logits.dtype or \
+            grad_logits.shape != logits.shape or (v > 1 and grad_logits.stride(1) != 1) or grad_logits.device != dev:
         raise TypeError("grad_logits must be a tensor of the logits' type, shape and device with contiguous rows")
-    with _Launch(dev, stream) as on:
-        if grad_logits is None:
-            grad_logits = on.empty((n, v), logits.dtype)
-        on.call("tree_ens_token_logp_backward", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale),
-                _ptr(stats), _ptr(grad_logp), _ptr(entropy), _ptr(grad_entropy), _ptr(grad_logits),
-                grad_logits.stride(0) if n > 1 else v)
+    _enqueue(dev, "tree_ens_token_logp_backward", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale),
+             _ptr(stats), _ptr(grad_logp), _ptr(entropy), _ptr(grad_entropy), _ptr(grad_logits),
+             grad_logits.stride(0) if n > 1 else v)
     return grad_logits
 
 
 def _check_tokens(logp, seq_offsets, mask, **others):
     """(n_tokens, n_seqs) of packed sequences; `others` are float vectors over the tokens, or None."""
     import torch
-    _vector("logp", logp, (torch.float32,), None, None)
+    f32 = (torch.float32,)
+    _vector("logp", logp, f32, None, None)
     n, dev = logp.shape[0], logp.device
     for name, t in others.items():
         if t is not None:
-            _vector(name, t, (torch.float32,), n, dev)
+            _vector(name, t, f32, n, dev)
     if mask is not None:
         _vector("mask", mask, (torch.bool, torch.uint8), n, dev)
     _vector("seq_offsets", seq_offsets, (torch.int64,), None, dev)
     if seq_offsets.shape[0] < 1:
         raise TypeError("seq_offsets must have n_seqs + 1 entries")
     return n, seq_offsets.shape[0] - 1
+
+
+def _float_out(name, t, n, device):
+    """A float vector of n entries: the caller's, or a new one."""
+    import torch
+    if t is None:
+        return torch.empty(n, dtype=torch.float32, device=device)
+    return _vector(name, t, (torch.float32,), n, device)
 
 
 def tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp=None, mask=None, beta: float = 0.1,
@@ -519,18 +539,22 @@ def tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp=
     respect to ``logp``, or None without ``want_grad``)."""
     import torch
     n, n_seqs = _check_tokens(logp, seq_offsets, mask, ref_logp=ref_logp, grad_logp=grad_logp)
-    f32, dev = (torch.float32,), logp.device
-    _vector("scores", scores, f32, n_seqs, dev)
+    dev = logp.device
+    _vector("scores", scores, (torch.float32,), n_seqs, dev)
     n_groups = _check_offsets(group_offsets, dev)
-    with _Launch(dev, stream) as on:
-        loss = on.empty(n_groups, torch.float32) if loss is None else _vector("loss", loss, f32, n_groups, dev)
-        margins = on.empty(n_seqs, torch.float32) if margins is None else _vector("margins", margins, f32, n_seqs, dev)
-        if grad_logp is None and want_grad:
-            grad_logp = on.empty(n, torch.float32)
-        work = on.workspace("tree_ens_preference_workspace", n, n_seqs, n_groups)
-        on.call("tree_ens_preference_loss", _ptr(logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(), n_seqs,
-                _ptr(scores), group_offsets.data_ptr(), n_groups, float(beta), float(smoothing), float(grad_scale),
-                int(flags), _ptr(loss), _ptr(margins), _ptr(grad_logp), _ptr(work), work.numel() if work is not None else 0)
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp, mask, beta, smoothing,
+                                            grad_scale, flags, want_grad, loss, margins, grad_logp)
+    loss = _float_out("loss", loss, n_groups, dev)
+    margins = _float_out("margins", margins, n_seqs, dev)
+    if grad_logp is None and want_grad:
+        grad_logp = torch.empty(n, dtype=torch.float32, device=dev)
+    _keep, work, size = _workspace(dev, "tree_ens_preference_workspace", n, n_seqs, n_groups)
+    _enqueue(dev, "tree_ens_preference_loss", _ptr(logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(), n_seqs,
+             _ptr(scores), group_offsets.data_ptr(), n_groups, float(beta), float(smoothing), float(grad_scale),
+             int(flags), _ptr(loss), _ptr(margins), _ptr(grad_logp), work, size)
     return loss, margins, grad_logp
 
 
@@ -540,13 +564,13 @@ def tree_ens_group_advantage(scores, group_offsets, eps: float = 1e-6, flags: in
     _vector("scores", scores, (torch.float32,), None, None)
     n, dev = scores.shape[0], scores.device
     n_groups = _check_offsets(group_offsets, dev)
-    with _Launch(dev, stream) as on:
-        if advantages is None:
-            advantages = on.empty(n, torch.float32)
-        else:
-            _vector("advantages", advantages, (torch.float32,), n, dev)
-        on.call("tree_ens_group_advantage", _ptr(scores), n, group_offsets.data_ptr(), n_groups, float(eps), int(flags),
-                _ptr(advantages))
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_group_advantage(scores, group_offsets, eps, flags, advantages)
+    advantages = _float_out("advantages", advantages, n, dev)
+    _enqueue(dev, "tree_ens_group_advantage", _ptr(scores), n, group_offsets.data_ptr(), n_groups, float(eps), int(flags),
+             _ptr(advantages))
     return advantages
 
 
@@ -558,20 +582,22 @@ def tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None,
     ``logp``, or None without ``want_grad``). ``old_logp`` None: the tokens were sampled by this very policy."""
     import torch
     n, n_seqs = _check_tokens(logp, seq_offsets, mask, old_logp=old_logp, ref_logp=ref_logp, grad_logp=grad_logp)
-    f32, dev = (torch.float32,), logp.device
-    _vector("advantages", advantages, f32, n_seqs, dev)
-    with _Launch(dev, stream) as on:
-        loss = on.empty(n_seqs, torch.float32) if loss is None else _vector("loss", loss, f32, n_seqs, dev)
-        if kl is not None:
-            _vector("kl", kl, f32, n_seqs, dev)
-        elif ref_logp is not None:
-            kl = on.empty(n_seqs, torch.float32)
-        if grad_logp is None and want_grad:
-            grad_logp = on.empty(n, torch.float32)
-        work = on.workspace("tree_ens_policy_workspace", n, n_seqs)
-        on.call("tree_ens_policy_loss", _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(),
-                n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef), float(grad_scale), int(flags),
-                _ptr(loss), _ptr(kl), _ptr(grad_logp), _ptr(work), work.numel() if work is not None else 0)
+    dev = logp.device
+    _vector("advantages", advantages, (torch.float32,), n_seqs, dev)
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp, mask, clip_low, clip_high,
+                                        kl_coef, grad_scale, flags, want_grad, loss, kl, grad_logp)
+    loss = _float_out("loss", loss, n_seqs, dev)
+    if kl is not None or ref_logp is not None:
+        kl = _float_out("kl", kl, n_seqs, dev)
+    if grad_logp is None and want_grad:
+        grad_logp = torch.empty(n, dtype=torch.float32, device=dev)
+    _keep, work, size = _workspace(dev, "tree_ens_policy_workspace", n, n_seqs)
+    _enqueue(dev, "tree_ens_policy_loss", _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(),
+             n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef), float(grad_scale), int(flags),
+             _ptr(loss), _ptr(kl), _ptr(grad_logp), work, size)
     return loss, kl, grad_logp
 
 

@@ -128,6 +128,7 @@ __device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, con
 constexpr int kTurns = 16; // a group takes at most so many times four tokens a thread
 
 template <int kN> struct Lanes {
+    static constexpr int kThreadsOf = kN;
     int id;
     // Sum over the group, in a fixed order, for each of its threads.
     template <typename T> __device__ __forceinline__ T sum(T v) const {
@@ -578,30 +579,44 @@ __global__ void __launch_bounds__(kThreads) pairs_few_kernel(int64_t n_seqs, Pre
 // ---------------------------------------------------------------------------------------------
 // Advantages and policy loss
 // ---------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(kThreads)
-advantage_kernel(const float *scores, int64_t n, const int64_t *groups, int64_t n_groups, float eps, bool center,
-                 float *out) {
-    for (int64_t g = blockIdx.x; g < n_groups; g += gridDim.x) {
-        const Span q = span_of(groups, g, n);
+// Advantages of the groups of `in` (candidates as its tokens): mean and spread in double, by two passes
+// over values that stay in registers where four fours a thread hold them.
+template <int kGroup>
+__global__ void __launch_bounds__(kThreads) advantage_kernel(Tokens in, float eps, bool center, float *out) {
+    for_sequences<kGroup>(in, 1, [&](auto lanes, int64_t, Span q, int) {
+        constexpr int kHold = 4, kN = decltype(lanes)::kThreadsOf;
+        const bool held = q.b - q.a <= kN * kFour * kHold;
         const double count = fmax(double(q.b - q.a), 1.0);
+        float x[kHold][kFour];
+        const auto load = [&](int k, int64_t t) { load_tokens(in.logp, t, in.n, x[k]); };
+        const auto again = [&](int k, int64_t t) { // for the passes after the first
+            if (!held)
+                load(k, t);
+        };
         double sum = 0.0, squares = 0.0;
-        for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
-            sum += scores[i];
-        const double mean = block_sum(sum) / count;
-        for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
-            squares += (scores[i] - mean) * (scores[i] - mean);
-        const double std = sqrt(block_sum(squares) / count);
-        const double by = center ? 1.0 : 1.0 / (std + eps);
-        for (int64_t i = q.a + threadIdx.x; i < q.b; i += kThreads)
-            out[i] = float((scores[i] - mean) * by);
-        // candidates outside every group
-        if (g == 0)
-            for (int64_t i = threadIdx.x; i < q.a; i += kThreads)
-                out[i] = 0.0f;
-        if (g == n_groups - 1)
-            for (int64_t i = q.b + threadIdx.x; i < n; i += kThreads)
-                out[i] = 0.0f;
-    }
+        lanes.template each<kHold>(q, load, [&](int k, int64_t, int some) {
+#pragma unroll
+            for (int i = 0; i < kFour; ++i)
+                sum += i < some ? x[k][i] : 0.0f;
+        });
+        const double mean = lanes.sum(sum) / count;
+        lanes.template each<kHold>(q, again, [&](int k, int64_t, int some) {
+#pragma unroll
+            for (int i = 0; i < kFour; ++i) {
+                const double d = i < some ? x[k][i] - mean : 0.0;
+                squares += d * d;
+            }
+        });
+        const double by = center ? 1.0 : 1.0 / (sqrt(lanes.sum(squares) / count) + eps);
+        lanes.template each<kHold>(q, again, [&](int k, int64_t t, int some) {
+            float d[kFour];
+#pragma unroll
+            for (int i = 0; i < kFour; ++i)
+                d[i] = float((x[k][i] - mean) * by);
+            store_tokens(out, t, some, d);
+        });
+    });
+    zero_outside(in, out);
 }
 
 // exp(x), off by 2^-24 (2 + |x|) of itself.
@@ -980,12 +995,18 @@ int tree_ens_group_advantage(void *stream, const float *scores, int64_t n_docs, 
         return set_error(TREE_ENS_E_ARG, "a pointer is misaligned for its type");
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     (void)hipGetLastError();
-    if (n_groups > 0)
-        hipLaunchKernelGGL(advantage_kernel, dim3(blocks_for(n_groups)), dim3(kThreads), 0, s, scores, n_docs,
-                           group_offsets, n_groups, eps, (flags & TREE_ENS_CENTER_ONLY) != 0, advantages);
-    else
-        hipLaunchKernelGGL(zero_kernel, dim3(blocks_for((n_docs + kThreads - 1) / kThreads)), dim3(kThreads), 0, s,
-                           advantages, n_docs);
+    if (n_groups > 0) {
+        const Tokens in{scores, nullptr, nullptr, n_docs, group_offsets, n_groups};
+        // threads enough to hold a group of twice the mean size
+        const double mean = double(n_docs) / double(n_groups);
+        const int lanes = mean <= 64.0 ? 8 : mean <= 128.0 ? 16 : mean <= 256.0 ? 32 : mean <= 512.0 ? kWave : kThreads;
+        with_group(lanes, [&](auto group) {
+            hipLaunchKernelGGL(advantage_kernel<decltype(group)::value>, blocks_of(n_groups, kThreads / lanes), dim3(kThreads), 0, s,
+                               in, eps, (flags & TREE_ENS_CENTER_ONLY) != 0, advantages);
+        });
+    } else {
+        hipLaunchKernelGGL(zero_kernel, blocks_of(n_docs, kThreads), dim3(kThreads), 0, s, advantages, n_docs);
+    }
     return launched("group advantage");
 }
 
