@@ -74,10 +74,12 @@ typedef unsigned unsigned_ __attribute__((aligned(1)));
 
 constexpr int kFour = 4; // neighbouring tokens that a thread takes at a time
 
-// Tokens [t, t + 4) of an array of n, 0 beyond its end.
+// Tokens [t, t + 4) of an array of n, 0 beyond its end. Every array is read once and the gradient is not
+// read here, so both go past the caches: the preference loss of 4,096 sequences of 3,700 tokens takes 44
+// us where cached loads and stores take 52, the policy loss 59 and 61; 1,660,000 tokens 13.7 and 14.3.
 __device__ __forceinline__ void load_tokens(const float *p, int64_t t, int64_t n, float (&x)[kFour]) {
     if (t + kFour <= n) {
-        const float4_ a = *reinterpret_cast<const float4_ *>(p + t);
+        const float4_ a = __builtin_nontemporal_load(reinterpret_cast<const float4_ *>(p + t));
 #pragma unroll
         for (int k = 0; k < kFour; ++k)
             x[k] = a[k];
@@ -109,7 +111,7 @@ __device__ __forceinline__ unsigned load_mask(const uint8_t *mask, int64_t t, in
 
 __device__ __forceinline__ void store_tokens(float *p, int64_t t, int count, const float (&x)[kFour]) {
     if (count == kFour) {
-        *reinterpret_cast<float4_ *>(p + t) = float4_{x[0], x[1], x[2], x[3]};
+        __builtin_nontemporal_store(float4_{x[0], x[1], x[2], x[3]}, reinterpret_cast<float4_ *>(p + t));
         return;
     }
 #pragma unroll
@@ -846,12 +848,13 @@ template <typename F> void with_group(int group, F &&f) {
 int64_t round_up(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 // Which kernels meet the pairs, by the mean sizes of groups and sequences. Measured (us of the whole loss;
-// groups x candidates x tokens; pairs_kernel fused / tile kernels with pairs_few_kernel / with pairs_kernel /
-// with pairs_part_kernel):
-//   64 x 2 x 250: 7.1 / 14.9 / 15.6; 512 x 2 x 500: 10.2 / 16.0 / 16.5; 512 x 8 x 500: 18.9 / 19.7 / 20.4;
-//   4,096 x 2 x 500: 39 / 23.9 / 34; 50,000 x 2 x 30: 272 / 29 / 153; 2 x 2 x 60,000: 451 / 12.9 / 14.2;
-//   5,000 x 8 x 20: 47 / 25.6 / 37; 512 x 16 x 500: 44 / 41 / 25.2; 2,000 x 40 x 100: - / - / 48 / 58;
-//   909 x 110 x 143: - / - / 79 / 75; 100 x 300 x 100: - / - / 137 / 45; 9,090 x 110 x 10: - / - / 190 / 210.
+// groups x candidates x tokens, means: pairs_kernel fused / pairs_few_kernel / pairs_kernel):
+//   64 x 2 x 200: 6.5 / 8.9 / 9.9; 1,000 x 2 x 810: 12.2 / 15.0 / 16.6; 512 x 8 x 405: 13.0 / 14.6 / 15.0; 2,000 x 4 x
+//   82: 15.0 / 12.0 / 15.6; 4 x 4 x 6,600: 36 / 11.6 / 12.6; 4,096 x 2 x 410: 30 / 19.3 / 26; 50,000 x 2 x 24: 258 / 23 /
+//   106; 5,000 x 8 x 16: 44 / 13.3 / 22; 512 x 16 x 410: 27 / 34 / 20.5; 100 x 16 x 82: 17.5 / 27 / 13.6.
+// pairs_kernel / pairs_part_kernel with 2 / 8 / 24 parts: 2,000 x 40 x 81: 42 / 54 / - / -; 300 x 65 x 243: 30 / 31 / 46 /
+//   79; 909 x 109 x 116: 74 / 68 / 93 / 179; 9,090 x 110 x 8: 209 / 242 / - / -; 100 x 303 x 81: 149 / 84 / 41 / 46; 4 x 640 x
+//   81: 271 / 113 / 42 / 25.
 enum class Pairs { kFused, kFew, kGroup, kParts };
 struct PreferencePlan {
     Pairs by;
@@ -862,7 +865,7 @@ PreferencePlan preference_plan(int64_t n_tokens, int64_t n_seqs, int64_t n_group
     if (n_groups == 0 || n_seqs == 0)
         return {Pairs::kGroup, 1};
     const double seqs = double(n_seqs) / double(n_groups), tokens = double(n_tokens) / double(n_seqs);
-    if (seqs <= 8.0 && n_seqs <= 2048 && tokens <= 512.0)
+    if (seqs <= 8.0 && n_seqs <= 4096 && tokens <= 1024.0)
         return {Pairs::kFused, 1};
     if (seqs <= 8.0)
         return {Pairs::kFew, 1};
