@@ -116,11 +116,12 @@ def policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None, mask=Non
             share = 1.0 / max(len(at), 1) if mean else 1.0
             ratio = np.ones(len(at)) if old_logp is None else np.exp(lp[at] - np.asarray(old_logp, np.float64)[at])
             q = np.zeros(len(at)) if ref_logp is None else np.asarray(ref_logp, np.float64)[at] - lp[at]
-            k = np.expm1(q) - q
+            k = np.where(np.isposinf(q), np.inf, np.expm1(q) - np.where(np.isposinf(q), 0.0, q))
             edge = 1 + clip_high if A >= 0 else 1 - clip_low
             out = ratio > edge if A >= 0 else ratio < edge
             gain = np.where(out, edge, ratio) * A
-            loss[s] = share * sum_of(kl_coef * k - gain)
+            loss[s] = share * sum_of((kl_coef * k if kl_coef else 0.0) - gain)
             kl[s] = share * sum_of(k)
-            grad[at] = grad_scale * share * (-np.where(out, 0.0, A * np.where(out, 0.0, ratio)) - kl_coef * np.expm1(q))
+            pull = kl_coef * np.expm1(q) if kl_coef else 0.0
+            grad[at] = grad_scale * share * (-np.where(out, 0.0, A * np.where(out, 0.0, ratio)) - pull)
     return loss, kl, grad

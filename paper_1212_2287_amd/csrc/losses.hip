@@ -136,8 +136,9 @@ template <int kN> struct Lanes {
     template <typename T> __device__ __forceinline__ T sum(T v) const {
         if constexpr (kN == kThreads)
             return T(block_sum(double(v)));
-        for (int off = kN / 2; off; off >>= 1)
-            v += __shfl_xor(v, off);
+        else
+            for (int off = kN / 2; off; off >>= 1)
+                v += __shfl_xor(v, off);
         return v;
     }
     // For this thread's fours of a span, kAhead at a time: load(k, t) for each, then use(k, t, count).
@@ -221,18 +222,18 @@ struct Preference {
     bool mean;
     float *loss, *margins, *weights; // weights: dh / dlogp of a counted token, then the loss's gradient
     // The margin and weight of a sequence with this sum of log ratios and so many counted tokens.
-    __device__ __forceinline__ void take(int64_t s, Pair<int> v) const {
-        const double w = mean ? double(beta) / max(v.b, 1) : double(beta);
+    __device__ __forceinline__ void take(int64_t s, Pair<int64_t> v) const {
+        const double w = mean ? double(beta) / double(max(v.b, int64_t(1))) : double(beta);
         margins[s] = float(w * v.a);
         weights[s] = float(w);
     }
 };
 
 // Sum of a span's log ratios and how many count, over a group's threads.
-template <int kN> __device__ __forceinline__ Pair<int> ratios_of(const Tokens &in, Lanes<kN> lanes, Span q) {
+template <int kN> __device__ __forceinline__ Pair<int64_t> ratios_of(const Tokens &in, Lanes<kN> lanes, Span q) {
     constexpr int kAhead = 4;
     double sum = 0.0;
-    int counted = 0;
+    int64_t counted = 0;
     float x[kAhead][kFour], r[kAhead][kFour] = {};
     unsigned mask[kAhead];
     lanes.template each<kAhead>(
@@ -271,9 +272,9 @@ template <int kN> __device__ __forceinline__ void spread(const Tokens &in, Lanes
 
 // Margins and weights, or with several parts what each adds to them.
 template <int kGroup>
-__global__ void __launch_bounds__(kThreads) margin_kernel(Tokens in, Preference p, int parts, Pair<int> *partial) {
+__global__ void __launch_bounds__(kThreads) margin_kernel(Tokens in, Preference p, int parts, Pair<int64_t> *partial) {
     for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
-        const Pair<int> v = ratios_of(in, lanes, q);
+        const Pair<int64_t> v = ratios_of(in, lanes, q);
         if (lanes.id != 0)
             return;
         if (parts > 1)
@@ -284,10 +285,10 @@ __global__ void __launch_bounds__(kThreads) margin_kernel(Tokens in, Preference 
 }
 
 // Margins and weights from the parts, a wave a sequence.
-__global__ void __launch_bounds__(kThreads) margin_join_kernel(int64_t n_seqs, Preference p, int parts, const Pair<int> *partial) {
+__global__ void __launch_bounds__(kThreads) margin_join_kernel(int64_t n_seqs, Preference p, int parts, const Pair<int64_t> *partial) {
     const Lanes<kWave> lanes{int(threadIdx.x % kWave)};
     for (int64_t s = blockIdx.x * int64_t(kWaves) + threadIdx.x / kWave; s < n_seqs; s += int64_t(gridDim.x) * kWaves) {
-        Pair<int> v{0.0, 0};
+        Pair<int64_t> v{0.0, 0};
         for (int k = lanes.id; k < parts; k += kWave) {
             v.a += partial[s * parts + k].a;
             v.b += partial[s * parts + k].b;
@@ -322,11 +323,16 @@ struct Loss {
 };
 
 // One pair: dl/dh of the candidate `me`, and with kLoss the pair's loss. Candidates are (margin, score),
-// margins and losses in units of ln 2 here. With d the margin by which the better one leads and e =
+// margins and losses in units of ln 2 here, margins from the group's first on (as far as that is finite), so
+// that the change of units rounds by their spread and not by their size. With d the margin by which the better one leads and e =
 // exp(-|d|): l = softplus(-d) + smoothing d, softplus(-d) = max(-d, 0) + log1p(e), dl/dd = smoothing -
 // sigmoid(-d).
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.693147180559945309417;
+__device__ __forceinline__ float origin_of(float first) { return fabsf(first) < INFINITY ? first : 0.0f; }
+__device__ __forceinline__ float2 candidate(float margin, float origin, float score) {
+    return make_float2((margin - origin) * kLog2e, score);
+}
 template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 other, float smoothing, Met &met) {
     const bool ahead = me.y > other.y, behind = me.y < other.y;
     const float lead = me.x - other.x;
@@ -392,8 +398,8 @@ __device__ __forceinline__ void clear_outside(const Preference &p, int64_t n_seq
 }
 
 // Loss of a group, and weights times the loss's gradient with respect to the margins, by a workgroup.
-// kFused: it also sums the sequences' tokens first and writes their gradients last, instead of the tile
-// kernels.
+// kFused: it also sums the sequences' tokens first and writes their gradients last, instead of
+// margin_kernel and spread_kernel.
 template <bool kFused>
 __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p, float *grad) {
     __shared__ float2 held[2 * kHeld];
@@ -407,7 +413,7 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         const int64_t lo = g == 0 ? 0 : q.a, hi = g == p.n_groups - 1 ? in.n_seqs : q.b;
         if constexpr (kFused) {
             for (int64_t s = lo + wave; s < hi; s += kWaves) {
-                const Pair<int> v = ratios_of(in, lanes, span_of(in.offsets, s, in.n));
+                const Pair<int64_t> v = ratios_of(in, lanes, span_of(in.offsets, s, in.n));
                 if (lanes.id == 0)
                     p.take(s, v);
             }
@@ -415,9 +421,10 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         }
         clear_outside(p, in.n_seqs, g, q, threadIdx.x, kThreads);
         Loss loss{0.0, 0.0};
+        const float origin = n > 0 ? origin_of(p.margins[q.a]) : 0.0f;
         if (n <= kHeld) {
             for (int i = threadIdx.x; i < n; i += kThreads)
-                held[i] = held[i + n] = make_float2(p.margins[q.a + i] * kLog2e, p.scores[q.a + i]);
+                held[i] = held[i + n] = candidate(p.margins[q.a + i], origin, p.scores[q.a + i]);
             __syncthreads();
             // waves take steps in turn and leave their slopes in rows of their own
             for (int i = lanes.id; i < n; i += kWave)
@@ -432,13 +439,13 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         } else {
             for (int64_t i0 = 0; i0 < n; i0 += kThreads) {
                 const int64_t i = q.a + i0 + threadIdx.x;
-                const float2 me = i < q.b ? make_float2(p.margins[i] * kLog2e, p.scores[i]) : make_float2(0.0f, 0.0f);
+                const float2 me = i < q.b ? candidate(p.margins[i], origin, p.scores[i]) : make_float2(0.0f, 0.0f);
                 double sum = 0.0;
                 for (int64_t j0 = q.a; j0 < q.b; j0 += kHeld) {
                     const int fit = int(min(int64_t(kHeld), q.b - j0));
                     __syncthreads();
                     for (int j = threadIdx.x; j < fit; j += kThreads)
-                        held[j] = make_float2(p.margins[j0 + j] * kLog2e, p.scores[j0 + j]);
+                        held[j] = candidate(p.margins[j0 + j], origin, p.scores[j0 + j]);
                     __syncthreads();
                     if (i < q.b)
                         sum += meet_window(me, held, fit, 0, 1, p.smoothing, loss);
@@ -480,18 +487,19 @@ __global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Pr
         const unsigned n = unsigned(q.b - q.a), chunk = (n + unsigned(parts) - 1) / unsigned(parts);
         const int64_t from = min(int64_t(part) * chunk, int64_t(n)), to = min(from + chunk, int64_t(n));
         Loss loss{0.0, 0.0};
+        const float origin = n > 0 ? origin_of(p.margins[q.a]) : 0.0f;
         // rows of even size, as few as fit
         const int turns = int((to - from + kThreads - 1) / kThreads), each = turns ? int((to - from + turns - 1) / turns) : 0;
         for (int64_t i0 = from; i0 < to; i0 += each) {
             const int rows = int(min(int64_t(each), to - i0)), shares = kThreads / rows;
             const int row = threadIdx.x % rows, share = threadIdx.x / rows;
             const int64_t i = i0 + row;
-            const float2 me = make_float2(p.margins[q.a + i] * kLog2e, p.scores[q.a + i]);
+            const float2 me = candidate(p.margins[q.a + i], origin, p.scores[q.a + i]);
             double slope = 0.0;
             if (n <= kHeldPart) {
                 if (i0 == from)
                     for (int j = threadIdx.x; j < n; j += kThreads)
-                        held[j] = held[j + n] = make_float2(p.margins[q.a + j] * kLog2e, p.scores[q.a + j]);
+                        held[j] = held[j + n] = candidate(p.margins[q.a + j], origin, p.scores[q.a + j]);
                 __syncthreads();
                 if (share < shares)
                     slope = meet_held(held, int(n), int(i), share, shares, p.smoothing, loss);
@@ -500,7 +508,7 @@ __global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Pr
                     const int fit = int(min(int64_t(kHeldPart), n - j0));
                     __syncthreads();
                     for (int j = threadIdx.x; j < fit; j += kThreads)
-                        held[j] = make_float2(p.margins[q.a + j0 + j] * kLog2e, p.scores[q.a + j0 + j]);
+                        held[j] = candidate(p.margins[q.a + j0 + j], origin, p.scores[q.a + j0 + j]);
                     __syncthreads();
                     if (share < shares)
                         slope += meet_window(me, held, fit, share, shares, p.smoothing, loss);
@@ -556,13 +564,14 @@ __global__ void __launch_bounds__(kThreads) pairs_few_kernel(int64_t n_seqs, Pre
         const Span q = span_of(p.groups, g, n_seqs);
         clear_outside(p, n_seqs, g, q, lane, kFew);
         Loss loss{0.0, 0.0};
+        const float origin = q.b > q.a ? origin_of(p.margins[q.a]) : 0.0f;
         for (int64_t i = q.a + lane; i < q.b; i += kFew) {
-            const float2 me = make_float2(p.margins[i] * kLog2e, p.scores[i]);
+            const float2 me = candidate(p.margins[i], origin, p.scores[i]);
             Met met{0.0f, 0.0f, 0};
             float slope = 0.0f;
 #pragma unroll 2
             for (int64_t j = q.a; j < q.b; ++j)
-                slope += meet<true>(me, make_float2(p.margins[j] * kLog2e, p.scores[j]), p.smoothing, met);
+                slope += meet<true>(me, candidate(p.margins[j], origin, p.scores[j]), p.smoothing, met);
             loss.add(met, p.smoothing, 0.5);
             p.weights[i] = float(p.weights[i] * slope);
         }
@@ -624,20 +633,6 @@ __global__ void __launch_bounds__(kThreads) advantage_kernel(Tokens in, float ep
 // exp(x), off by 2^-24 (2 + |x|) of itself.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-// exp(q) - q - 1: the sum of q^k / k! from k = 2 where the difference would cancel. Below 1/2 the
-// terms up to k = 9 leave out less than 2e-9 of it.
-__device__ __forceinline__ float exp_less_tangent(float q) {
-    float s = 1.0f / 362880.0f;
-    s = fmaf(s, q, 1.0f / 40320.0f);
-    s = fmaf(s, q, 1.0f / 5040.0f);
-    s = fmaf(s, q, 1.0f / 720.0f);
-    s = fmaf(s, q, 1.0f / 120.0f);
-    s = fmaf(s, q, 1.0f / 24.0f);
-    s = fmaf(s, q, 1.0f / 6.0f);
-    s = fmaf(s, q, 0.5f);
-    return fabsf(q) < 0.5f ? s * q * q : exp_of(q) - q - 1.0f;
-}
-
 struct Policy {
     const float *old_logp, *advantages;
     float low, high, kl_coef, grad_scale;
@@ -645,34 +640,45 @@ struct Policy {
     float *loss, *kl, *grad;
     // The sums of a sequence's gains and of exp(q) - q - 1.
     __device__ __forceinline__ void take(int64_t s, Pair<double> v, double share) const {
-        loss[s] = float(share * (v.a + kl_coef * v.b));
+        loss[s] = float(share * (kl_coef != 0.0f ? v.a + kl_coef * v.b : v.a));
         if (kl)
             kl[s] = float(share * v.b);
     }
 };
 
-// Of one token: the ratio, k = exp(q) - q - 1 and dk/dq = exp(q) - 1.
+// Of one token: the ratio, k = exp(q) - q - 1 and up = dk/dq = exp(q) - 1. Below 1/2 the differences would
+// cancel: k is the sum of q^i / i! from i = 2 there, whose terms up to i = 9 leave out less than 2e-9 of it.
+// An infinite q has k = inf.
 struct Terms {
     float ratio, k, up;
 };
 __device__ __forceinline__ Terms terms_of(const Tokens &in, const Policy &p, float logp, float old, float ref) {
     const float d = p.old_logp ? logp - old : 0.0f, q = in.ref ? ref - logp : 0.0f; // without them: 0, whatever logp is
-    const float k = exp_less_tangent(q);
-    return {exp_of(d), k, k + q};
+    float s = 1.0f / 362880.0f;
+    s = fmaf(s, q, 1.0f / 40320.0f);
+    s = fmaf(s, q, 1.0f / 5040.0f);
+    s = fmaf(s, q, 1.0f / 720.0f);
+    s = fmaf(s, q, 1.0f / 120.0f);
+    s = fmaf(s, q, 1.0f / 24.0f);
+    s = fmaf(s, q, 1.0f / 6.0f);
+    s = fmaf(s, q, 0.5f) * q * q;
+    const float up = exp_of(q) - 1.0f;
+    const bool small = fabsf(q) < 0.5f;
+    return {exp_of(d), small ? s : up - fminf(q, 3e38f), small ? s + q : up};
 }
 // The clipped gain's share in the loss, and the gradient of the token's loss. Comparisons pass a NaN
 // ratio unchanged.
 __device__ __forceinline__ float policy_of(const Policy &p, const Terms &x, float a, float &slope) {
     const float edge = a >= 0.0f ? p.high : p.low;
     const bool clipped = a >= 0.0f ? x.ratio > edge : x.ratio < edge;
-    slope = (clipped ? 0.0f : -a * x.ratio) - p.kl_coef * x.up;
+    slope = (clipped ? 0.0f : -a * x.ratio) - (p.kl_coef != 0.0f ? p.kl_coef * x.up : 0.0f);
     return -(clipped ? edge : x.ratio) * a;
 }
 
 // How many of a span's tokens count.
-template <int kN> __device__ __forceinline__ int counted_of(const Tokens &in, Lanes<kN> lanes, Span q) {
+template <int kN> __device__ __forceinline__ int64_t counted_of(const Tokens &in, Lanes<kN> lanes, Span q) {
     constexpr int kAhead = 4;
-    int count = 0;
+    int64_t count = 0;
     unsigned mask[kAhead];
     lanes.template each<kAhead>(
         q, [&](int k, int64_t t) { mask[k] = load_mask(in.mask, t, in.n); },
@@ -681,9 +687,9 @@ template <int kN> __device__ __forceinline__ int counted_of(const Tokens &in, La
 }
 
 // How many tokens of each part of a sequence count, for the mean over masked sequences in parts.
-__global__ void __launch_bounds__(kThreads) count_kernel(Tokens in, int parts, int *counts) {
+__global__ void __launch_bounds__(kThreads) count_kernel(Tokens in, int parts, int64_t *counts) {
     for_sequences<kThreads>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
-        const int count = counted_of(in, lanes, q);
+        const int64_t count = counted_of(in, lanes, q);
         if (lanes.id == 0)
             counts[s * parts + part] = count;
     });
@@ -691,7 +697,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Tokens in, int parts, i
 
 // What a sequence's loss is multiplied by, for the threads that take it (or the part q of it).
 template <int kN>
-__device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, Lanes<kN> lanes, int64_t s, Span q, int parts, const int *counts) {
+__device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, Lanes<kN> lanes, int64_t s, Span q, int parts, const int64_t *counts) {
     if (!p.mean)
         return 1.0;
     if (!in.mask) {
@@ -699,15 +705,15 @@ __device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, La
         return 1.0 / double(max(all.b - all.a, int64_t(1)));
     }
     if (parts == 1)
-        return 1.0 / max(counted_of(in, lanes, q), 1);
+        return 1.0 / double(max(counted_of(in, lanes, q), int64_t(1)));
     double count = 0.0; // of all parts
     for (int k = lanes.id; k < parts; k += kN)
-        count += counts[s * parts + k];
+        count += double(counts[s * parts + k]);
     return 1.0 / fmax(lanes.sum(count), 1.0);
 }
 
 template <int kGroup>
-__global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, int parts, const int *counts, Pair<double> *partial) {
+__global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, int parts, const int64_t *counts, Pair<double> *partial) {
     for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
         const float a = p.advantages[s];
         const double share = share_of(in, p, lanes, s, q, parts, counts);
@@ -754,7 +760,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, i
 }
 
 // Losses from the parts, a wave a sequence.
-__global__ void __launch_bounds__(kThreads) policy_join_kernel(Tokens in, Policy p, int parts, const int *counts, const Pair<double> *partial) {
+__global__ void __launch_bounds__(kThreads) policy_join_kernel(Tokens in, Policy p, int parts, const int64_t *counts, const Pair<double> *partial) {
     const Lanes<kWave> lanes{int(threadIdx.x % kWave)};
     for (int64_t s = blockIdx.x * int64_t(kWaves) + threadIdx.x / kWave; s < in.n_seqs; s += int64_t(gridDim.x) * kWaves) {
         Pair<double> v{0.0, 0.0};
@@ -883,7 +889,7 @@ PreferenceSpace preference_space(int64_t n_tokens, int64_t n_seqs, int64_t n_gro
     const SequencePlan seqs = sequence_plan(n_tokens, n_seqs);
     PreferenceSpace p{0, round_up(4 * n_seqs), 0, 0};
     p.sums = p.losses + (pairs.by == Pairs::kParts ? n_groups * pairs.parts * int64_t(sizeof(Loss)) : 0);
-    p.bytes = p.sums + (seqs.parts > 1 ? n_seqs * seqs.parts * int64_t(sizeof(Pair<int>)) : 0);
+    p.bytes = p.sums + (seqs.parts > 1 ? n_seqs * seqs.parts * int64_t(sizeof(Pair<int64_t>)) : 0);
     return p;
 }
 
@@ -896,7 +902,7 @@ PolicySpace policy_space(int64_t n_tokens, int64_t n_seqs) {
     if (parts == 1)
         return {0, 0};
     const int64_t sums = n_seqs * parts * int64_t(sizeof(Pair<double>));
-    return {sums, sums + 4 * n_seqs * parts};
+    return {sums, sums + 8 * n_seqs * parts};
 }
 
 } // namespace
@@ -941,7 +947,7 @@ int tree_ens_preference_loss(void *stream, const float *logp, const float *ref_l
     char *const at = static_cast<char *>(workspace);
     float *weights = reinterpret_cast<float *>(at + space.weights);
     Loss *losses = reinterpret_cast<Loss *>(at + space.losses);
-    Pair<int> *sums = reinterpret_cast<Pair<int> *>(at + space.sums);
+    Pair<int64_t> *sums = reinterpret_cast<Pair<int64_t> *>(at + space.sums);
     const Preference p{scores, group_offsets, n_groups, beta, smoothing, grad_scale, (flags & TREE_ENS_SEQ_MEAN) != 0,
                        loss, margins, weights};
     const PreferencePlan pairs = preference_plan(n_tokens, n_seqs, n_groups);
@@ -1055,7 +1061,7 @@ int tree_ens_policy_loss(void *stream, const float *logp, const float *old_logp,
                    (flags & TREE_ENS_SEQ_MEAN) != 0, loss, kl, grad_logp};
     const SequencePlan seqs = sequence_plan(n_tokens, n_seqs);
     Pair<double> *sums = static_cast<Pair<double> *>(workspace);
-    int *counts = reinterpret_cast<int *>(static_cast<char *>(workspace) + space.counts);
+    int64_t *counts = reinterpret_cast<int64_t *>(static_cast<char *>(workspace) + space.counts);
     (void)hipGetLastError();
     if (n_seqs == 0) {
         if (grad_logp && n_tokens > 0)

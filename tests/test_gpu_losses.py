@@ -414,3 +414,36 @@ def test_every_way_to_take_the_tokens_of_a_policy_loss(T, seqs_, length):
     for mean in (False, True):
         for m in (None, mask):
             _check_policy(T, seqs, lp, old, ref, m, adv, 0.2, 0.25, 0.05, 0.5, mean, f"{seqs_} {length} {mean}")
+
+
+@pytest.mark.parametrize("repeat", [1, 50_000])
+def test_tokens_that_one_model_excludes(T, repeat):
+    """Infinite log ratios to the reference: the KL term is infinite, its gradient that of exp(q) - 1; without a
+    coefficient it is reported and leaves the loss alone."""
+    lp = np.tile(np.array([-1.0, -2.0, -np.inf, -0.5], np.float32), repeat)
+    ref = np.tile(np.array([-1.5, -np.inf, -3.0, -0.5], np.float32), repeat)
+    seqs, adv = np.arange(4 * repeat + 1), np.resize(np.array([1.0, -2.0, 0.5], np.float32), 4 * repeat)
+    for kl_coef in (0.0, 0.25):
+        got = T.tree_ens_policy_loss(_dev(lp), None, _dev(adv), _dev(seqs), ref_logp=_dev(ref), kl_coef=kl_coef)
+        want = O.policy_loss(lp, None, adv, seqs, ref, kl_coef=kl_coef)
+        for a, b, what in zip(got, want, ("loss", "kl", "gradient")):
+            _close(a, b, 1e-6 * (1 + np.abs(np.where(np.isfinite(b), b, 0.0))), f"{what} {kl_coef}")
+
+
+@pytest.mark.parametrize("n,length", [(2, 3), (40, 3), (200, 2), (700, 1), (2_500, 1)])
+def test_preference_loss_of_close_margins_far_from_zero(T, n, length):
+    """Margins about 1,000 that differ by hundredths: the loss goes by their differences, which the rounding of the
+    margins themselves (2^-24 of 1,000) limits and nothing else."""
+    rng = np.random.default_rng(n)
+    lp = (-1000.0 / length + 0.01 * rng.normal(size=n * length)).astype(np.float32)
+    seqs, groups = np.arange(0, n * length + 1, length), np.array([0, n])
+    scores = rng.normal(size=n).astype(np.float32)
+    loss, h, grad = T.tree_ens_preference_loss(_dev(lp), _dev(seqs), _dev(scores), _dev(groups), beta=1.0)
+    # the pairs of the margins as they were rounded
+    m = h.double().cpu().numpy()
+    want = O.preference_loss(m, np.arange(n + 1), scores, groups, beta=1.0)
+    _close(h, O.margins(lp, seqs, beta=1.0)[0], 2 * U * 1100, "margins")
+    _close(loss, want[0], 40 * U, "loss")
+    pairs = n * (n - 1) / 2
+    per = (n - 1) / pairs * 40 * U
+    _close(grad, np.repeat(want[2], length), per + 4 * U * np.abs(np.repeat(want[2], length)), "gradient")
