@@ -381,16 +381,16 @@ def tree_ens_predict_topk(h, X, group_offsets, k: int, scores=None, top_idx=None
 def _vector(name, t, dtypes, n, device):
     """Check a contiguous device vector of n entries (any number if n is None)."""
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != 1 or \
-            not t.is_contiguous() or (device is not None and t.device != device):
-        raise TypeError(f"{name} must be a contiguous {str(dtypes[0])[6:]} vector on the device")
-    if n is not None and t.shape[0] != n:
-        raise TypeError(f"{name} must have {n} entries, not {t.shape[0]}")
-    return t
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.dim() == 1 and t.is_contiguous() and \
+            (t.device == device if device is not None else t.is_cuda):
+        if n is None or t.numel() == n:
+            return t
+        raise TypeError(f"{name} must have {n} entries, not {t.numel()}")
+    raise TypeError(f"{name} must be a contiguous {str(dtypes[0])[6:]} vector on the device")
 
 
 def _ptr(t):
-    return t.data_ptr() if t is not None and t.numel() else None
+    return t.data_ptr() or None if t is not None else None
 
 
 def _elsewhere(device, stream):
@@ -398,30 +398,25 @@ def _elsewhere(device, stream):
     then runs inside it, so that memory it allocates belongs to the stream its work runs on."""
     import torch
     if stream is None:
-        return torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+        return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device)
     return torch.cuda.stream(stream)
 
 
-def _workspace(device, fn, *sizes):
+def _workspace(lib, device, fn, *sizes):
     """(tensor or None, pointer, bytes) that the function of these sizes needs."""
     import torch
     need = ctypes.c_int64()
-    _check(getattr(load_library(), fn)(*sizes, ctypes.byref(need)), fn)
+    _check(getattr(lib, fn)(*sizes, ctypes.byref(need)), fn)
     if not need.value:
         return None, None, 0
     t = torch.empty(need.value, dtype=torch.uint8, device=device)
     return t, t.data_ptr(), need.value
 
 
-def _enqueue(device, fn, *args):
-    rc = getattr(load_library(), fn)(_stream_of_device(device), *args)
-    if rc != TREE_ENS_OK:
-        _check(rc, fn)
-
-
-def _stream_of_device(device):
+def _stream_on(device):
+    """torch's current stream on a device, as tree_ens_predict takes it."""
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
@@ -471,9 +466,10 @@ def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool 
         stats = torch.empty((n, 2), dtype=f32, device=dev)
     else:
         _check_stats(stats, n, dev)
-    _keep, work, size = _workspace(dev, "tree_ens_token_logp_workspace", code, n, v)
-    _enqueue(dev, "tree_ens_token_logp", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale), _ptr(logp),
-             _ptr(entropy), _ptr(stats), work, size)
+    lib = load_library()
+    _keep, work, size = _workspace(lib, dev, "tree_ens_token_logp_workspace", code, n, v)
+    _check(lib.tree_ens_token_logp(_stream_on(dev), _ptr(logits), code, n, v, stride, _ptr(targets), float(scale),
+           _ptr(logp), _ptr(entropy), _ptr(stats), work, size), "tree_ens_token_logp")
     return logp, entropy, stats
 
 
@@ -500,9 +496,9 @@ def tree_ens_token_logp_backward(logits, targets, stats, grad_logp, scale: float
     elif not isinstance(grad_logits, torch.Tensor) or grad_logits.dtype != logits.dtype or \
             grad_logits.shape != logits.shape or (v > 1 and grad_logits.stride(1) != 1) or grad_logits.device != dev:
         raise TypeError("grad_logits must be a tensor of the logits' type, shape and device with contiguous rows")
-    _enqueue(dev, "tree_ens_token_logp_backward", _ptr(logits), code, n, v, stride, _ptr(targets), float(scale),
-             _ptr(stats), _ptr(grad_logp), _ptr(entropy), _ptr(grad_entropy), _ptr(grad_logits),
-             grad_logits.stride(0) if n > 1 else v)
+    _check(load_library().tree_ens_token_logp_backward(_stream_on(dev), _ptr(logits), code, n, v, stride,
+           _ptr(targets), float(scale), _ptr(stats), _ptr(grad_logp), _ptr(entropy), _ptr(grad_entropy), _ptr(grad_logits),
+           grad_logits.stride(0) if n > 1 else v), "tree_ens_token_logp_backward")
     return grad_logits
 
 
@@ -551,10 +547,12 @@ def tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp=
     margins = _float_out("margins", margins, n_seqs, dev)
     if grad_logp is None and want_grad:
         grad_logp = torch.empty(n, dtype=torch.float32, device=dev)
-    _keep, work, size = _workspace(dev, "tree_ens_preference_workspace", n, n_seqs, n_groups)
-    _enqueue(dev, "tree_ens_preference_loss", _ptr(logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(), n_seqs,
-             _ptr(scores), group_offsets.data_ptr(), n_groups, float(beta), float(smoothing), float(grad_scale),
-             int(flags), _ptr(loss), _ptr(margins), _ptr(grad_logp), work, size)
+    lib = load_library()
+    _keep, work, size = _workspace(lib, dev, "tree_ens_preference_workspace", n, n_seqs, n_groups)
+    _check(lib.tree_ens_preference_loss(_stream_on(dev), _ptr(logp), _ptr(ref_logp), _ptr(mask), n,
+           seq_offsets.data_ptr(), n_seqs, _ptr(scores), group_offsets.data_ptr(), n_groups, float(beta), float(smoothing),
+           float(grad_scale), int(flags), _ptr(loss), _ptr(margins), _ptr(grad_logp), work, size),
+           "tree_ens_preference_loss")
     return loss, margins, grad_logp
 
 
@@ -569,8 +567,8 @@ def tree_ens_group_advantage(scores, group_offsets, eps: float = 1e-6, flags: in
         with elsewhere:
             return tree_ens_group_advantage(scores, group_offsets, eps, flags, advantages)
     advantages = _float_out("advantages", advantages, n, dev)
-    _enqueue(dev, "tree_ens_group_advantage", _ptr(scores), n, group_offsets.data_ptr(), n_groups, float(eps), int(flags),
-             _ptr(advantages))
+    _check(load_library().tree_ens_group_advantage(_stream_on(dev), _ptr(scores), n, group_offsets.data_ptr(),
+           n_groups, float(eps), int(flags), _ptr(advantages)), "tree_ens_group_advantage")
     return advantages
 
 
@@ -594,10 +592,11 @@ def tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None,
         kl = _float_out("kl", kl, n_seqs, dev)
     if grad_logp is None and want_grad:
         grad_logp = torch.empty(n, dtype=torch.float32, device=dev)
-    _keep, work, size = _workspace(dev, "tree_ens_policy_workspace", n, n_seqs)
-    _enqueue(dev, "tree_ens_policy_loss", _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(mask), n, seq_offsets.data_ptr(),
-             n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef), float(grad_scale), int(flags),
-             _ptr(loss), _ptr(kl), _ptr(grad_logp), work, size)
+    lib = load_library()
+    _keep, work, size = _workspace(lib, dev, "tree_ens_policy_workspace", n, n_seqs)
+    _check(lib.tree_ens_policy_loss(_stream_on(dev), _ptr(logp), _ptr(old_logp), _ptr(ref_logp), _ptr(mask), n,
+           seq_offsets.data_ptr(), n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef),
+           float(grad_scale), int(flags), _ptr(loss), _ptr(kl), _ptr(grad_logp), work, size), "tree_ens_policy_loss")
     return loss, kl, grad_logp
 
 
