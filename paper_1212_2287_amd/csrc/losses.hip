@@ -869,7 +869,8 @@ int64_t round_up(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 // groups x candidates x tokens, means: pairs_kernel fused / pairs_few_kernel / pairs_kernel):
 //   64 x 2 x 200: 6.5 / 8.9 / 9.9; 1,000 x 2 x 810: 12.2 / 15.0 / 16.6; 512 x 8 x 405: 13.0 / 14.6 / 15.0; 2,000 x 4 x
 //   82: 15.0 / 12.0 / 15.6; 4 x 4 x 6,600: 36 / 11.6 / 12.6; 4,096 x 2 x 410: 30 / 19.3 / 26; 50,000 x 2 x 24: 258 / 23 /
-//   106; 5,000 x 8 x 16: 44 / 13.3 / 22; 512 x 16 x 410: 27 / 34 / 20.5; 100 x 16 x 82: 17.5 / 27 / 13.6.
+//   106; 5,000 x 8 x 16: 44 / 13.3 / 22; 2,048 x 2 x 405: 18.2 / 13.9 / -; 512 x 16 x 410: 27 / 34 / 20.5; 100 x 16 x
+//   82: 17.5 / 27 / 13.6.
 // pairs_kernel / pairs_part_kernel with 2 / 8 / 24 parts: 2,000 x 40 x 81: 42 / 54 / - / -; 300 x 65 x 243: 30 / 31 / 46 /
 //   79; 909 x 109 x 116: 74 / 68 / 93 / 179; 9,090 x 110 x 8: 209 / 242 / - / -; 100 x 303 x 81: 149 / 84 / 41 / 46; 4 x 640 x
 //   81: 271 / 113 / 42 / 25.
@@ -883,7 +884,7 @@ PreferencePlan preference_plan(int64_t n_tokens, int64_t n_seqs, int64_t n_group
     if (n_groups == 0 || n_seqs == 0)
         return {Pairs::kGroup, 1};
     const double seqs = double(n_seqs) / double(n_groups), tokens = double(n_tokens) / double(n_seqs);
-    if (seqs <= 8.0 && n_seqs <= 4096 && tokens <= 1024.0)
+    if (seqs <= 8.0 && n_groups <= 1024 && n_seqs <= 4096 && tokens <= 1024.0)
         return {Pairs::kFused, 1};
     if (seqs <= 8.0)
         return {Pairs::kFew, 1};
