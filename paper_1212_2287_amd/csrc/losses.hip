@@ -722,8 +722,8 @@ __device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, La
 }
 
 // Bound by memory, 17 bytes a masked token, with the sum of instructions at half of it: 19 million tokens of
-// 4,096 sequences take 68 to 72 us (4.7 to 4.4 TB/s). A mean over masked tokens needs their number first, which
-// reads the mask twice, the second time from the cache.
+// 4,096 sequences take 73 us (4.4 TB/s). A mean over masked tokens needs their number first, which reads the
+// mask twice, the second time from the cache.
 template <int kGroup>
 __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, int parts, const int64_t *counts, Pair<double> *partial) {
     for_sequences<kGroup>(in, parts, [&](auto lanes, int64_t s, Span q, int part) {
@@ -731,7 +731,10 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, i
         const double share = share_of(in, p, lanes, s, q, parts, counts);
         const float w = float(p.grad_scale * share);
         double loss = 0.0, kl = 0.0;
-        constexpr int kAhead = 2;
+        // Four tokens a thread in flight: 84 registers and six waves a SIMD, where eight take 101 and four waves (us, one
+        // / two fours; sequences x mean tokens): 16,384 x 1,620: 101 / 110; 200,000 x 8: 28.5 / 32; 20,000 x 325: 39 / 42;
+        // 97,000 x 116: 70 / 72; 4,096 x 3,700: 60 / 59; 4,096 x 405: 13.9 / 13.7; 4,096 x 4,640: 73 / 72.
+        constexpr int kAhead = 1;
         float x[kAhead][kFour], old[kAhead][kFour] = {}, ref[kAhead][kFour] = {};
         unsigned mask[kAhead];
         lanes.template each<kAhead>(
