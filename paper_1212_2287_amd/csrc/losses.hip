@@ -833,12 +833,12 @@ int check_tokens(const float *logp, int64_t n_tokens, const int64_t *seq_offsets
 // How sequences are shared out: threads for each, or parts of it. By their mean length, and more threads
 // where the sequences are too few for 2,000 waves, 8 to a CU. Measured on the policy loss (us; sequences x mean
 // tokens: 8 / 16 / 32 / 64 / 256 threads):
-//   200,000 x 24: 35 / 45 / 77 / 144 / 483; 99,000 x 49: 29 / 32 / 44 / 76 / 241; 50,000 x 98: 31 / 28 / 31 / 45 /
-//   127; 30,000 x 195: 48 / 31 / 29 / 34 / 81; 20,000 x 325: - / - / 31 / 31 / 58; 10,000 x 818: - / - / 43 / 33 / 39;
-//   4,096 x 2,030: - / - / 54 / 41 / 31; 4,000 x 24: 5.7 / 4.9 / 4.4 / 5.5 / 11.5; 2,000 x 81: 9.7 / 6.4 / 5.0 / 4.5 / 7.4.
+//   200,000 x 24: 39 / 49 / 81 / 152 / 423; 99,000 x 49: 34 / 37 / 47 / 80 / 210; 50,000 x 98: 41 / 31 / 34 / 46 /
+//   111; 30,000 x 195: 60 / 37 / 32 / 37 / 72; 20,000 x 325: - / - / 34 / 35 / 53; 10,000 x 818: - / - / 48 / 36 / 38;
+//   4,096 x 2,030: - / - / 63 / 47 / 31; 4,000 x 24: 6.4 / 5.6 / 5.1 / 6.5 / 12.4; 2,000 x 81: 10.6 / 7.7 / 6.0 / 5.2 / 8.4.
 // In parts of a thousand tokens or more where long sequences are few (1 / 2 / 4 / 8 / 64 parts): 512 x 23,600:
-// 120 / 72 / 55 / 48 / -; 4 x 61,400: 122 / 62 / 35 / 18 / 7.2; 256 x 3,200: 15.2 / 13.4 / 11.5 / 12.5 / -; 2,048 x
-// 1,600: 18 / 22 / 29 / 46 / -.
+// 85 / 59 / 52 / 44 / -; 4 x 73,700: 133 / 72 / 40 / 23 / 8.0; 256 x 3,200: 14.0 / 12.3 / 10.9 / 12.5 / -; 2,048 x
+// 1,600: 17 / 23 / 30 / 47 / -.
 struct SequencePlan {
     int group, parts;
 };
