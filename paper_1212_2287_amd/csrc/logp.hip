@@ -42,8 +42,9 @@ struct Running {
 };
 
 // Scores below the maximum by more than this (in powers of two) are held here: exp2 is 0 there, and
-// 0 times it is 0, where 0 times the -inf of a masked logit would be NaN.
-constexpr float kFar = -1e30f;
+// 0 times it is 0, where 0 times the -inf of a masked logit would be NaN. Its products with the sum of
+// any row and with an entropy's gradient of any size up to 1e35 are floats.
+constexpr float kFar = -1024.0f;
 
 // m = -inf (nothing but masked logits so far) subtracts 0: their differences stay -inf.
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }

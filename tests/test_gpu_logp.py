@@ -331,3 +331,34 @@ def _full(values, pick, n):
     out = np.zeros(n)
     out[pick] = values
     return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [60, 900, 5_000])
+def test_gradients_of_any_size_leave_excluded_tokens_at_zero(T, dtype, V):
+    """Gradients of the entropy (and of the log-probability) up to 1e35: logits of -inf have gradient 0 all the same, the
+    others are as large as they are."""
+    import torch
+    d, td, x, t = _logits(dtype, 6, V, seed=3, banned=0.4)
+    d[:, 0] = x[:, 0] = 1.0
+    h = np.array([5e8, -1e12, 1e35, 0.0, 1.0, -1e35], np.float32)
+    g = np.array([1.0, 1.0, 1.0, 1e30, -1e30, 0.0], np.float32)
+    for scale in (1.0, 1.7):
+        _, entropy, stats = O.token_logp(x, t, scale)
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()  # noqa: E731
+        for k, more in enumerate(({}, dict(entropy=dev(entropy), grad_entropy=dev(h)))):
+            out = T.tree_ens_token_logp_backward(d, td, dev(stats), dev(g), scale=scale, **more).double().cpu().numpy()
+            want = O.token_logp_grad(x, t, g, h * k, scale)
+            tol = _grad_tolerance(want, x, t, g.astype(np.float64), k * h.astype(np.float64), scale, dtype, stats, entropy)
+            assert not out[np.isneginf(x) & (np.arange(V) != t[:, None])].any()
+            assert (np.abs(out - want) <= tol).all()
+
+
+def test_entropy_of_a_vocabulary_masked_by_the_lowest_value(T):
+    """800 million logits of bfloat16's lowest value and one of 0: its token is certain."""
+    import torch
+    V = 800_000_000
+    d = torch.full((1, V), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16, device="cuda")
+    d[0, V - 5] = 0.0
+    logp, entropy, stats = T.tree_ens_token_logp(d, torch.tensor([V - 5], device="cuda"), want_entropy=True)
+    assert (logp.item(), entropy.item(), stats.tolist()) == (0.0, 0.0, [[0.0, 0.0]])
