@@ -296,8 +296,8 @@ int tree_ens_token_logp_workspace(int32_t dtype, int64_t n_tokens, int64_t n_voc
  *                    row is written, rounded once (to nearest). May be `logits` itself with the same
  *                    stride; it may not overlap the logits otherwise (TREE_ENS_E_ARG).
  * Rows that do not count, and rows whose gradients are both 0, receive zeros and are not read. So do
- * logits of -inf beside the target, whatever the gradients, as long as
- * scale * (|grad_logp| + (entropy + 1024) * |grad_entropy|) is a float.
+ * logits of -inf beside the target, however large the gradients, as long as scale * grad_logp is a
+ * float.
  */
 int tree_ens_token_logp_backward(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
                                  int64_t n_vocab, int64_t row_stride, const int64_t *targets,

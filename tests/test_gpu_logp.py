@@ -362,3 +362,18 @@ def test_entropy_of_a_vocabulary_masked_by_the_lowest_value(T):
     d[0, V - 5] = 0.0
     logp, entropy, stats = T.tree_ens_token_logp(d, torch.tensor([V - 5], device="cuda"), want_entropy=True)
     assert (logp.item(), entropy.item(), stats.tolist()) == (0.0, 0.0, [[0.0, 0.0]])
+
+
+def test_scales_up_to_the_largest_float(T):
+    """Any finite scale > 0: at 3e38 the largest logit takes everything, and log2(e) times the scale is no float."""
+    import torch
+    x = np.array([[3.0, 2.5, 2.5, 2.25], [2.5, 3.0, 3.0, 2.5], [2.5, 2.25, 3.0, -np.inf]])
+    t = np.array([0, 2, 1])
+    d, td, scale = torch.from_numpy(x).float().cuda(), torch.from_numpy(t).cuda(), float(np.float32(3e38))
+    want = O.token_logp(x, t, scale)
+    got = T.tree_ens_token_logp(d, td, scale=scale, want_entropy=True)
+    _check_forward(got, want, 4, "scale 3e38")
+    g, h = torch.full((3,), 0.25, device="cuda"), torch.full((3,), 0.125, device="cuda")
+    out = T.tree_ens_token_logp_backward(d, td, got[2], g, scale=scale, entropy=got[1], grad_entropy=h).double().cpu().numpy()
+    ref = O.token_logp_grad(x, t, np.full(3, 0.25), np.full(3, 0.125), scale)
+    assert (np.abs(out - ref) <= 32 * U * scale).all()
