@@ -327,20 +327,16 @@ struct Loss {
     }
 };
 
-// One pair: dl/dh of the candidate `me`, and with kLoss the pair's loss. Candidates are (margin, score),
-// margins and losses in units of ln 2 here, margins from the group's first on (as far as that is finite), so
-// that the change of units rounds by their spread and not by their size. With d the margin by which the better one leads and e =
+// One pair: dl/dh of the candidate `me`, and with kLoss the pair's loss. Candidates are (margin, score). The margins'
+// difference comes first and goes by log2(e) then, so that a pair is rounded by the size of its own difference, whatever
+// the margins of others; losses are in units of ln 2 here. With d the margin by which the better one leads and e =
 // exp(-|d|): l = softplus(-d) + smoothing d, softplus(-d) = max(-d, 0) + log1p(e), dl/dd = smoothing -
 // sigmoid(-d).
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.693147180559945309417;
-__device__ __forceinline__ float origin_of(float first) { return fabsf(first) < INFINITY ? first : 0.0f; }
-__device__ __forceinline__ float2 candidate(float margin, float origin, float score) {
-    return make_float2((margin - origin) * kLog2e, score);
-}
 template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 other, float smoothing, Met &met) {
     const bool ahead = me.y > other.y, behind = me.y < other.y;
-    const float lead = me.x - other.x;
+    const float lead = (me.x - other.x) * kLog2e;
     const float e = __builtin_amdgcn_exp2f(-fabsf(lead));
     const float u = 1.0f + e, r = __builtin_amdgcn_rcpf(u);
     if (kLoss) {
@@ -426,10 +422,9 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         }
         clear_outside(p, in.n_seqs, g, q, threadIdx.x, kThreads);
         Loss loss{0.0, 0.0};
-        const float origin = n > 0 ? origin_of(p.margins[q.a]) : 0.0f;
         if (n <= kHeld) {
             for (int i = threadIdx.x; i < n; i += kThreads)
-                held[i] = held[i + n] = candidate(p.margins[q.a + i], origin, p.scores[q.a + i]);
+                held[i] = held[i + n] = make_float2(p.margins[q.a + i], p.scores[q.a + i]);
             __syncthreads();
             // waves take steps in turn and leave their slopes in rows of their own
             for (int i = lanes.id; i < n; i += kWave)
@@ -444,13 +439,13 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         } else {
             for (int64_t i0 = 0; i0 < n; i0 += kThreads) {
                 const int64_t i = q.a + i0 + threadIdx.x;
-                const float2 me = i < q.b ? candidate(p.margins[i], origin, p.scores[i]) : make_float2(0.0f, 0.0f);
+                const float2 me = i < q.b ? make_float2(p.margins[i], p.scores[i]) : make_float2(0.0f, 0.0f);
                 double sum = 0.0;
                 for (int64_t j0 = q.a; j0 < q.b; j0 += kHeld) {
                     const int fit = int(min(int64_t(kHeld), q.b - j0));
                     __syncthreads();
                     for (int j = threadIdx.x; j < fit; j += kThreads)
-                        held[j] = candidate(p.margins[j0 + j], origin, p.scores[j0 + j]);
+                        held[j] = make_float2(p.margins[j0 + j], p.scores[j0 + j]);
                     __syncthreads();
                     if (i < q.b)
                         sum += meet_window(me, held, fit, 0, 1, p.smoothing, loss);
@@ -494,19 +489,18 @@ __global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Pr
         const unsigned n = unsigned(q.b - q.a), chunk = (n + unsigned(parts) - 1) / unsigned(parts);
         const int64_t from = min(int64_t(part) * chunk, int64_t(n)), to = min(from + chunk, int64_t(n));
         Loss loss{0.0, 0.0};
-        const float origin = n > 0 ? origin_of(p.margins[q.a]) : 0.0f;
         // rows of even size, as few as fit
         const int turns = int((to - from + kThreads - 1) / kThreads), each = turns ? int((to - from + turns - 1) / turns) : 0;
         for (int64_t i0 = from; i0 < to; i0 += each) {
             const int rows = int(min(int64_t(each), to - i0)), shares = kThreads / rows;
             const int row = threadIdx.x % rows, share = threadIdx.x / rows;
             const int64_t i = i0 + row;
-            const float2 me = candidate(p.margins[q.a + i], origin, p.scores[q.a + i]);
+            const float2 me = make_float2(p.margins[q.a + i], p.scores[q.a + i]);
             double slope = 0.0;
             if (n <= kHeldPart) {
                 if (i0 == from)
                     for (int j = threadIdx.x; j < n; j += kThreads)
-                        held[j] = held[j + n] = candidate(p.margins[q.a + j], origin, p.scores[q.a + j]);
+                        held[j] = held[j + n] = make_float2(p.margins[q.a + j], p.scores[q.a + j]);
                 __syncthreads();
                 if (share < shares)
                     slope = meet_held(held, int(n), int(i), share, shares, p.smoothing, loss);
@@ -515,7 +509,7 @@ __global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Pr
                     const int fit = int(min(int64_t(kHeldPart), n - j0));
                     __syncthreads();
                     for (int j = threadIdx.x; j < fit; j += kThreads)
-                        held[j] = candidate(p.margins[q.a + j0 + j], origin, p.scores[q.a + j0 + j]);
+                        held[j] = make_float2(p.margins[q.a + j0 + j], p.scores[q.a + j0 + j]);
                     __syncthreads();
                     if (share < shares)
                         slope += meet_window(me, held, fit, share, shares, p.smoothing, loss);
@@ -571,14 +565,13 @@ __global__ void __launch_bounds__(kThreads) pairs_few_kernel(int64_t n_seqs, Pre
         const Span q = span_of(p.groups, g, n_seqs);
         clear_outside(p, n_seqs, g, q, lane, kFew);
         Loss loss{0.0, 0.0};
-        const float origin = q.b > q.a ? origin_of(p.margins[q.a]) : 0.0f;
         for (int64_t i = q.a + lane; i < q.b; i += kFew) {
-            const float2 me = candidate(p.margins[i], origin, p.scores[i]);
+            const float2 me = make_float2(p.margins[i], p.scores[i]);
             Met met{0.0f, 0.0f, 0};
             float slope = 0.0f;
 #pragma unroll 2
             for (int64_t j = q.a; j < q.b; ++j)
-                slope += meet<true>(me, candidate(p.margins[j], origin, p.scores[j]), p.smoothing, met);
+                slope += meet<true>(me, make_float2(p.margins[j], p.scores[j]), p.smoothing, met);
             loss.add(met, p.smoothing, 0.5);
             p.weights[i] = float(p.weights[i] * slope);
         }

@@ -447,3 +447,43 @@ def test_preference_loss_of_close_margins_far_from_zero(T, n, length):
     pairs = n * (n - 1) / 2
     per = (n - 1) / pairs * 40 * U
     _close(grad, np.repeat(want[2], length), per + 4 * U * np.abs(np.repeat(want[2], length)), "gradient")
+
+
+# groups and their sizes, for each of the ways pairs are met
+WAYS = {"one kernel": (40, [8]), "few": (1_100, [8, 2]), "a workgroup": (30, [40]), "its windows": (60, [20] * 29 + [700]),
+        "parts": (5, [130]), "windows of parts": (1, [2_500])}
+
+
+def _margins_alone(way, seed, spread):
+    """Sequences of one token, so that a margin is its log-probability: (log-probabilities, sequence and group offsets,
+    scores)."""
+    count, sizes = WAYS[way]
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    rng = np.random.default_rng([seed, count])
+    n = int(groups[-1])
+    return (spread * rng.normal(size=n)).astype(np.float32), np.arange(n + 1), groups, rng.normal(size=n).astype(np.float32)
+
+
+def _per_pair(scores, groups):
+    """How many pairs a candidate is in, over the group's number of pairs."""
+    out = np.zeros(len(scores))
+    for a, b in zip(groups[:-1], groups[1:]):
+        ahead = scores[a:b, None] > scores[None, a:b]
+        out[a:b] = (ahead.sum(0) + ahead.sum(1)) / max(int(ahead.sum()), 1)
+    return out
+
+
+@pytest.mark.parametrize("first", [0.0, -50.0, -5_000.0, -50_000.0, 1e30])
+@pytest.mark.parametrize("way", list(WAYS))
+def test_one_far_candidate_leaves_the_other_pairs_exact(T, way, first):
+    """Margins of spread 0.3 and one far off, in front of its group: each pair goes by the difference of its own two
+    margins, of one rounding. A pair's slope is off by 32 u, and a chain of 128 floats adds 64 u to each at most."""
+    lp, seqs, groups, scores = _margins_alone(way, 1, 0.3)
+    lp[groups[:-1]] = first
+    for smoothing in (0.0, 0.125):
+        loss, h, grad = T.tree_ens_preference_loss(_dev(lp), _dev(seqs), _dev(scores), _dev(groups), beta=1.0, smoothing=smoothing)
+        assert np.array_equal(h.cpu().numpy(), lp)
+        with np.errstate(over="ignore"):
+            want = O.preference_loss(lp, seqs, scores, groups, beta=1.0, smoothing=smoothing)
+        _close(loss, want[0], 100 * U * (1 + want[0]), f"{way} loss")
+        _close(grad, want[2], 100 * U * _per_pair(scores, groups) + 4 * U * np.abs(want[2]), f"{way} gradient")
