@@ -312,7 +312,7 @@ template <int kGroup> __global__ void __launch_bounds__(kThreads) spread_kernel(
 // where meeting each pair from both sides takes 42 (909 groups of 110, by pairs_kernel).
 constexpr int kHeld = 512; // candidates of a group that are held in LDS
 
-// What the pairs that a thread met add up to: softplus(-d), d and 1.
+// What the pairs that a thread met add up to: (1 - smoothing) max(-d, 0) + log1p(exp(-|d|)), max(d, 0) and 1.
 struct Met {
     float loss, lead;
     int pairs;
@@ -320,7 +320,7 @@ struct Met {
 // The same over threads, with the smoothing.
 struct Loss {
     double sum, pairs;
-    // Margins that are infinite have no smoothed loss that is finite, but may have a plain one.
+    // An infinite lead costs nothing without smoothing, where 0 times it would be NaN.
     __device__ __forceinline__ void add(const Met &m, float smoothing, double weight) {
         sum += weight * (smoothing > 0.0f ? m.loss + double(smoothing) * m.lead : double(m.loss));
         pairs += weight * m.pairs;
@@ -330,8 +330,8 @@ struct Loss {
 // One pair: dl/dh of the candidate `me`, and with kLoss the pair's loss. Candidates are (margin, score). The margins'
 // difference comes first and goes by log2(e) then, so that a pair is rounded by the size of its own difference, whatever
 // the margins of others; losses are in units of ln 2 here. With d the margin by which the better one leads and e =
-// exp(-|d|): l = softplus(-d) + smoothing d, softplus(-d) = max(-d, 0) + log1p(e), dl/dd = smoothing -
-// sigmoid(-d).
+// exp(-|d|): l = (1 - smoothing) softplus(-d) + smoothing softplus(d), softplus(x) = max(x, 0) + log1p(e), dl/dd =
+// smoothing - sigmoid(-d). The two maxima are added apart, so that infinite ones never meet with both signs.
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.693147180559945309417;
 template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 other, float smoothing, Met &met) {
@@ -342,10 +342,10 @@ template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 ot
     if (kLoss) {
         const float d = ahead ? lead : -lead;
         // log1p(e) = log u + log(1 + rest / u), with the rest that u was rounded by
-        float l = __builtin_amdgcn_logf(u) + fmaxf(-d, 0.0f);
+        float l = fmaf(1.0f - smoothing, fmaxf(-d, 0.0f), __builtin_amdgcn_logf(u));
         l = fmaf((e - (u - 1.0f)) * r, kLog2e, l);
         met.loss += ahead || behind ? l : 0.0f;
-        met.lead += ahead || behind ? d : 0.0f;
+        met.lead += ahead || behind ? fmaxf(d, 0.0f) : 0.0f;
         met.pairs += ahead || behind;
     }
     const float dl = smoothing - ((lead >= 0.0f) == ahead ? e * r : r);

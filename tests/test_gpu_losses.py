@@ -487,3 +487,30 @@ def test_one_far_candidate_leaves_the_other_pairs_exact(T, way, first):
             want = O.preference_loss(lp, seqs, scores, groups, beta=1.0, smoothing=smoothing)
         _close(loss, want[0], 100 * U * (1 + want[0]), f"{way} loss")
         _close(grad, want[2], 100 * U * _per_pair(scores, groups) + 4 * U * np.abs(want[2]), f"{way} gradient")
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.125])
+@pytest.mark.parametrize("way", list(WAYS))
+def test_margins_of_impossible_answers(T, way, smoothing):
+    """An answer that the model excludes has margin -inf: a pair that wants it ahead costs infinitely much, one that wants it
+    behind nothing without smoothing and infinitely much with it; the slopes are those of the sigmoid's ends."""
+    lp, seqs, groups, scores = _margins_alone(way, 2, 1.0)
+    some = groups[:-1][::2]  # in every other group: its first answer, as good as its neighbours or the worst of all
+    lp[some] = -np.inf
+    scores[some[1::2]] = -9.0
+    loss, h, grad = T.tree_ens_preference_loss(_dev(lp), _dev(seqs), _dev(scores), _dev(groups), beta=1.0, smoothing=smoothing)
+    assert np.array_equal(h.cpu().numpy(), lp)
+    want, slope = np.zeros(len(groups) - 1), np.zeros(len(lp))
+    for g, (a, b) in enumerate(zip(groups[:-1], groups[1:])):
+        i, j = np.nonzero(scores[a:b, None] > scores[None, a:b])
+        d = lp[a + i].astype(np.float64) - lp[a + j]
+        each = (1 - smoothing) * np.logaddexp(0, -d)
+        if smoothing:
+            each += smoothing * np.logaddexp(0, d)
+        want[g] = each.mean()
+        with np.errstate(over="ignore"):
+            dl = (smoothing - 1 / (1 + np.exp(d))) / len(i)
+        np.add.at(slope, a + i, dl)
+        np.add.at(slope, a + j, -dl)
+    _close(loss, want, 100 * U * (1 + np.where(np.isfinite(want), want, 0.0)), "loss")
+    _close(grad, slope, 100 * U * _per_pair(scores, groups) + 4 * U * np.abs(slope), "gradient")
