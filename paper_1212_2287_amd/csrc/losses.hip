@@ -310,7 +310,8 @@ template <int kGroup> __global__ void __launch_bounds__(kThreads) spread_kernel(
 // Pairs are bound by instructions: 19 a pair for a slope and 33 with the loss, three (two) of them exp2, log2
 // and a reciprocal. Adding a pair's slope to both candidates by LDS atomics, which halves the pairs, took 95 us
 // where meeting each pair from both sides takes 42 (909 groups of 110, by pairs_kernel).
-constexpr int kHeld = 512; // candidates of a group that are held in LDS
+constexpr int kHeld = 512;  // candidates of a group that are held in LDS
+constexpr unsigned kChain = 128; // pairs whose losses and slopes are added in float
 
 // What the pairs that a thread met add up to: (1 - smoothing) max(-d, 0) + log1p(exp(-|d|)), max(d, 0) and 1.
 struct Met {
@@ -553,37 +554,68 @@ __global__ void __launch_bounds__(kThreads) pairs_finish_kernel(int64_t n_seqs, 
     }
 }
 
-// Groups of a few candidates: eight lanes take one. Larger ones among them are met from memory.
-constexpr int kFew = 8;
+// All of group g = [q.a, q.b) by kN neighbouring threads, candidates from memory: a thread takes one at a time and meets
+// the whole group with it, every pair twice.
+template <int kN> __device__ __forceinline__ void meet_in_memory(const Preference &p, Lanes<kN> lanes, int64_t g, Span q) {
+    const float *margins = p.margins + q.a, *scores = p.scores + q.a;
+    float *weights = p.weights + q.a;
+    const unsigned n = unsigned(q.b - q.a);
+    Loss loss{0.0, 0.0};
+    for (unsigned i = lanes.id; i < n; i += kN) {
+        const float2 me = make_float2(margins[i], scores[i]);
+        double sum = 0.0;
+        for (unsigned j = 0; j < n;) {
+            const unsigned end = kN < kWave ? n : min(j + kChain, n); // fewer lanes have kFewMost at most
+            Met met{0.0f, 0.0f, 0};
+            float slope = 0.0f;
+#pragma unroll 2
+            for (; j < end; ++j)
+                slope += meet<true>(me, make_float2(margins[j], scores[j]), p.smoothing, met);
+            loss.add(met, p.smoothing, 0.5);
+            sum += slope;
+        }
+        weights[i] = float(weights[i] * sum);
+    }
+    loss.sum = lanes.sum(loss.sum);
+    loss.pairs = lanes.sum(loss.pairs);
+    const double share = 1.0 / fmax(loss.pairs, 1.0);
+    if (lanes.id == 0)
+        p.loss[g] = float(loss.sum * (kLn2 * share));
+    for (unsigned i = lanes.id; i < n; i += kN)
+        weights[i] = float(weights[i] * (p.grad_scale * share));
+}
+
+// Groups of a few candidates: eight lanes take one. Those of more than kFewMost among them are left to the waves
+// afterwards, one to a wave, and those of more than kWaveMost to the whole workgroup after that: 10,000 pairs and one
+// group of 5,000 take 10.5 ms. Measured (us of the whole loss; kFewMost 64 / 24): 10,000 groups of 2, each 100th of 40: 43 /
+// 24, of 64: 94 / 26, of 65: - / 36; 5,000 of 2 and then 400 of 64: 63 / 80, 1,000 of 28: 24 / 51. Of 65 instead of 64: 207.
+// kWaveMost 128 / 256: each 100th of 200: 46 / 104.
+constexpr int kFew = 8, kFewMost = 64, kWaveMost = 128;
 __global__ void __launch_bounds__(kThreads) pairs_few_kernel(int64_t n_seqs, Preference p) {
     constexpr int kGroups = kThreads / kFew;
     const int lane = threadIdx.x % kFew;
     for (int64_t g0 = blockIdx.x * int64_t(kGroups); g0 < p.n_groups; g0 += int64_t(gridDim.x) * kGroups) {
-        const int64_t g = g0 + threadIdx.x / kFew;
-        if (g >= p.n_groups)
+        const int64_t g = g0 + threadIdx.x / kFew, end = min(g0 + kGroups, p.n_groups);
+        Span q{0, 0};
+        if (g < end) {
+            q = span_of(p.groups, g, n_seqs);
+            clear_outside(p, n_seqs, g, q, lane, kFew);
+        }
+        const bool rest = q.b - q.a > kFewMost;
+        if (g < end && !rest)
+            meet_in_memory(p, Lanes<kFew>{lane}, g, q);
+        if (!__syncthreads_or(rest))
             continue;
-        const Span q = span_of(p.groups, g, n_seqs);
-        clear_outside(p, n_seqs, g, q, lane, kFew);
-        Loss loss{0.0, 0.0};
-        for (int64_t i = q.a + lane; i < q.b; i += kFew) {
-            const float2 me = make_float2(p.margins[i], p.scores[i]);
-            Met met{0.0f, 0.0f, 0};
-            float slope = 0.0f;
-#pragma unroll 2
-            for (int64_t j = q.a; j < q.b; ++j)
-                slope += meet<true>(me, make_float2(p.margins[j], p.scores[j]), p.smoothing, met);
-            loss.add(met, p.smoothing, 0.5);
-            p.weights[i] = float(p.weights[i] * slope);
+        for (int64_t i = g0 + threadIdx.x / kWave; i < end; i += kWaves) {
+            const Span r = span_of(p.groups, i, n_seqs);
+            if (r.b - r.a > kFewMost && r.b - r.a <= kWaveMost)
+                meet_in_memory(p, Lanes<kWave>{int(threadIdx.x % kWave)}, i, r);
         }
-        for (int off = kFew / 2; off; off >>= 1) {
-            loss.sum += __shfl_xor(loss.sum, off);
-            loss.pairs += __shfl_xor(loss.pairs, off);
+        for (int64_t i = g0; i < end; ++i) {
+            const Span r = span_of(p.groups, i, n_seqs);
+            if (r.b - r.a > kWaveMost)
+                meet_in_memory(p, Lanes<kThreads>{int(threadIdx.x)}, i, r);
         }
-        const double share = 1.0 / fmax(loss.pairs, 1.0);
-        if (lane == 0)
-            p.loss[g] = float(loss.sum * (kLn2 * share));
-        for (int64_t i = q.a + lane; i < q.b; i += kFew)
-            p.weights[i] = float(p.weights[i] * (p.grad_scale * share));
     }
 }
 

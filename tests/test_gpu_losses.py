@@ -514,3 +514,35 @@ def test_margins_of_impossible_answers(T, way, smoothing):
         np.add.at(slope, a + j, -dl)
     _close(loss, want, 100 * U * (1 + np.where(np.isfinite(want), want, 0.0)), "loss")
     _close(grad, slope, 100 * U * _per_pair(scores, groups) + 4 * U * np.abs(slope), "gradient")
+
+
+@pytest.mark.parametrize("count,sizes", [(3_000, [2] * 99 + [9, 64, 65]), (2_200, [2] * 1_099 + [100]), (5_000, [2] * 1_666 + [700]),
+                                         (5_000, [2] * 4_998 + [3_000, 1])])
+def test_a_large_group_among_small_ones(T, count, sizes):
+    rng = np.random.default_rng([count, len(sizes)])
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    n_seqs = int(groups[-1])
+    seqs = np.concatenate([[0], np.cumsum(rng.integers(0, 8, n_seqs))]).astype(np.int64)
+    n = int(seqs[-1])
+    lp, ref = -rng.exponential(size=n).astype(np.float32), -rng.exponential(size=n).astype(np.float32)
+    scores = (np.round(rng.normal(size=n_seqs) * 8) / 8).astype(np.float32)
+    for smoothing, mean in ((0.0, False), (0.2, True)):
+        _check_preference(T, seqs, lp, ref, rng.random(n) < 0.8, scores, groups, 0.2, smoothing, 1.0, mean, f"{count} of {sizes}")
+
+
+def test_time_of_a_large_group_among_small_ones(T):
+    """16 million ordered pairs of one group, met by 256 threads: 63,000 in a row for each, of some 35 instructions that
+    take four cycles: 4 ms and what they wait for. Eight threads would take 110 ms and more."""
+    import torch
+    groups = _dev(np.concatenate([np.arange(0, 10_000, 2), [14_000]]))
+    lp, seqs = -torch.rand(14_000, device="cuda"), torch.arange(14_001, device="cuda")
+    scores = torch.randn(14_000, device="cuda")
+    times = []
+    for _ in range(3):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        T.tree_ens_preference_loss(lp, seqs, scores, groups)
+        b.record()
+        b.synchronize()
+        times.append(a.elapsed_time(b))
+    assert min(times) < 40, times
