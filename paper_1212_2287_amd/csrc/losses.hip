@@ -401,7 +401,10 @@ __device__ __forceinline__ void clear_outside(const Preference &p, int64_t n_seq
 
 // Loss of a group, and weights times the loss's gradient with respect to the margins, by a workgroup.
 // kFused: it also sums the sequences' tokens first and writes their gradients last, instead of
-// margin_kernel and spread_kernel.
+// margin_kernel and spread_kernel: a wave a sequence, or a quarter of each where the group has many more
+// tokens than sequences, so that no long sequence keeps one wave busy alone: one of 1.9 million tokens among
+// 2,000 takes 1.05 ms, 3.6 by one wave.
+constexpr int64_t kSplit = 2048; // tokens for each sequence of the group and two more
 template <bool kFused>
 __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p, float *grad) {
     __shared__ float2 held[2 * kHeld];
@@ -413,11 +416,32 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         const int64_t n = q.b - q.a;
         // fused, sequences outside every group go with the first and the last one
         const int64_t lo = g == 0 ? 0 : q.a, hi = g == p.n_groups - 1 ? in.n_seqs : q.b;
+        bool split = false;
         if constexpr (kFused) {
-            for (int64_t s = lo + wave; s < hi; s += kWaves) {
-                const Pair<int64_t> v = ratios_of(in, lanes, span_of(in.offsets, s, in.n));
-                if (lanes.id == 0)
+            __shared__ Pair<int64_t> quarter[kWaves];
+            int64_t s = lo + wave;
+            Span t = s < hi ? span_of(in.offsets, s, in.n) : Span{0, 0};
+            split = lo < hi && min(in.offsets[hi], in.n) - max(in.offsets[lo], int64_t(0)) > kSplit * (hi - lo + 2);
+            if (split)
+                t = part_of(span_of(in.offsets, s = lo, in.n), wave, kWaves);
+            while (s < hi) {
+                Pair<int64_t> v = ratios_of(in, lanes, t);
+                if (split) {
+                    if (lanes.id == 0)
+                        quarter[wave] = v;
+                    __syncthreads();
+                    v = quarter[0];
+                    for (int w = 1; w < kWaves; ++w)
+                        v = {v.a + quarter[w].a, v.b + quarter[w].b};
+                    __syncthreads(); // quarter is free
+                }
+                if (lanes.id == 0 && (!split || wave == 0))
                     p.take(s, v);
+                s += split ? 1 : kWaves;
+                if (s < hi)
+                    t = span_of(in.offsets, s, in.n);
+                if (split)
+                    t = part_of(t, wave, kWaves);
             }
             __syncthreads();
         }
@@ -466,8 +490,10 @@ __global__ void __launch_bounds__(kThreads) pairs_kernel(Tokens in, Preference p
         __syncthreads(); // held and slopes are free, weights are there
         if constexpr (kFused)
             if (grad)
-                for (int64_t s = lo + wave; s < hi; s += kWaves)
-                    spread(in, lanes, span_of(in.offsets, s, in.n), p.weights[s], grad);
+                for (int64_t s = split ? lo : lo + wave; s < hi; s += split ? 1 : kWaves) {
+                    const Span t = span_of(in.offsets, s, in.n);
+                    spread(in, lanes, split ? part_of(t, wave, kWaves) : t, p.weights[s], grad);
+                }
     }
     if constexpr (kFused)
         if (grad)

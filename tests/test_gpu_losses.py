@@ -546,3 +546,22 @@ def test_time_of_a_large_group_among_small_ones(T):
         b.synchronize()
         times.append(a.elapsed_time(b))
     assert min(times) < 40, times
+
+
+@pytest.mark.parametrize("count,sizes,lengths", [(300, [2], [7] * 399 + [100_003]), (60, [3, 8, 1], [400] * 9 + [4_096, 4_097, 0]),
+                                                 (1, [8], [0, 1, 5_000, 1, 2, 3, 1, 2]), (200, [1, 2, 0], [3] * 150 + [60_000] * 2)])
+def test_long_answers_among_short_ones_in_small_batches(T, count, sizes, lengths):
+    rng = np.random.default_rng([count, len(lengths)])
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    n_seqs = int(groups[-1])
+    seqs = np.concatenate([[0], np.cumsum(np.resize(lengths, n_seqs))]).astype(np.int64)
+    assert seqs[-1] <= 1_024 * n_seqs
+    n = int(seqs[-1])
+    lp = -rng.exponential(size=n).astype(np.float32)
+    ref, scores = (lp + rng.normal(0, 0.3, n)).astype(np.float32), rng.normal(size=n_seqs).astype(np.float32)
+    for mask in (None, rng.random(n) < 0.8):
+        for mean in (False, True):
+            _check_preference(T, seqs, lp, ref, mask, scores, groups, 0.01, 0.1, 1.0, mean, f"{count} of {sizes} {mean}")
+    inner = groups[1:-1]  # sequences before the first and after the last group
+    if len(inner) > 1:
+        _check_preference(T, seqs, lp, ref, None, scores, inner, 0.01, 0.0, 1.0, True, "outside")
