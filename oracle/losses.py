@@ -97,7 +97,7 @@ def group_advantage(scores, group_offsets, eps, center_only=False):
     with np.errstate(invalid="ignore"):
         for a, b in _segments(group_offsets, len(s)):
             if b > a:
-                out[a:b] = s[a:b] - s[a:b].mean()
+                out[a:b] = s[a:b] - s[a:b].mean() if np.isfinite(s[a:b]).all() else np.nan
                 if not center_only:
                     out[a:b] /= s[a:b].std() + eps
     return out

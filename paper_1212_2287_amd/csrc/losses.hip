@@ -678,7 +678,8 @@ __global__ void __launch_bounds__(kThreads) advantage_kernel(Tokens in, float ep
                 squares += d * d;
             }
         });
-        const double by = center ? 1.0 : 1.0 / (sqrt(lanes.sum(squares) / count) + eps);
+        const double std_ = sqrt(lanes.sum(squares) / count); // NaN if a score is infinite or NaN
+        const double by = isnan(std_) ? std_ : center ? 1.0 : 1.0 / (std_ + eps);
         lanes.template each<kHold>(q, again, [&](int k, int64_t t, int some) {
             float d[kFour];
 #pragma unroll

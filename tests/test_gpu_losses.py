@@ -565,3 +565,17 @@ def test_long_answers_among_short_ones_in_small_batches(T, count, sizes, lengths
     inner = groups[1:-1]  # sequences before the first and after the last group
     if len(inner) > 1:
         _check_preference(T, seqs, lp, ref, None, scores, inner, 0.01, 0.0, 1.0, True, "outside")
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("size", [3, 70, 400, 3_000])
+def test_centred_advantages_of_special_scores(T, size, value):
+    """A NaN or an infinity makes its whole group NaN, centred or standardised, and no other group."""
+    scores = np.random.default_rng(size).normal(size=4 * size).astype(np.float32)
+    scores[size + size // 2] = value
+    groups = np.arange(0, 4 * size + 1, size)
+    for flags in (0, T.TREE_ENS_CENTER_ONLY):
+        got = T.tree_ens_group_advantage(_dev(scores), _dev(groups), flags=flags).cpu().numpy()
+        assert np.isnan(got[size:2 * size]).all() and np.isfinite(np.delete(got, np.s_[size:2 * size])).all()
+        want = O.group_advantage(scores, groups, 1e-6, bool(flags))
+        assert np.array_equal(np.isnan(got), np.isnan(want))
