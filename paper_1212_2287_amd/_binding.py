@@ -401,6 +401,8 @@ def _elsewhere(device, stream):
         return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device)
+    elif stream.device != device:
+        raise TypeError(f"stream must be on the tensors' device {device}, not on {stream.device}")
     return torch.cuda.stream(stream)
 
 

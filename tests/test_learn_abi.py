@@ -129,3 +129,16 @@ def test_binding_refuses_host_tensors():
         T.tree_ens_group_advantage(torch.zeros(2), off)
     with pytest.raises(TypeError, match="logp"):
         T.tree_ens_policy_loss(torch.zeros(2), None, torch.zeros(1), off)
+
+
+def test_binding_refuses_a_stream_of_another_device(monkeypatch):
+    """Work on it would go to the tensors' device all the same, unordered with it."""
+    import torch
+    from types import SimpleNamespace
+
+    from paper_1212_2287_amd import _binding as B
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: ("inside", stream))
+    here, there = (SimpleNamespace(cuda_stream=7, device=torch.device("cuda", k)) for k in (0, 1))
+    assert B._elsewhere(torch.device("cuda", 0), here) == ("inside", here)
+    with pytest.raises(TypeError, match="stream"):
+        B._elsewhere(torch.device("cuda", 0), there)
