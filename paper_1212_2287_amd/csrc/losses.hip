@@ -2,7 +2,8 @@
 // advantages of scores relative to their group, on gfx950.
 //
 // Segments: sequence s owns tokens [seq_offsets[s], seq_offsets[s+1]), group g owns sequences
-// [group_offsets[g], group_offsets[g+1]). Sums over tokens and over pairs are held in double.
+// [group_offsets[g], group_offsets[g+1]). Sums over tokens are held in double, those over pairs in float for up
+// to 128 pairs of one candidate and in double beyond.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -311,7 +312,7 @@ template <int kGroup> __global__ void __launch_bounds__(kThreads) spread_kernel(
 // and a reciprocal. Adding a pair's slope to both candidates by LDS atomics, which halves the pairs, took 95 us
 // where meeting each pair from both sides takes 42 (909 groups of 110, by pairs_kernel).
 constexpr int kHeld = 512;  // candidates of a group that are held in LDS
-constexpr unsigned kChain = 128; // pairs whose losses and slopes are added in float
+constexpr int kChain = 128; // pairs whose losses and slopes are added in float
 
 // What the pairs that a thread met add up to: (1 - smoothing) max(-d, 0) + log1p(exp(-|d|)), max(d, 0) and 1.
 struct Met {
@@ -353,39 +354,47 @@ template <bool kLoss> __device__ __forceinline__ float meet(float2 me, float2 ot
     return ahead ? dl : behind ? -dl : 0.0f;
 }
 
+// `me` meets every step-th candidate of `others` from k on below `end`: returns the sum of its slopes, and with kLoss
+// adds weight times the losses.
+template <bool kLoss>
+__device__ __forceinline__ double meet_every(float2 me, const float2 *others, int &k, int end, int step, float smoothing, double weight, Loss &loss) {
+    double slope = 0.0;
+    while (k < end) {
+        const int stop = min(end, k + kChain * step);
+        Met met{0.0f, 0.0f, 0};
+        float sum = 0.0f;
+#pragma unroll 4
+        for (; k < stop; k += step)
+            sum += meet<kLoss>(me, others[k], smoothing, met);
+        if (kLoss)
+            loss.add(met, smoothing, weight);
+        slope += sum;
+    }
+    return slope;
+}
+
 // The n <= kHeld candidates of a group lie twice in a row, so that i + k needs no remainder. In step k
 // candidate i meets i + k (modulo n), for its own slope alone, so nothing is added atomically; the first
 // half of the steps meets every pair once and takes its loss. One thread takes candidate i in every
 // `shares`-th step from 1 + share on; returns its slope.
 __device__ __forceinline__ float meet_held(const float2 *held, int n, int i, int share, int shares, float smoothing, Loss &loss) {
     const float2 me = held[i], *other = held + i;
-    Met met{0.0f, 0.0f, 0}, unused = met;
-    float slope = 0.0f;
     int k = 1 + share;
-#pragma unroll 4
-    for (; k <= (n - 1) / 2; k += shares)
-        slope += meet<true>(me, other[k], smoothing, met);
+    double slope = meet_every<true>(me, other, k, (n + 1) / 2, shares, smoothing, 1.0, loss);
     if (2 * k == n) { // opposite each other: the lower one takes the loss
-        slope += meet<true>(me, other[k], smoothing, i < k ? met : unused);
+        Met met{0.0f, 0.0f, 0};
+        slope += meet<true>(me, other[k], smoothing, met);
+        if (i < k)
+            loss.add(met, smoothing, 1.0);
         k += shares;
     }
-#pragma unroll 4
-    for (; k < n; k += shares)
-        slope += meet<false>(me, other[k], smoothing, met);
-    loss.add(met, smoothing, 1.0);
-    return slope;
+    return float(slope + meet_every<false>(me, other, k, n, shares, smoothing, 0.0, loss));
 }
 
 // One thread's candidate against the kHeld or fewer of a larger group that are held: every pair is met
 // twice.
-__device__ __forceinline__ float meet_window(float2 me, const float2 *held, int fit, int share, int shares, float smoothing, Loss &loss) {
-    Met met{0.0f, 0.0f, 0};
-    float slope = 0.0f;
-#pragma unroll 4
-    for (int j = share; j < fit; j += shares)
-        slope += meet<true>(me, held[j], smoothing, met);
-    loss.add(met, smoothing, 0.5);
-    return slope;
+__device__ __forceinline__ double meet_window(float2 me, const float2 *held, int fit, int share, int shares, float smoothing, Loss &loss) {
+    return meet_every<true>(me, held, share, fit, shares, smoothing, 0.5, loss);
 }
 
 // Sequences outside every group have no gradient: those before the first and after the last group, for the
@@ -591,7 +600,7 @@ template <int kN> __device__ __forceinline__ void meet_in_memory(const Preferenc
         const float2 me = make_float2(margins[i], scores[i]);
         double sum = 0.0;
         for (unsigned j = 0; j < n;) {
-            const unsigned end = kN < kWave ? n : min(j + kChain, n); // fewer lanes have kFewMost at most
+            const unsigned end = kN < kWave ? n : min(j + unsigned(kChain), n); // fewer lanes have kFewMost at most
             Met met{0.0f, 0.0f, 0};
             float slope = 0.0f;
 #pragma unroll 2

@@ -579,3 +579,30 @@ def test_centred_advantages_of_special_scores(T, size, value):
         assert np.isnan(got[size:2 * size]).all() and np.isfinite(np.delete(got, np.s_[size:2 * size])).all()
         want = O.group_advantage(scores, groups, 1e-6, bool(flags))
         assert np.array_equal(np.isnan(got), np.isnan(want))
+
+
+@pytest.mark.parametrize("count,sizes", [(1_212, [96] * 605 + [2_040]), (1_212, [96] * 605 + [2_500]), (60, [20] * 29 + [700]),
+                                         (3_000, [2] * 2_999 + [2_000]), (1, [2_047])])
+def test_many_alike_pairs_add_up(T, count, sizes):
+    """The best answer of a large group leads all others, which are alike, by the same margin: adding equal terms rounds
+    the same way each time. A pair is off by 32 u, and a chain of 128 floats adds 64 u to each at most."""
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    n = int(groups[-1])
+    lp, scores = np.zeros(n, np.float32), -np.arange(n, dtype=np.float32)
+    for lead in (0.1, 0.3, 0.7, 1.1, 2.3):
+        lp[groups[:-1]] = lead
+        loss, _, grad = T.tree_ens_preference_loss(_dev(lp), _dev(np.arange(n + 1)), _dev(scores), _dev(groups), beta=1.0)
+        for g in range(0, count, max(1, count // 20)) if count > 60 else range(count):
+            _alike(loss[g:g + 1], grad[groups[g]:groups[g + 1]], lead, f"group {g}")
+        _alike(loss[-1:], grad[groups[-2]:], lead, "last group")
+
+
+def _alike(loss, grad, lead, what):
+    n, d = grad.numel(), float(np.float32(lead))
+    pairs = n * (n - 1) / 2
+    rank = np.arange(1, n)  # of the others, from the second best on: with r others ahead and n - 1 - r behind
+    slope, even = -1 / (1 + np.exp(d)), 0.5
+    want = np.concatenate([[(n - 1) * slope], -slope + even * (rank - 1) - even * (n - 1 - rank)]) / pairs
+    _close(grad, want, 100 * U * (n - 1) / pairs + 4 * U * np.abs(want), what + " gradient")
+    mean = ((n - 1) * np.log1p(np.exp(-d)) + (pairs - (n - 1)) * np.log(2)) / pairs
+    _close(loss, np.array([mean]), 100 * U, what + " loss")
