@@ -606,3 +606,34 @@ def _alike(loss, grad, lead, what):
     _close(grad, want, 100 * U * (n - 1) / pairs + 4 * U * np.abs(want), what + " gradient")
     mean = ((n - 1) * np.log1p(np.exp(-d)) + (pairs - (n - 1)) * np.log(2)) / pairs
     _close(loss, np.array([mean]), 100 * U, what + " loss")
+
+
+@pytest.mark.parametrize("count,sizes", [
+    (300, [2] * 99 + [9]), (3_000, [2] * 99 + [9]), (3_000, [1, 2, 3, 20, 30, 2, 3, 1, 2]),  # more candidates than lanes
+    (60, [30] * 28 + [513, 1_500]), (700, [10] * 69 + [512]),                                # the windows of a workgroup
+])
+def test_groups_of_every_size_among_small_ones(T, count, sizes):
+    rng = np.random.default_rng([count, len(sizes)])
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    n_seqs = int(groups[-1])
+    seqs = np.concatenate([[0], np.cumsum(rng.integers(0, 12, n_seqs))]).astype(np.int64)
+    n = int(seqs[-1])
+    lp, ref = -rng.exponential(size=n).astype(np.float32), -rng.exponential(size=n).astype(np.float32)
+    scores = (np.round(rng.normal(size=n_seqs) * 8) / 8).astype(np.float32)
+    for smoothing, mean in ((0.0, False), (0.2, True)):
+        _check_preference(T, seqs, lp, ref, rng.random(n) < 0.8, scores, groups, 0.2, smoothing, 1.0, mean, f"{count} of {sizes}")
+
+
+@pytest.mark.parametrize("count,sizes", [(5_000, [1] * 4_999 + [3_000]), (5_000, [3] * 2_499 + [2_000]), (600, [80] * 99 + [4_000]),
+                                         (300, [200] * 99 + [2_049]), (120, [300] * 59 + [9_000])])
+def test_advantages_of_a_large_group_among_small_ones(T, count, sizes):
+    rng = np.random.default_rng([count, sizes[-1]])
+    groups = np.concatenate([[0], np.cumsum(np.resize(sizes, count))]).astype(np.int64)
+    scores = (5 + 0.1 * rng.normal(size=int(groups[-1]))).astype(np.float32)
+    for flags in (0, T.TREE_ENS_CENTER_ONLY):
+        x = _dev(scores)
+        got = T.tree_ens_group_advantage(x, _dev(groups), eps=1e-3, flags=flags)
+        want = O.group_advantage(scores, groups, float(np.float32(1e-3)), bool(flags))
+        _close(got, want, 4 * U * np.abs(want) + 1e-12, f"{count} of {sizes} {flags}")
+        T.tree_ens_group_advantage(x, _dev(groups), eps=1e-3, flags=flags, advantages=x)
+        assert bool((x == got).all())
