@@ -377,6 +377,9 @@ def tree_ens_predict_topk(h, X, group_offsets, k: int, scores=None, top_idx=None
 
 # ----------------------------------------------------------------------------------------------
 # learning from scores
+#
+# No call records an autograd graph, whether its inputs require gradients or not: what it returns has none, and
+# gradients are handed on by the caller (logits.backward(grad_logits) where torch made the logits).
 # ----------------------------------------------------------------------------------------------
 def _vector(name, t, dtypes, n, device):
     """Check a contiguous device vector of n entries (any number if n is None)."""
@@ -448,7 +451,8 @@ def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool 
                         stats=None, stream=None):
     """Log-probabilities of ``targets`` (device int64 [n_tokens]; outside [0, n_vocab): not counted) under
     softmax(scale * logits): (logp float32 [n_tokens], entropy float32 [n_tokens] or None, stats float32
-    [n_tokens, 2] for the gradient). Rows of ``logits`` may lie any stride apart."""
+    [n_tokens, 2] for the gradient). Rows of ``logits`` may lie any stride apart. No autograd graph is recorded:
+    tree_ens_token_logp_backward gives the gradient."""
     import torch
     code, n, v, stride = _check_logits(logits, targets)
     f32, dev = torch.float32, logits.device
@@ -478,7 +482,8 @@ def tree_ens_token_logp(logits, targets, scale: float = 1.0, want_entropy: bool 
 def tree_ens_token_logp_backward(logits, targets, stats, grad_logp, scale: float = 1.0, entropy=None, grad_entropy=None,
                                  grad_logits=None, stream=None):
     """The gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to ``logits``, in their type
-    (``entropy`` as the forward gave it; both or neither). ``grad_logits`` may be ``logits`` itself."""
+    (``entropy`` as the forward gave it; both or neither). ``grad_logits`` may be ``logits`` itself.
+    ``logits.backward(grad_logits)`` hands it on where torch's autograd made the logits."""
     import torch
     code, n, v, stride = _check_logits(logits, targets)
     f32, dev = torch.float32, logits.device
@@ -534,7 +539,7 @@ def tree_ens_preference_loss(logp, seq_offsets, scores, group_offsets, ref_logp=
                              loss=None, margins=None, grad_logp=None, stream=None):
     """Pairwise preference loss of each group's sequences, in the order of their ``scores``, on log ratios to a
     reference model: (loss float32 [n_groups], margins float32 [n_seqs], gradient of grad_scale * loss.sum() with
-    respect to ``logp``, or None without ``want_grad``)."""
+    respect to ``logp``, or None without ``want_grad``). No autograd graph is recorded."""
     import torch
     n, n_seqs = _check_tokens(logp, seq_offsets, mask, ref_logp=ref_logp, grad_logp=grad_logp)
     dev = logp.device
@@ -579,7 +584,8 @@ def tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None,
                          want_grad: bool = True, loss=None, kl=None, grad_logp=None, stream=None):
     """Clipped policy loss of each sequence with kl_coef times its KL estimate to a reference model: (loss float32
     [n_seqs], kl float32 [n_seqs] or None without ``ref_logp``, gradient of grad_scale * loss.sum() with respect to
-    ``logp``, or None without ``want_grad``). ``old_logp`` None: the tokens were sampled by this very policy."""
+    ``logp``, or None without ``want_grad``). ``old_logp`` None: the tokens were sampled by this very policy.
+    No autograd graph is recorded."""
     import torch
     n, n_seqs = _check_tokens(logp, seq_offsets, mask, old_logp=old_logp, ref_logp=ref_logp, grad_logp=grad_logp)
     dev = logp.device

@@ -377,3 +377,23 @@ def test_scales_up_to_the_largest_float(T):
     out = T.tree_ens_token_logp_backward(d, td, got[2], g, scale=scale, entropy=got[1], grad_entropy=h).double().cpu().numpy()
     ref = O.token_logp_grad(x, t, np.full(3, 0.25), np.full(3, 0.125), scale)
     assert (np.abs(out - ref) <= 32 * U * scale).all()
+
+
+def test_gradient_handed_on_to_autograd(T):
+    """Outputs carry no graph, and logits.backward(grad_logits) reaches the weights behind the logits as autograd's own
+    log_softmax does."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(0)
+    hidden = torch.randn(40, 16, generator=g, device="cuda")
+    weight = torch.randn(16, 300, generator=g, device="cuda", requires_grad=True)
+    t = torch.randint(0, 300, (40,), generator=g, device="cuda")
+    grad_logp = torch.randn(40, generator=g, device="cuda")
+    logits = hidden @ weight
+    logp, _, stats = T.tree_ens_token_logp(logits, t)
+    assert not logp.requires_grad and not stats.requires_grad
+    logits.backward(T.tree_ens_token_logp_backward(logits, t, stats, grad_logp))
+    got, weight.grad = weight.grad, None
+    wide = (hidden.double() @ weight.detach().double()).requires_grad_()
+    (torch.log_softmax(wide, 1).gather(1, t[:, None])[:, 0] * grad_logp).sum().backward()
+    # logits of 16 products are off by 16 u of about 30, and the gradient as much; 40 of them are added
+    assert torch.allclose(got.double(), hidden.double().t() @ wide.grad, rtol=0, atol=1e-3)
