@@ -182,8 +182,8 @@ template <int kGroup> __device__ __forceinline__ Running row_join(Running r, int
 }
 
 // kGroup threads take a row, in workgroups of at least kThreads. Bound by memory: 16,384 rows of 131,072
-// (bf16) with entropies go in 620 us, 6.9 TB/s; their instructions (8.7 a logit, one of them exp2) come close
-// behind.
+// (bf16) with entropies go in 620 us, 6.9 TB/s (in a row of passes; 669 in a trace); their instructions (8.7 a
+// logit, one of them exp2) come close behind.
 template <typename T, bool kEntropy, bool kStream, int kGroup>
 __global__ void __launch_bounds__(kGroup < kThreads ? kThreads : kGroup)
 logp_kernel(const T *logits, int64_t n, int V, int64_t stride, const int64_t *targets, float scale, RowOut out) {
@@ -330,14 +330,15 @@ struct Plan {
     bool stream;             // loads past the caches
 };
 
-// The fewest threads a row that still make 2,000 waves, 8 to a CU, and no more than its vectors can feed.
-// Measured (us, bf16, with entropies; 16 / 64 / 256 / 1,024 threads): 16,384 x 500: 8.6 / 13.3; 16,384 x
-// 2,000: 16.9 / 19.9; 16,384 x 8,000: - / 49 / 66 / 133; 8,192 x 32,000: - / 93 / 93; 16,384 x 131,072:
-// - / 680 / 649; 1,000 x 128,000: - / 74 / 54 / 53; 200 x 128,000: - / - / 28 / 17; 300 x 8,000: - /
-// 7.9 / 6.8 / 6.4; 8,192 x 32,000 with 40% of the rows ignored: - / 69 / 57 (the others' waves are then
-// too few). Few long rows are split: one of 128,000 takes 12.7 us with 1,024 threads, 5.5 in 62
-// shares and their join, 64 of them 15.3 and 10.1; one of 32,000 6.3 and 5.2, where the second launch
-// costs the host what it gains; 200 of 128,000 17.3 and 18.8.
+// The fewest threads a row that still make 2,000 waves, 8 to a CU, and no more than its vectors can
+// feed. Measured (us, bf16, with entropies, in graphs of 20 passes over one to 20 inputs; 16 / 64 / 256
+// / 1,024 threads): 16,384 x 500: 8.6 / 13.3; 16,384 x 2,000: 16.9 / 19.9; 16,384 x 8,000: - / 49 / 66 /
+// 133; 8,192 x 32,000: - / 93 / 93; 16,384 x 131,072: - / 680 / 649; 1,000 x 128,000: - / 74 / 54 / 53;
+// 200 x 128,000: - / - / 28 / 17; 300 x 8,000: - / 7.9 / 6.8 / 6.4; 8,192 x 32,000 with 40% of the rows
+// ignored: - / 69 / 57 (the others' waves are then too few). Few long rows are split: one of 128,000
+// takes 12.7 us with 1,024 threads, 5.5 in 62 shares and their join, 64 of them 15.3 and 10.1; one of
+// 32,000 6.3 and 5.2, where the second launch costs the host what it gains; 200 of 128,000 17.3 and
+// 18.8.
 // Loads past the caches: 16,384 x 131,072 731 -> 649, 16,384 x 8,000 54 -> 49. Below 64 MiB the pass
 // that made the logits has left them in the caches, and the gradient wants them there: a copy, this
 // pass, the gradient and a sum over 256 x 32,000 take 28.4 us with cached loads, 30.8 past the caches.

@@ -308,8 +308,8 @@ template <int kGroup> __global__ void __launch_bounds__(kThreads) spread_kernel(
     zero_outside(in, grad);
 }
 
-// Pairs are bound by instructions: 19 a pair for a slope and 33 with the loss, three (two) of them exp2, log2
-// and a reciprocal. Adding a pair's slope to both candidates by LDS atomics, which halves the pairs, took 95 us
+// Pairs are bound by instructions: 15 a pair for a slope and 30 with the loss, two (three) of them exp2, a reciprocal
+// (and log2). Adding a pair's slope to both candidates by LDS atomics, which halves the pairs, took 95 us
 // where meeting each pair from both sides takes 42 (909 groups of 110, by pairs_kernel).
 constexpr int kHeld = 512;  // candidates of a group that are held in LDS
 constexpr int kChain = 128; // pairs whose losses and slopes are added in float
@@ -513,7 +513,7 @@ constexpr int kHeldPart = 2048;
 
 // One of `parts` shares of a group's candidates, against all of the group. As many threads take a
 // candidate as there are, each every so many steps of it. 13 million ordered pairs of 909 groups take 23 us in
-// three parts, 12 of them for the instructions if every unit had the same number; pairs_kernel, whose
+// three parts, 13 of them for the instructions if every unit had the same number; pairs_kernel, whose
 // workgroups differ more, took 36.
 __global__ void __launch_bounds__(kThreads) pairs_part_kernel(int64_t n_seqs, Preference p, int parts, Loss *partial) {
     __shared__ float2 held[2 * kHeldPart];
@@ -782,8 +782,9 @@ __device__ __forceinline__ double share_of(const Tokens &in, const Policy &p, La
     return 1.0 / fmax(lanes.sum(count), 1.0);
 }
 
-// Bound by memory, 17 bytes a masked token, with the sum of instructions at half of it: 19 million tokens of
-// 4,096 sequences take 73 us (4.4 TB/s). A mean over masked tokens needs their number first, which reads the
+// 17 bytes a masked token: 19 million tokens of 4,096 sequences take 74 us, 4.3 TB/s, 37 of them for the instructions
+// if every unit had the same number. Their lengths differ, 512 to 16,384, and a workgroup takes each: as many tokens in
+// sequences of 4,571 take 61 us. A mean over masked tokens needs their number first, which reads the
 // mask twice, the second time from the cache.
 template <int kGroup>
 __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, int parts, const int64_t *counts, Pair<double> *partial) {
@@ -792,8 +793,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(Tokens in, Policy p, i
         const double share = share_of(in, p, lanes, s, q, parts, counts);
         const float w = float(p.grad_scale * share);
         double loss = 0.0, kl = 0.0;
-        // Four tokens a thread in flight: 84 registers and six waves a SIMD, where eight take 101 and four waves (us, one
-        // / two fours; sequences x mean tokens): 16,384 x 1,620: 101 / 110; 200,000 x 8: 28.5 / 32; 20,000 x 325: 39 / 42;
+        // Four tokens a thread in flight: 84 registers and five waves a SIMD, with a workgroup a sequence 75 and six, where
+        // eight take 101 and four waves (us, one / two fours; sequences x mean tokens): 16,384 x 1,620: 101 / 110; 200,000 x 8: 28.5 / 32; 20,000 x 325: 39 / 42;
         // 97,000 x 116: 70 / 72; 4,096 x 3,700: 60 / 59; 4,096 x 405: 13.9 / 13.7; 4,096 x 4,640: 73 / 72.
         constexpr int kAhead = 1;
         float x[kAhead][kFour], old[kAhead][kFour] = {}, ref[kAhead][kFour] = {};
@@ -892,7 +893,8 @@ int check_tokens(const float *logp, int64_t n_tokens, const int64_t *seq_offsets
 }
 
 // How sequences are shared out: threads for each, or parts of it. By their mean length, and more threads
-// where the sequences are too few for 2,000 waves, 8 to a CU. Measured on the policy loss (us; sequences x mean
+// where the sequences are too few for 2,000 waves, 8 to a CU. The preference loss's margins and gradients follow the
+// same plan. Measured on the policy loss alone (us; sequences x mean
 // tokens: 8 / 16 / 32 / 64 / 256 threads):
 //   200,000 x 24: 39 / 49 / 81 / 152 / 423; 99,000 x 49: 34 / 37 / 47 / 80 / 210; 50,000 x 98: 41 / 31 / 34 / 46 /
 //   111; 30,000 x 195: 60 / 37 / 32 / 37 / 72; 20,000 x 325: - / - / 34 / 35 / 53; 10,000 x 818: - / - / 48 / 36 / 38;
