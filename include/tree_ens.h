@@ -375,6 +375,80 @@ int tree_ens_policy_loss(void *stream, const float *logp, const float *old_logp,
 int tree_ens_policy_workspace(int64_t n_tokens, int64_t n_seqs, int64_t *bytes);
 
 /*
+ * tree_ens_sample -- one token for each row of logits, from a given random number. With
+ * z = scale * (logits - their largest) and weights w = exp(z), tokens in the order of their logits, the
+ * largest first and equal ones by their index, are kept as follows:
+ *   top_k   the first top_k of the order (0: all),
+ *   min_p   of these, the ones with w >= min_p (the largest weight is 1; 0: all),
+ *   top_p   of these, the fewest from the front whose weights make up at least top_p of theirs together
+ *           (1: all; never fewer than one).
+ * The row's token is the first, in the order of the vocabulary, at which the sum of the kept weights
+ * exceeds `uniform` times their total.
+ *
+ *   logits .. row_stride  as for tree_ens_token_logp.
+ *   uniform     device, double [n_tokens], in [0, 1): others count as the nearest such number, NaN as 0.
+ *   scale       finite, > 0: the inverse of the temperature. (top_k = 1 takes the largest logit.)
+ *   top_k       >= 0; top_p in (0, 1]; min_p in [0, 1].
+ *   row_scale, row_top_k, row_top_p, row_min_p  device, float or int32 [n_tokens], or NULL: parameters of
+ *               each row in the place of the four above. A row whose scale is not finite and > 0 has no
+ *               distribution. Beyond their ranges row_top_k <= 0, row_top_p >= 1, row_min_p <= 0 and NaN
+ *               keep all, row_top_p <= 0 and row_min_p >= 1 the largest logit (and row_min_p its equals).
+ *   tokens      device, int64 [n_tokens].
+ *   logp        device, float [n_tokens], or NULL: log softmax(scale * row)[token] over the whole
+ *               vocabulary, what tree_ens_token_logp gives (old_logp of tree_ens_policy_loss).
+ *   log_kept    device, float [n_tokens], or NULL: the logarithm of the share of the probability that the
+ *               kept tokens have, <= 0; logp - log_kept is the log-probability among the kept ones.
+ * Logits of -inf are tokens that cannot be sampled. A row of nothing else has token -1, logp -inf and
+ * log_kept 0; a row with a NaN or +inf, or without a proper scale, token -1, logp and log_kept NaN
+ * (tree_ens_token_logp takes -1 for a row that does not count).
+ *
+ * Weights are whole numbers of 2^-44 (of more from an n_vocab of 2^19 on: their sum stays below 2^63), taken from a
+ * double off by at most 2^-39 of it, so sums are exact in whatever order they are taken, and so is what is
+ * decided by them: a row's token depends neither on the rows beside it nor on their number. Tokens of less than
+ * half a unit are never sampled.
+ */
+int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
+                    int64_t n_vocab, int64_t row_stride, const double *uniform, float scale,
+                    int32_t top_k, float top_p, float min_p, const float *row_scale,
+                    const int32_t *row_top_k, const float *row_top_p, const float *row_min_p,
+                    int64_t *tokens, float *logp, float *log_kept, void *workspace,
+                    int64_t workspace_bytes);
+int tree_ens_sample_workspace(int32_t dtype, int64_t n_tokens, int64_t n_vocab, int64_t *bytes);
+
+/*
+ * tree_ens_grad_norm -- the 2-norm of the elements of many tensors together, such as all gradients of
+ * a model: sqrt(sum of squares), summed in double.
+ *
+ *   n_tensors   >= 0.
+ *   grads       host, [n_tensors] device pointers, each aligned for its type (NULL where the count is 0).
+ *   counts      host, int64 [n_tensors]: elements of each, >= 0, one behind the other in memory.
+ *   dtypes      host, int32 [n_tensors]: TREE_ENS_F32, TREE_ENS_BF16 or TREE_ENS_F16.
+ *   norm        device, float [1]: 0 where there is no element; inf beyond the largest float.
+ * The host arrays are read during the call only. A NaN among the elements makes the norm NaN, an infinity
+ * without one inf. A tensor that is given twice counts twice.
+ */
+int tree_ens_grad_norm(void *stream, int64_t n_tensors, const void *const *grads, const int64_t *counts,
+                       const int32_t *dtypes, float *norm, void *workspace, int64_t workspace_bytes);
+int tree_ens_grad_norm_workspace(int64_t n_tensors, int64_t *bytes);
+
+/*
+ * tree_ens_grad_clip -- many tensors times min(1, max_norm / (norm + eps)), rounded once to their type.
+ *
+ *   n_tensors .. dtypes  as for tree_ens_grad_norm.
+ *   norm        device, float [1]: what tree_ens_grad_norm gave, or the norm over several processes'
+ *               shards.
+ *   max_norm    finite, >= 0; eps finite, >= 0.
+ *   out         host, [n_tensors] device pointers to tensors of the same counts and types. Each may be
+ *               the one of `grads` itself; otherwise none of them may overlap another of `out` or any of
+ *               `grads` (TREE_ENS_E_ARG).
+ * Gradients in place are left alone, and not read, where the factor is 1. A NaN norm makes everything NaN; an
+ * infinite one makes finite elements 0 and the others NaN.
+ */
+int tree_ens_grad_clip(void *stream, int64_t n_tensors, const void *const *grads, const int64_t *counts,
+                       const int32_t *dtypes, const float *norm, float max_norm, float eps,
+                       void *const *out);
+
+/*
  * tree_ens_info -- facts about a packed model; every output pointer may be NULL.
  *   n_trees        number of trees.
  *   min_features   1 + the largest feature id any node reads (0 if there is none).

@@ -10,5 +10,5 @@ from ._binding import (  # noqa: F401
     tree_ens_last_path,
     tree_ens_outputs, tree_ens_policy_loss, tree_ens_predict,
     tree_ens_predict_leaves, tree_ens_predict_noalloc, tree_ens_predict_topk,
-    tree_ens_preference_loss, tree_ens_token_logp, tree_ens_token_logp_backward, tree_ens_topk,
+    tree_ens_preference_loss, tree_ens_grad_clip, tree_ens_grad_norm, tree_ens_sample, tree_ens_token_logp, tree_ens_token_logp_backward, tree_ens_topk,
 )

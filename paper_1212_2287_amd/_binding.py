@@ -102,7 +102,12 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             "tree_ens_preference_workspace": [i64, i64, i64, P],
             "tree_ens_group_advantage": [P, P, i64, P, i64, f32, u32, P],
             "tree_ens_policy_loss": [P, P, P, P, P, i64, P, i64, P, f32, f32, f32, f32, u32, P, P, P, P, i64],
-            "tree_ens_policy_workspace": [i64, i64, P]}.items():
+            "tree_ens_policy_workspace": [i64, i64, P],
+            "tree_ens_sample": [P, P, i32, i64, i64, i64, P, f32, i32, f32, f32, P, P, P, P, P, P, P, P, i64],
+            "tree_ens_sample_workspace": [i32, i64, i64, P],
+            "tree_ens_grad_norm": [P, i64, P, P, P, P, P, i64],
+            "tree_ens_grad_norm_workspace": [i64, P],
+            "tree_ens_grad_clip": [P, i64, P, P, P, P, f32, f32, P]}.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = ctypes.c_int, args
     lib.tree_ens_destroy.restype = None
@@ -427,16 +432,21 @@ def _stream_on(device):
     return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
-def _check_logits(logits, targets):
-    """(dtype code, n_tokens, n_vocab, row stride) of device logits [n_tokens, n_vocab]."""
+def _dtype_codes():
     import torch
-    codes = {torch.float32: TREE_ENS_F32, torch.bfloat16: TREE_ENS_BF16, torch.float16: TREE_ENS_F16}
+    return {torch.float32: TREE_ENS_F32, torch.bfloat16: TREE_ENS_BF16, torch.float16: TREE_ENS_F16}
+
+
+def _check_logits(logits, targets, name="targets", dtype=None):
+    """(dtype code, n_tokens, n_vocab, row stride) of device logits [n_tokens, n_vocab] and a vector over their rows."""
+    import torch
+    codes = _dtype_codes()
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dtype not in codes or \
             logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise TypeError("logits must be a CUDA (HIP) float32, bfloat16 or float16 [n_tokens, n_vocab] tensor with "
                         "contiguous rows")
     n, v = logits.shape
-    _vector("targets", targets, (torch.int64,), n, logits.device)
+    _vector(name, targets, (dtype or torch.int64,), n, logits.device)
     return codes[logits.dtype], n, v, logits.stride(0) if n > 1 else v
 
 
@@ -606,6 +616,127 @@ def tree_ens_policy_loss(logp, old_logp, advantages, seq_offsets, ref_logp=None,
            seq_offsets.data_ptr(), n_seqs, _ptr(advantages), float(clip_low), float(clip_high), float(kl_coef),
            float(grad_scale), int(flags), _ptr(loss), _ptr(kl), _ptr(grad_logp), work, size), "tree_ens_policy_loss")
     return loss, kl, grad_logp
+
+
+def _row_parameter(name, value, dtype, n, device):
+    """(number, device vector or None) of a parameter that is one number or a vector over the rows."""
+    import torch
+    if isinstance(value, torch.Tensor):
+        return 1, _vector(name, value, (dtype,), n, device)
+    return value, None
+
+
+def tree_ens_sample(logits, uniform, scale=1.0, top_k=0, top_p=1.0, min_p=0.0, want_logp: bool = True, tokens=None, logp=None,
+                    log_kept=None, stream=None):
+    """One token of every row of ``logits`` (as for tree_ens_token_logp) under softmax(scale * logits) cut down by ``top_k``
+    (0: off), ``min_p`` (0: off) and ``top_p`` (1: off), from the random numbers ``uniform`` (device float64 [n_tokens] in
+    [0, 1)): (tokens int64 [n_tokens], logp float32 [n_tokens] over the whole vocabulary, as tree_ens_token_logp gives it,
+    log_kept float32 [n_tokens], the logarithm of the share of the probability that is kept; both None without
+    ``want_logp``). ``scale``, ``top_p`` and ``min_p`` may be device float32 vectors over the rows, ``top_k`` an int32 one."""
+    import torch
+    f32 = torch.float32
+    code, n, v, stride = _check_logits(logits, uniform, "uniform", torch.float64)
+    dev = logits.device
+    scale_, row_scale = _row_parameter("scale", scale, f32, n, dev)
+    top_k_, row_top_k = _row_parameter("top_k", top_k, torch.int32, n, dev)
+    top_p_, row_top_p = _row_parameter("top_p", top_p, f32, n, dev)
+    min_p_, row_min_p = _row_parameter("min_p", min_p, f32, n, dev)
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_sample(logits, uniform, scale, top_k, top_p, min_p, want_logp, tokens, logp, log_kept)
+    if tokens is None:
+        tokens = torch.empty(n, dtype=torch.int64, device=dev)
+    else:
+        _vector("tokens", tokens, (torch.int64,), n, dev)
+    if logp is not None or want_logp:
+        logp = _float_out("logp", logp, n, dev)
+    if log_kept is not None or want_logp:
+        log_kept = _float_out("log_kept", log_kept, n, dev)
+    lib = load_library()
+    _keep, work, size = _workspace(lib, dev, "tree_ens_sample_workspace", code, n, v)
+    _check(lib.tree_ens_sample(_stream_on(dev), _ptr(logits), code, n, v, stride, _ptr(uniform), float(scale_),
+           min(int(top_k_), 2**31 - 1), float(top_p_), float(min_p_), _ptr(row_scale), _ptr(row_top_k), _ptr(row_top_p),
+           _ptr(row_min_p), _ptr(tokens), _ptr(logp), _ptr(log_kept), work, size), "tree_ens_sample")
+    return tokens, logp, log_kept
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's elements lie one behind the other, in whatever order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+def _check_grads(grads):
+    """(device, addresses, counts and dtype codes as C arrays) of a sequence of dense device tensors."""
+    import torch
+    grads = list(grads)
+    if not grads or not all(isinstance(t, torch.Tensor) for t in grads):
+        raise TypeError("grads must be a sequence of one tensor or more")
+    dev, codes = grads[0].device, _dtype_codes()
+    if dev.type != "cuda" or any(t.device != dev for t in grads):
+        raise TypeError("grads must be CUDA (HIP) tensors of one device")
+    if not all(t.dtype in codes for t in grads) or not all(_dense(t) for t in grads):
+        raise TypeError("grads must be float32, bfloat16 or float16 tensors without gaps between their elements")
+    n = len(grads)
+    return dev, grads, ((ctypes.c_void_p * n)(*[t.data_ptr() for t in grads]), (ctypes.c_int64 * n)(*[t.numel() for t in grads]),
+                        (ctypes.c_int32 * n)(*[codes[t.dtype] for t in grads]))
+
+
+def tree_ens_grad_norm(grads, norm=None, stream=None):
+    """The 2-norm of the elements of all tensors of ``grads`` together, such as ``[p.grad for p in parameters]``: a float32
+    scalar on their device (``norm``, if given). Types may be mixed; tensors are dense, in any order of their dimensions."""
+    import torch
+    dev, grads, (ptrs, counts, codes) = _check_grads(grads)
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_grad_norm(grads, norm)
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+    else:
+        _check_norm(norm, dev)
+    lib = load_library()
+    _keep, work, size = _workspace(lib, dev, "tree_ens_grad_norm_workspace", len(grads))
+    _check(lib.tree_ens_grad_norm(_stream_on(dev), len(grads), ptrs, counts, codes, norm.data_ptr(), work, size),
+           "tree_ens_grad_norm")
+    return norm
+
+
+def _check_norm(norm, device):
+    import torch
+    if not isinstance(norm, torch.Tensor) or norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != device:
+        raise TypeError("norm must be a float32 tensor of one element on the gradients' device")
+
+
+def tree_ens_grad_clip(grads, norm, max_norm: float, eps: float = 1e-6, out=None, stream=None):
+    """``grads`` times min(1, max_norm / (norm + eps)), each rounded once to its type, in place or into the tensors of
+    ``out`` (of the same shapes, strides and types; they may be some of the same tensors): the tensors written. ``norm`` as
+    tree_ens_grad_norm gives it, or over all processes' shards."""
+    dev, grads, (ptrs, counts, codes) = _check_grads(grads)
+    _check_norm(norm, dev)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads):
+        raise TypeError(f"out must hold {len(grads)} tensors, not {len(out)}")
+    to = ptrs
+    if out is not grads:
+        if any(o.shape != t.shape or o.dtype != t.dtype or o.device != dev or (o.stride() != t.stride() and t.numel() > 1)
+               for o, t in zip(out, grads)):
+            raise TypeError("out must hold tensors of the gradients' shapes, strides, types and device")
+        to = (ctypes.c_void_p * len(out))(*[o.data_ptr() for o in out])
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return tree_ens_grad_clip(grads, norm, max_norm, eps, out)
+    _check(load_library().tree_ens_grad_clip(_stream_on(dev), len(grads), ptrs, counts, codes, norm.data_ptr(), float(max_norm),
+           float(eps), to), "tree_ens_grad_clip")
+    return out
 
 
 def tree_ens_info(h) -> dict:

@@ -1,0 +1,364 @@
+"""GPU sampling through the C ABI, against the float64 oracle on the same (already rounded) logits.
+
+Tokens are equal. Weights are off by 2^-39 of themselves and half a unit (2^-45, for fewer than 2^19 tokens) at most, so
+the total, at least 1, by 2^-39 + 2^-45 V relative, and logp by as much beside its own rounding, 2^-24 of it; the dropped
+weights and the total by the same relative to the total, so log_kept by twice that over the share that is kept."""
+from __future__ import annotations
+
+from fractions import Fraction
+
+import numpy as np
+import pytest
+
+from oracle import sampling as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def T():
+    import paper_1212_2287_amd as T
+    T.load_library()
+    return T
+
+
+def _torch_dtype(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def _logits(dtype, n, V, pad=0, first=0, seed=0, banned=0.0, spread=2.0, peak=9.0):
+    """Device logits [n, V] with rows V + pad apart, the first one `first` elements into its allocation, the values
+    they stand for, and a random number for each row. Peaks of 0 to `peak` stand out of noise."""
+    import torch
+    rng = np.random.default_rng([seed, n, V])
+    x = rng.normal(0, spread, (n, V))
+    for r in range(n):
+        at = rng.integers(0, V, min(V, 40))
+        x[r, at] += rng.uniform(0, peak) - 0.8 * np.log(np.arange(1, len(at) + 1))
+    if banned:
+        x[:, rng.random(V) < banned] = -np.inf
+        x[:, V // 2] = 1.0
+    flat = torch.zeros(first + n * (V + pad), dtype=_torch_dtype(dtype), device="cuda")
+    d = flat[first:].view(n, V + pad)[:, :V]
+    d.copy_(torch.from_numpy(x))
+    return d, d.double().cpu().numpy(), rng.random(n)
+
+
+def _dev(a, dtype=None):
+    import torch
+    return torch.from_numpy(np.array(a, dtype=dtype)).cuda()
+
+
+def _check(got, want, V, what):
+    tokens, logp, log_kept = (g.cpu().numpy() for g in got)
+    assert np.array_equal(tokens, want[0]), (what, np.nonzero(tokens != want[0])[0][:5], tokens[:5], want[0][:5])
+    off = 2.0 ** -39 + 2.0 ** -45 * max(V, 1) * max(1.0, V / 2 ** 18)
+    for name, a, b, e in (("logp", logp, want[1], off + U * np.abs(want[1])),
+                          ("log_kept", log_kept, want[2], 2 * off / np.exp(want[2]) + U * np.abs(want[2]))):
+        fine = np.isfinite(b)
+        assert np.array_equal(a[~fine], b[~fine], equal_nan=True), (what, name)
+        err = np.abs(a[fine].astype(np.float64) - b[fine]) - e[fine]
+        assert (err <= 0).all(), (what, name, float(err.max()))
+    assert not (log_kept > 0).any()
+
+
+def _f32(v):
+    return float(np.float32(v))
+
+
+SHAPES = [
+    # tokens, vocabulary, padding of a row, elements before the first row
+    (1, 1, 0, 0), (3, 2, 0, 0), (5, 7, 1, 1), (9, 63, 0, 0), (4, 64, 0, 0), (300, 65, 0, 3), (17, 255, 2, 0), (8, 257, 0, 1),
+    (30, 1000, 0, 0), (33, 1023, 0, 0), (6, 2047, 2, 5), (5, 2048, 0, 0), (3, 2049, 7, 0), (5, 4095, 0, 0), (4, 4097, 1, 0),
+    (4, 8193, 8, 0), (2, 20_001, 0, 0), (5, 32_000, 0, 0), (2, 65_537, 0, 1), (2, 131_072, 0, 0), (6, 50_001, 0, 0),
+]
+PARAMS = [
+    dict(), dict(scale=0.7), dict(top_k=1), dict(top_k=50), dict(top_k=700), dict(top_p=0.9), dict(top_p=0.3, scale=1.6),
+    dict(min_p=0.05), dict(top_k=40, top_p=0.8, min_p=0.01), dict(top_k=5_000, top_p=0.97), dict(min_p=1.0), dict(top_p=1e-6),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,V,pad,first", SHAPES)
+def test_against_the_oracle(T, dtype, n, V, pad, first):
+    what = f"{dtype} {n} x {V} + {pad} from {first}"
+    print("[sample]", what, flush=True)
+    for k, params in enumerate(PARAMS):
+        if n * V > 100_000 and k % 3 != (n + V) % 3:
+            continue
+        params = {p: v if p == "top_k" else _f32(v) for p, v in params.items()}
+        d, x, u = _logits(dtype, n, V, pad, first, seed=k, banned=0.4 if k % 2 else 0.0, peak=(14.0, 3.0)[k % 5 == 0])
+        got = T.tree_ens_sample(d, _dev(u), **params)
+        _check(got, O.sample(x, u, **params), V, (what, params))
+        tokens, none, also = T.tree_ens_sample(d, _dev(u), want_logp=False, **params)
+        assert none is None and also is None and (tokens == got[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [1, 2, 5, 300, 3000, 5000, 40_000])
+def test_rows_of_special_values(T, dtype, V):
+    import torch
+    lowest = torch.finfo(_torch_dtype(dtype)).min
+    n = 12
+    x = np.random.default_rng(V).normal(0, 2, (n, V))
+    x[0] = -np.inf                     # nothing can be sampled
+    x[1] = -np.inf
+    x[1, V - 1] = 2.0                  # one token
+    x[2] = lowest                      # masked by the lowest value, all alike
+    x[3] = lowest
+    x[3, V - 1] = 0.5
+    x[4, V // 2] = np.nan
+    x[5, V // 2] = np.inf
+    x[6] = 0.0                         # equals by index, whatever the sign of their zero
+    x[6, ::2] = -0.0
+    x[7] = -lowest                     # the largest
+    x[8] = np.where(np.arange(V) % 3, 1.0, 2.0)
+    x[9, V // 2] = -np.nan
+    x[10] = -np.inf
+    x[10, V // 3:V // 3 + 2] = [-lowest, lowest][:len(x[10, V // 3:V // 3 + 2])]
+    x[11, 0] = -lowest
+    d = torch.from_numpy(x).to(_torch_dtype(dtype)).cuda()
+    x = d.double().cpu().numpy()
+    for k, params in enumerate(({}, dict(top_k=2), dict(top_p=0.5), dict(min_p=0.5), dict(top_k=max(V - 1, 1), top_p=0.75, min_p=0.25))):
+        for u in (np.random.default_rng(k).random(n), np.zeros(n), np.full(n, 1 - 2.0 ** -53)):
+            _check(T.tree_ens_sample(d, _dev(u), **params), O.sample(x, u, **params), V, (dtype, V, params, u[0]))
+
+
+@pytest.mark.parametrize("V", [1000, 6000, 70_000])
+@pytest.mark.parametrize("levels", [1, 2, 7])
+def test_many_equal_logits(T, V, levels):
+    """Borders of top-k and top-p inside runs of equals, far longer than any list of candidates: the first by index stay."""
+    rng = np.random.default_rng([V, levels])
+    n = 16
+    x = rng.integers(0, levels, (n, V)) * 0.75
+    d, u = _dev(x, np.float32), rng.random(n)
+    top_p = rng.uniform(0.01, 0.99, n).astype(np.float32)
+    top_k = rng.integers(1, V + 1, n).astype(np.int32)
+    for dtype in ("f32", "bf16", "f16"):
+        for params in (dict(top_p=top_p), dict(top_k=top_k), dict(top_k=top_k, top_p=top_p), dict(min_p=0.3, top_p=top_p)):
+            given = {k: _dev(v) if isinstance(v, np.ndarray) else _f32(v) for k, v in params.items()}
+            params = {k: v if isinstance(v, np.ndarray) else _f32(v) for k, v in params.items()}
+            _check(T.tree_ens_sample(d.to(_torch_dtype(dtype)), _dev(u), **given), O.sample(x, u, **params), V, (V, levels, dtype, list(params)))
+
+
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 40, 300), ("f32", 24, 5_000), ("f16", 16, 60_001)])
+def test_parameters_of_each_row(T, dtype, n, V):
+    d, x, u = _logits(dtype, n, V, seed=4)
+    rng = np.random.default_rng(V)
+    scale = rng.uniform(0.5, 2.0, n).astype(np.float32)
+    top_k = np.where(rng.random(n) < 0.5, 0, rng.integers(1, V, n)).astype(np.int32)
+    top_p = np.where(rng.random(n) < 0.4, 1.0, rng.random(n)).astype(np.float32)
+    min_p = np.where(rng.random(n) < 0.5, 0.0, rng.uniform(0, 0.2, n)).astype(np.float32)
+    got = T.tree_ens_sample(d, _dev(u), scale=_dev(scale), top_k=_dev(top_k), top_p=_dev(top_p), min_p=_dev(min_p))
+    _check(got, O.sample(x, u, scale, top_k, top_p, min_p), V, "rows' own")
+    _check(T.tree_ens_sample(d, _dev(u), scale=1.25, top_p=_dev(top_p)), O.sample(x, u, 1.25, 0, top_p), V, "some of them")
+    # beyond their ranges: (given, what it counts as)
+    for name, kind, given, counts in (("top_k", np.int32, [-3, 0, V, V + 9, 2**31 - 1], [0, 0, 0, 0, 0]),
+                                      ("top_p", np.float32, [-1.0, 0.0, 1.5, np.inf, np.nan], [1e-9, 1e-9, 1, 1, 1]),
+                                      ("min_p", np.float32, [-1.0, 0.0, 1.5, np.inf, np.nan], [0, 0, 1, 1, 0])):
+        got = T.tree_ens_sample(d[:5], _dev(u[:5]), **{name: _dev(given, kind)})
+        _check(got, O.sample(x[:5], u[:5], **{name: counts}), V, (name, "beyond its range"))
+    wrong = _dev([1.0, 0.0, -1.0, np.inf, np.nan], np.float32)
+    tokens, logp, log_kept = (t.cpu().numpy() for t in T.tree_ens_sample(d[:5], _dev(u[:5]), scale=wrong))
+    assert tokens[0] >= 0 and (tokens[1:] == -1).all() and np.isnan(logp[1:]).all() and np.isnan(log_kept[1:]).all()
+
+
+def test_random_numbers_at_the_borders(T):
+    """Weights that are exact: a running sum that the random number equals is not past it. Others count as the nearest
+    in [0, 1), NaN as 0."""
+    for V in (4, 4096, 8192):
+        u = np.array([0.0, 0.25, 0.5, 0.75, 0.25 - 2.0 ** -53, 0.75 - 2.0 ** -53, 1 - 2.0 ** -53])
+        d = _dev(np.zeros((len(u), V)), np.float32)
+        assert T.tree_ens_sample(d, _dev(u))[0].tolist() == [int(f * V) for f in u]
+        assert T.tree_ens_sample(d, _dev(u), top_k=4)[0].tolist() == [0, 1, 2, 3, 0, 2, 3]
+        beyond = np.array([-0.5, 1.0, 2.0, np.inf, -np.inf, np.nan, -0.0])
+        assert T.tree_ens_sample(d, _dev(beyond))[0].tolist() == [0, V - 1, V - 1, V - 1, 0, 0, 0]
+
+
+@pytest.mark.parametrize("V", [50, 6_000])
+def test_even_random_numbers_give_the_distribution(T, V):
+    """n even random numbers hit a token n p times, give or take one."""
+    import torch
+    n = 4_000
+    d, x, _ = _logits("f32", 1, V, seed=2)
+    u = (np.arange(n) + 0.5) / n
+    tokens, _, _ = T.tree_ens_sample(d.repeat(n, 1), _dev(u), scale=1.5, top_k=30, top_p=0.875)
+    order, w = O.kept_tokens(x[0], 1.5, 30, 0.875)
+    p = np.zeros(V)
+    p[order] = w[order] / w[order].sum()
+    assert np.abs(np.bincount(tokens.cpu().numpy(), minlength=V) - n * p).max() <= 1 + 1e-6
+    assert isinstance(tokens, torch.Tensor) and tokens.dtype == torch.int64
+
+
+@pytest.mark.parametrize("V", [700, 9_000])
+def test_scales_of_any_size(T, V):
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 3, (6, V)).astype(np.float32)
+    u = rng.random(6)
+    for scale in (1e-30, 1e-6, 0.01, 30.0, 1e6, 3e38):
+        for params in ({}, dict(min_p=0.1), dict(top_p=0.5), dict(top_k=V // 2)):
+            params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
+            _check(T.tree_ens_sample(_dev(x), _dev(u), scale=_f32(scale), **params), O.sample(x, u, _f32(scale), **params), V, (scale, params))
+
+
+@pytest.mark.parametrize("V", [524_287, 524_288, 3_000_001])
+def test_the_largest_vocabularies(T, V):
+    """Units grow so that the sum stays in its 63 bits; equal weights of a power of two are exact all the same."""
+    import torch
+    d = torch.zeros(3, V, dtype=torch.bfloat16, device="cuda")
+    d[1, ::2] = -1.0
+    u = np.array([0.5, 0.25, 0.999])
+    x = d.double().cpu().numpy()
+    tokens, logp, _ = (t.cpu().numpy() for t in T.tree_ens_sample(d, _dev(u)))
+    w = np.exp(x)
+    for r in range(3):
+        c = np.cumsum(w[r])
+        assert abs(tokens[r] - np.searchsorted(c, u[r] * c[-1], side="right")) <= (0 if r != 1 else 1)
+        assert abs(logp[r] - (x[r, tokens[r]] - np.log(c[-1]))) <= 2 * U * abs(logp[r])
+    kept = T.tree_ens_sample(d[1:2].repeat(3, 1), _dev(u), top_k=_dev([1, 1000, V // 2], np.int32))
+    order = 1 + 2 * np.arange(V // 2)
+    # the product of the random number as it is, which a double's would round up to a whole number at 1,500,000 tokens
+    assert kept[0].tolist() == [order[0], order[250], order[int(Fraction(u[2]) * (V // 2))]]
+
+
+def test_rows_do_not_depend_on_their_batch(T):
+    for dtype, n, V in (("bf16", 600, 5_000), ("f32", 70, 33_001), ("f16", 300, 300)):
+        d, _, u = _logits(dtype, n, V, seed=6)
+        u = _dev(u)
+        whole = T.tree_ens_sample(d, u, top_p=0.9)
+        for r in (0, 1, n // 2, n - 1):
+            for a, b in zip(whole, T.tree_ens_sample(d[r:r + 1], u[r:r + 1], top_p=0.9)):
+                assert (a[r:r + 1] == b).all(), (dtype, r)
+
+
+def test_another_stream_and_equal_bits(T):
+    import torch
+    d, _, u = _logits("bf16", 37, 30_011)
+    u = _dev(u)
+    side = torch.cuda.Stream()
+    first = T.tree_ens_sample(d, u, top_p=0.8)
+    side.wait_stream(torch.cuda.current_stream())
+    again = T.tree_ens_sample(d, u, top_p=0.8, stream=side)
+    raw = T.tree_ens_sample(d, u, top_p=0.8, stream=side.cuda_stream)
+    side.synchronize()
+    for a, b, c in zip(first, again, raw):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_two_calls_at_once(T):
+    """Calls on two streams with workspaces of their own."""
+    import torch
+    d, _, u = _logits("f32", 64, 20_000, seed=1)
+    e, _, v = _logits("f32", 64, 20_000, seed=2)
+    u, v = _dev(u), _dev(v)
+    want = [T.tree_ens_sample(d, u, top_p=0.9), T.tree_ens_sample(e, v, top_k=30)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        got = [T.tree_ens_sample(d, u, top_p=0.9), T.tree_ens_sample(e, v, top_k=30, stream=side)]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+
+def test_offsets_past_32_bits(T):
+    """Rows whose logits lie beyond 2^31 elements (and 2^32 bytes) of the first."""
+    import torch
+    n, stride = 5, 600_000_000
+    flat = torch.empty((n - 1) * stride + 9_000, dtype=torch.bfloat16, device="cuda")
+    for V in (1000, 9_000):
+        d = flat.as_strided((n, V), (stride, 1))
+        x = torch.from_numpy(np.random.default_rng(0).normal(0, 2, (n, V))).to(torch.bfloat16)
+        d.copy_(x)
+        u = np.random.default_rng(1).random(n)
+        _check(T.tree_ens_sample(d, _dev(u), top_p=_f32(0.9)), O.sample(x.double().numpy(), u, top_p=_f32(0.9)), V, "far rows")
+
+
+@pytest.mark.parametrize("n,V", [(3, 60_001), (40, 500)])
+def test_captured_into_a_graph(T, n, V):
+    import torch
+    d, _, _ = _logits("f32", n, V)
+    u = torch.rand(n, dtype=torch.float64, device="cuda")
+    out = [torch.empty(n, dtype=torch.int64, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")]
+    top_p = torch.full((n,), 0.9, device="cuda")
+
+    def step():
+        T.tree_ens_sample(d, u, top_p=top_p, tokens=out[0], logp=out[1], log_kept=out[2])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        g = torch.Generator().manual_seed(k)
+        d.copy_(torch.randn(d.shape, generator=g) * 3)
+        u.copy_(torch.rand(n, generator=g, dtype=torch.float64))
+        top_p.copy_(torch.rand(n, generator=g))
+        step()
+        want = [o.clone() for o in out]
+        for o in out:
+            o.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), k
+
+
+def test_logp_is_that_of_token_logp(T):
+    """Both give log softmax(scale * row)[token]; token_logp's error is that of single-precision sums of the row."""
+    import torch
+    for dtype, n, V in (("bf16", 200, 32_000), ("f32", 50, 700)):
+        d, _, u = _logits(dtype, n, V, seed=9)
+        tokens, logp, _ = T.tree_ens_sample(d, _dev(u), scale=1.25, top_k=20)
+        want, _, stats = T.tree_ens_token_logp(d, tokens, scale=1.25)
+        z = 4 * (1 + want.abs() + stats[:, 1].abs()) + V / 256 + 72
+        assert torch.all((logp - want).abs() <= U * (z + want.abs()))
+    d[0] = -float("inf")
+    tokens, _, _ = T.tree_ens_sample(d, _dev(u))
+    assert tokens[0] == -1 and T.tree_ens_token_logp(d, tokens)[0][0] == 0  # a row that does not count
+
+
+def test_only_rows_of_the_call_are_written(T):
+    import torch
+    d, _, u = _logits("bf16", 5, 6_001)
+    wide = [torch.full((9,), -7, dtype=t, device="cuda") for t in (torch.int64, torch.float32, torch.float32)]
+    T.tree_ens_sample(d, _dev(u), top_p=0.9, tokens=wide[0][2:7], logp=wide[1][2:7], log_kept=wide[2][2:7])
+    for w in wide:
+        assert (w[:2] == -7).all() and (w[7:] == -7).all() and (w[2:7] != -7).all()
+
+
+def test_argument_errors(T):
+    import torch
+    d, _, u = _logits("f32", 3, 8)
+    u = _dev(u)
+    for bad in (u.float(), u[:2], u.repeat(2)[::2]):
+        with pytest.raises(TypeError, match="uniform"):
+            T.tree_ens_sample(d, bad)
+    with pytest.raises(TypeError, match="contiguous rows"):
+        T.tree_ens_sample(d.t(), _dev(np.zeros(8)))
+    with pytest.raises(TypeError, match="logits"):
+        T.tree_ens_sample(d.double(), u)
+    with pytest.raises(TypeError, match="top_k"):
+        T.tree_ens_sample(d, u, top_k=torch.ones(3, device="cuda"))
+    with pytest.raises(TypeError, match="scale"):
+        T.tree_ens_sample(d, u, scale=torch.ones(2, device="cuda"))
+    with pytest.raises(TypeError, match="top_p"):
+        T.tree_ens_sample(d, u, top_p=torch.ones(3))
+    with pytest.raises(TypeError, match="tokens"):
+        T.tree_ens_sample(d, u, tokens=torch.empty(3, dtype=torch.int32, device="cuda"))
+    with pytest.raises(TypeError, match="logp"):
+        T.tree_ens_sample(d, u, logp=torch.empty(2, device="cuda"))
+    for bad in (dict(scale=0.0), dict(top_k=-1), dict(top_p=0.0), dict(min_p=2.0)):
+        with pytest.raises(T.TreeEnsError) as ei:
+            T.tree_ens_sample(d, u, **bad)
+        assert ei.value.code == T.TREE_ENS_E_ARG
+    with pytest.raises(T.TreeEnsError):
+        T.tree_ens_sample(d[:1].expand(3, 8), u)  # rows that share their logits
+    tokens, logp, log_kept = T.tree_ens_sample(torch.empty(0, 8, device="cuda"), u[:0])
+    assert tokens.shape == logp.shape == log_kept.shape == (0,)
+    assert (T.tree_ens_sample(d, u, top_k=2**40)[0] == T.tree_ens_sample(d, u)[0]).all()
