@@ -51,16 +51,47 @@ struct Params {
 
 constexpr uint64_t kOne = uint64_t(1) << 53;
 
+// The natural logarithm of a number of at least 2^-1000, to about 2^-45: of the exponent, and 2 atanh of (m - 1) / (m + 1) for
+// the rest m, within sqrt(2) of 1, by its series. A few dozen instructions where the library's has hundreds, which a
+// workgroup that comes by once has to fetch first.
+__device__ __forceinline__ double log_of(double x) {
+    const int high = __double2hiint(x), n = (high - 0x3fe6a09e) >> 20; // 0x3fe6a09e...: sqrt(1/2)
+    const double m = __hiloint2double(high - (n << 20), __double2loint(x));
+    const double q = (m - 1.0) / (m + 1.0), y = q * q;
+    double p = 1.0 / 15;
+    p = fma(p, y, 1.0 / 13);
+    p = fma(p, y, 1.0 / 11);
+    p = fma(p, y, 1.0 / 9);
+    p = fma(p, y, 1.0 / 7);
+    p = fma(p, y, 1.0 / 5);
+    p = fma(p, y, 1.0 / 3);
+    return fma(double(n), 0.6931471805599453, 2.0 * fma(p * y, q, q));
+}
+
+__device__ __forceinline__ double scale_of(const Args &a, int64_t row) {
+    const float scale = a.row_scale ? a.row_scale[row] : a.scale;
+    return scale > 0.0f && scale < INFINITY ? double(scale) : 0.0;
+}
+__device__ __forceinline__ int top_k_of(const Args &a, int64_t row) {
+    const int k = a.row_top_k ? a.row_top_k[row] : a.top_k;
+    return k > 0 && k < a.V ? k : a.V;
+}
+__device__ __forceinline__ float min_p_of(const Args &a, int64_t row) { return a.row_min_p ? a.row_min_p[row] : a.min_p; }
+
+// Whether the weights of a whole row are asked for: for its log-probabilities, or because nothing but top_p, or nothing
+// at all, cuts it off.
+__device__ __forceinline__ bool needs_mass(const Args &a, int64_t row) {
+    return a.logp || a.log_kept || (top_k_of(a, row) == a.V && !(min_p_of(a, row) > 0.0f));
+}
+
 __device__ __forceinline__ Params params_of(const Args &a, int64_t row) {
     Params p;
-    const float scale = a.row_scale ? a.row_scale[row] : a.scale;
-    p.scale = scale > 0.0f && scale < INFINITY ? double(scale) : 0.0;
-    const int k = a.row_top_k ? a.row_top_k[row] : a.top_k;
-    p.top_k = k > 0 && k < a.V ? k : a.V;
+    p.scale = scale_of(a, row);
+    p.top_k = top_k_of(a, row);
     const float q = a.row_top_p ? a.row_top_p[row] : a.top_p;
     p.fraction = q < 1.0f ? uint64_t(double(fmaxf(q, 0.0f)) * 0x1p53) : kOne;
-    const float m = a.row_min_p ? a.row_min_p[row] : a.min_p;
-    p.least = m > 0.0f ? log(double(fminf(m, 1.0f))) : -INFINITY;
+    const float m = min_p_of(a, row);
+    p.least = m > 0.0f ? log_of(double(fminf(m, 1.0f))) : -INFINITY;
     const double u = a.uniform[row];
     p.at = u > 0.0 ? min(uint64_t(fmin(u, 1.0) * 0x1p53), kOne - 1) : 0;
     return p;
@@ -74,12 +105,12 @@ __device__ __forceinline__ uint64_t share_up(uint64_t sum, uint64_t fraction) {
     return share_down(sum, fraction) + ((sum * fraction & (kOne - 1)) != 0);
 }
 
-// 2^(d c) in whole numbers of 2^-shift for -128 <= d c <= 0: the exponent taken apart into a whole number n and a rest
-// r within a half, and 2^r by the polynomial of degree 8 whose largest relative error there, 1.1e-12, is the smallest
-// with p(0) = 1 (found by exchange). Double-precision multiply-adds run at the rate of single ones on this card.
+// 2^(d c + shift) for -1000 <= d c <= 0: the exponent taken apart into a whole number and a rest r within a half, and 2^r by
+// the polynomial of degree 8 whose largest relative error there, 1.1e-12, is the smallest with p(0) = 1 (found by exchange).
+// Double-precision multiply-adds run at the rate of single ones on this card.
 __device__ __forceinline__ double power_of(double d, double c, int shift) {
-    constexpr double kRound = 0x1.8p52; // adding it leaves the whole number in the low bits
-    const double t = fma(d, c, kRound), r = fma(d, c, kRound - t);
+    const double round = 0x1.8p52 + double(shift); // adding it leaves the whole number in the low bits
+    const double t = fma(d, c, round), r = fma(d, c, round - t);
     double p = 0x1.663487d8abc81p-20;
     p = fma(p, r, 0x1.00ee071c7c030p-16);
     p = fma(p, r, 0x1.4306c1165a375p-13);
@@ -89,14 +120,13 @@ __device__ __forceinline__ double power_of(double d, double c, int shift) {
     p = fma(p, r, 0x1.ebfbdff7c5a79p-3);
     p = fma(p, r, 0x1.62e42fef7a78bp-1);
     p = fma(p, r, 1.0);
-    return __hiloint2double(__double2hiint(p) + ((__double2loint(t) + shift) << 20), __double2loint(p));
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
 
-// The number that adding 2^52 leaves in the low bits, rounded to nearest, for 0 <= v < 2^52.
+// The whole number nearest to 0 <= v < 2^52, which adding 2^52 leaves in the low bits.
 __device__ __forceinline__ uint64_t whole_of(double v) {
     return uint64_t(__double_as_longlong(v + 0x1p52)) & ((uint64_t(1) << 52) - 1);
 }
-__device__ __forceinline__ uint64_t weight_of(double d, double c, int shift) { return whole_of(power_of(d, c, shift)); }
 
 // Whole numbers in the order of the floats; -0 counts as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -127,24 +157,49 @@ __device__ __forceinline__ uint32_t floor_key(double m, double scale, double lea
     return top;
 }
 
-template <typename V> __device__ __forceinline__ V wave_sum(V v) {
-    for (int off = kWave / 2; off; off >>= 1)
-        v += __shfl_xor(v, off);
-    return v;
-}
-
-// Sums over the lanes up to and with this one.
-template <typename V> __device__ __forceinline__ V wave_scan(V v) {
-    const int lane = threadIdx.x % kWave;
-    for (int off = 1; off < kWave; off *= 2) {
-        const V o = __shfl_up(v, off);
-        v += lane >= off ? o : V(0);
-    }
-    return v;
-}
-
 // The larger one; NaN if either is.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A value of another lane by kCtrl, or 0 (the lane's own with kOwn) where there is none or kRows leaves the row of 16 out.
+template <int kCtrl, int kRows, bool kOwn = false> __device__ __forceinline__ unsigned moved(unsigned v) {
+    return unsigned(__builtin_amdgcn_update_dpp(kOwn ? int(v) : 0, int(v), kCtrl, kRows, 0xf, false));
+}
+template <int kCtrl, int kRows> __device__ __forceinline__ uint64_t moved(uint64_t v) {
+    return uint64_t(moved<kCtrl, kRows>(unsigned(v >> 32))) << 32 | moved<kCtrl, kRows>(unsigned(v));
+}
+template <int kCtrl, int kRows> __device__ __forceinline__ double moved(double v) {
+    return __longlong_as_double(moved<kCtrl, kRows>(uint64_t(__double_as_longlong(v))));
+}
+
+// Sums over the lanes up to and with this one: within rows of 16, then the rows' ends are added to the rows behind them.
+template <typename V> __device__ __forceinline__ V wave_scan(V v) {
+    v += moved<0x111, 0xf>(v); // from 1, 2, 4 and 8 lanes before
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v); // the last lane of a row, to the second and fourth
+    v += moved<0x143, 0xc>(v); // that of the first half, to the second
+    return v;
+}
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
+    return uint64_t(unsigned(__builtin_amdgcn_readlane(int(v >> 32), kWave - 1))) << 32 |
+           unsigned(__builtin_amdgcn_readlane(int(unsigned(v)), kWave - 1));
+}
+__device__ __forceinline__ double last_lane(double v) { return __longlong_as_double(last_lane(uint64_t(__double_as_longlong(v)))); }
+template <typename V> __device__ __forceinline__ V wave_sum(V v) { return last_lane(wave_scan(v)); }
+
+template <int kCtrl, int kRows = 0xf> __device__ __forceinline__ float moved_larger(float v) {
+    return larger(v, __uint_as_float(moved<kCtrl, kRows, true>(__float_as_uint(v))));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = moved_larger<0x111>(v);
+    v = moved_larger<0x112>(v);
+    v = moved_larger<0x114>(v);
+    v = moved_larger<0x118>(v);
+    v = moved_larger<0x142, 0xa>(v);
+    v = moved_larger<0x143, 0xc>(v);
+    return __uint_as_float(unsigned(__builtin_amdgcn_readlane(int(__float_as_uint(v)), kWave - 1)));
+}
 
 __device__ __forceinline__ void store_row(const Args &a, int64_t row, int64_t token, float logp, float log_kept) {
     a.tokens[row] = token;
@@ -158,31 +213,41 @@ __device__ __forceinline__ void store_row(const Args &a, int64_t row, int64_t to
 struct Row {
     double m, scale, c, far;
     int shift;
-    uint32_t floor; // keys below it are not kept (min_p)
-    __device__ __forceinline__ Row(float top, const Params &p, int shift_)
-        : m(double(top)), scale(p.scale), c(p.scale * kLog2e), far(-64.0 / p.scale), shift(shift_), floor(0) {}
-    // masked logits are taken at `far`, where the weight is 0
-    __device__ __forceinline__ uint64_t weight(float x) const { return weight_of(fmax(double(x) - m, far), c, shift); }
+    __device__ __forceinline__ Row(float top, double scale_, int shift_)
+        : m(double(top)), scale(scale_), c(scale_ * kLog2e), far(-64.0 * __builtin_amdgcn_rcp(scale_)), shift(shift_) {}
+    // The weight in units, not rounded. Masked logits are taken at `far`, where it is less than half of one.
+    __device__ __forceinline__ double power(float x) const { return power_of(fmax(double(x) - m, far), c, shift); }
+    __device__ __forceinline__ uint64_t weight(float x) const { return whole_of(power(x)); }
     __device__ __forceinline__ uint64_t key_weight(uint32_t k) const { return weight(float_of(k)); }
 };
 
 // The token's log-probability and the logarithm of the kept share, which is 0 exactly where everything is kept.
 __device__ __forceinline__ void finish_row(const Args &a, int64_t row, const Row &r, int token, float x, uint64_t kept, uint64_t total) {
-    if (!a.logp && !a.log_kept)
-        return store_row(a, row, token, 0.0f, 0.0f);
-    const double logp = (double(x) - r.m) * r.scale - log(ldexp(double(total), -r.shift));
-    const double dropped = total > kept ? double(total - kept) / double(total) : 0.0;
-    store_row(a, row, token, float(logp), float(log1p(-dropped)));
+    a.tokens[row] = token;
+    if (a.logp)
+        a.logp[row] = float((double(x) - r.m) * r.scale - log_of(double(total)) + r.shift * 0.6931471805599453);
+    if (a.log_kept) {
+        const double dropped = total > kept ? double(total - kept) / double(total) : 0.0;
+        a.log_kept[row] = float(dropped < 0x1p-16 ? -fma(dropped, fma(dropped, 1.0 / 3, 0.5) * dropped, dropped) : log_of(1.0 - dropped));
+    }
 }
 __device__ __forceinline__ void finish_without(const Args &a, int64_t row, bool bad) {
     if (threadIdx.x == 0)
         store_row(a, row, -1, bad ? NAN : -INFINITY, bad ? NAN : 0.0f);
 }
 
-// A place in the order of the logits: keys above `key` are kept, and the first `spare` ones of it.
-struct Place {
-    uint32_t key;
-    uint64_t spare;
+// Entries are in the order of the logits: a larger one comes first. A token is kept if its entry is at least that of the
+// last one kept.
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, int index) { return uint64_t(key) << 32 | uint32_t(~index); }
+__device__ __forceinline__ int index_of(uint64_t entry) { return int(~uint32_t(entry)); }
+__device__ __forceinline__ uint32_t key_in(uint64_t entry) { return uint32_t(entry >> 32); }
+
+// The logit and the index of the last one kept; entry 0 keeps all.
+struct Last {
+    float value;
+    int index;
+    __device__ __forceinline__ explicit Last(uint64_t entry) : value(entry ? float_of(key_in(entry)) : -INFINITY), index(index_of(entry)) {}
+    __device__ __forceinline__ bool keeps(float v, int i) const { return v > value || (v == value && unsigned(i) <= unsigned(index)); }
 };
 
 constexpr int kBins = 256;
@@ -198,7 +263,7 @@ template <int kT> struct Block {
     };
 
     // The sum over all threads.
-    static __device__ uint64_t sum(uint64_t v, Shared &s) {
+    static __device__ __forceinline__ uint64_t sum(uint64_t v, Shared &s) {
         v = wave_sum(v);
         if constexpr (kWaves == 1)
             return v;
@@ -213,10 +278,10 @@ template <int kT> struct Block {
     }
 
     // The sum over the threads before this one; `total` receives that over all.
-    static __device__ uint64_t before(uint64_t v, uint64_t &total, Shared &s) {
+    static __device__ __forceinline__ uint64_t before(uint64_t v, uint64_t &total, Shared &s) {
         const uint64_t with = wave_scan(v);
         if constexpr (kWaves == 1) {
-            total = __shfl(with, kWave - 1);
+            total = last_lane(with);
             return with - v;
         }
         __syncthreads();
@@ -232,9 +297,8 @@ template <int kT> struct Block {
         return sum;
     }
 
-    static __device__ float max(float v, Shared &s) {
-        for (int off = kWave / 2; off; off >>= 1)
-            v = larger(v, __shfl_xor(v, off));
+    static __device__ __forceinline__ float max(float v, Shared &s) {
+        v = wave_max(v);
         if constexpr (kWaves == 1)
             return v;
         __syncthreads();
@@ -246,22 +310,22 @@ template <int kT> struct Block {
         return v;
     }
 
-    // Where the count (kByMass: the weights) of the keys from the top reaches `target`, which it does; `above` receives
-    // the weights of the keys above the place's. Eight bits of the keys at a time, from histograms.
+    // The entry at which the count (kByMass: the weights) of the logits from the top down to `least` reaches `target`, which it
+    // does; `inside` receives the weights down to it. Eight bits of the keys at a time, from histograms, and then its index.
     template <bool kByMass, typename T>
-    static __device__ Place place_of(const T *x, int V, const Row &r, uint64_t target, uint64_t &above, uint64_t *mass, uint32_t *count,
-                                     Shared &s) {
-        Place p{0, target};
-        above = 0;
+    static __device__ uint64_t place_of(const T *x, int V, const Row &r, float least, uint64_t target, uint64_t &inside, uint64_t *mass,
+                                        uint32_t *count, Shared &s) {
+        uint32_t key = 0;
+        uint64_t spare = target, above = 0;
         for (int bit = 24; bit >= 0; bit -= 8) {
             __syncthreads();
             for (int i = threadIdx.x; i < kBins; i += kT)
                 mass[i] = count[i] = 0;
             __syncthreads();
-            for (int i = threadIdx.x; i < V; i += kT) {
+            for (int64_t i = threadIdx.x; i < V; i += kT) {
                 const float v = float(x[i]);
                 const uint32_t k = key_of(v);
-                if (k < r.floor || (bit < 24 && (k ^ p.key) >> (bit + 8)))
+                if (!(v >= least) || (bit < 24 && (k ^ key) >> (bit + 8)))
                     continue;
                 const int bin = k >> bit & (kBins - 1);
                 atomicAdd(&count[bin], 1u);
@@ -269,7 +333,7 @@ template <int kT> struct Block {
             }
             __syncthreads();
             if (threadIdx.x == 0) {
-                uint64_t left = p.spare, over = 0;
+                uint64_t left = spare, over = 0;
                 int d = kBins - 1;
                 for (;; --d) {
                     const uint64_t here = kByMass ? mass[d] : count[d];
@@ -283,25 +347,40 @@ template <int kT> struct Block {
                 s.part[0] = over;
             }
             __syncthreads();
-            p.key |= s.digit << bit;
-            p.spare = s.left;
+            key |= s.digit << bit;
+            spare = s.left;
             above += s.part[0];
         }
-        if (kByMass) { // the weight that is left, in tokens of this one's
-            const uint64_t w = r.key_weight(p.key);
-            p.spare = w ? (p.spare + w - 1) / w : 1;
-        }
+        const uint64_t level = r.key_weight(key);
+        if (kByMass) // the weight that is left, in tokens of this one's
+            spare = level ? (spare + level - 1) / level : 1;
+        inside = above + spare * level;
+        // the index of the last of them: threads take stretches
+        const int each = (V - 1) / kT + 1;
+        const int64_t from = std::min(int64_t(threadIdx.x) * each, int64_t(V)), to = std::min(from + each, int64_t(V));
+        const float value = float_of(key);
+        uint64_t same = 0, unused;
+        for (int64_t i = from; i < to; ++i)
+            same += float(x[i]) == value;
+        uint64_t rank = before(same, unused, s);
+        if (rank < spare && spare <= rank + same)
+            for (int64_t i = from; i < to; ++i) {
+                rank += float(x[i]) == value;
+                if (rank == spare) {
+                    s.digit = uint32_t(i);
+                    break;
+                }
+            }
         __syncthreads();
-        return p;
+        const uint64_t entry = entry_of(key, int(s.digit));
+        __syncthreads();
+        return entry;
     }
 };
 
 // ------------------------------------------------------------------------------------------------
 // sorting in LDS
 // ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint64_t entry_of(uint32_t key, int index) { return uint64_t(key) << 32 | uint32_t(~index); }
-__device__ __forceinline__ int index_of(uint64_t entry) { return int(~uint32_t(entry)); }
-
 // Waits for the other threads of what shares stretches of `stride` pairs: a wave's LDS accesses are in order.
 template <int kT> __device__ __forceinline__ void sort_wait(int stride) {
     if (kT > kWave && stride > kWave)
@@ -336,17 +415,14 @@ __device__ __forceinline__ int power_of_two(int n) { return n <= 2 ? 2 : 1 << (3
 // ------------------------------------------------------------------------------------------------
 // short rows
 // ------------------------------------------------------------------------------------------------
-constexpr int kOwn = 8; // logits of a thread
-
-template <typename T, int kT>
-__global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
+template <typename T, int kT, int kOwn>
+__global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn == 4 ? 4 : 3))) small_kernel(const T *logits, Args a) {
     using B = Block<kT>;
     __shared__ typename B::Shared s;
     __shared__ uint64_t list[kOwn * kT];
     __shared__ uint64_t last;
     const int tid = threadIdx.x, each = (a.V + kT - 1) / kT, from = tid * each;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const Params p = params_of(a, row);
         const T *x = logits + row * a.stride;
         float v[kOwn], m = -INFINITY;
 #pragma unroll
@@ -354,13 +430,14 @@ __global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
             v[i] = i < each && from + i < a.V ? float(x[from + i]) : -INFINITY;
             m = larger(m, v[i]);
         }
+        const Params p = params_of(a, row);
         m = B::max(m, s);
         if (p.scale == 0.0 || !(m < INFINITY) || m == -INFINITY) {
             finish_without(a, row, p.scale == 0.0 || m != -INFINITY);
             continue;
         }
-        Row r(m, p, a.shift);
-        r.floor = floor_key(r.m, p.scale, p.least, key_of(m));
+        const Row r(m, p.scale, a.shift);
+        const uint32_t floor = floor_key(r.m, p.scale, p.least, key_of(m));
         uint64_t w[kOwn], total = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
@@ -368,20 +445,19 @@ __global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
             total += w[i];
         }
         total = B::sum(total, s);
-        uint64_t lowest = entry_of(r.floor, -1); // entries from here on are kept
+        uint64_t lowest = entry_of(floor, -1); // entries from here on are kept
         if (p.top_k < a.V || p.fraction < kOne) {
             const int n = power_of_two(a.V);
             __syncthreads();
             if (tid == 0)
                 last = 0;
-            for (int i = tid; i < n; i += kT)
-                if (i >= a.V)
-                    list[i] = 0;
+            for (int i = a.V + tid; i < n; i += kT)
+                list[i] = 0;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i)
                 if (i < each && from + i < a.V) {
                     const uint32_t k = key_of(v[i]);
-                    list[from + i] = k >= r.floor ? entry_of(k, from + i) : 0;
+                    list[from + i] = k >= floor ? entry_of(k, from + i) : 0;
                 }
             sort_down<kT>(list, n);
             const int share = std::max(n / kT, 1);
@@ -390,7 +466,7 @@ __global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
             for (int i = 0; i < kOwn; ++i) {
                 const int at = tid * share + i;
                 const uint64_t e = i < share && at < std::min(n, p.top_k) ? list[at] : 0;
-                sorted[i] = e ? r.key_weight(uint32_t(e >> 32)) : 0;
+                sorted[i] = e ? r.key_weight(key_in(e)) : 0;
                 mine += sorted[i];
             }
             uint64_t all;
@@ -419,13 +495,19 @@ __global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
         uint64_t kept;
         uint64_t sum = B::before(mine, kept, s);
         const uint64_t target = share_down(kept, p.at);
+        int token = -1;
+        float at = 0.0f;
         if (sum <= target && target < sum + mine)
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
-                if (sum <= target && target < sum + w[i])
-                    finish_row(a, row, r, from + i, v[i], kept, total);
+                if (sum <= target && target < sum + w[i]) {
+                    token = from + i;
+                    at = v[i];
+                }
                 sum += w[i];
             }
+        if (token >= 0)
+            finish_row(a, row, r, token, at, kept, total);
     }
 }
 
@@ -433,7 +515,7 @@ __global__ void __launch_bounds__(kT) small_kernel(const T *logits, Args a) {
 // the digest of a row
 // ------------------------------------------------------------------------------------------------
 constexpr int kPart = 2048, kSeg = 128, kSegs = kPart / kSeg;
-constexpr int kMostParts = (1 << 19) / kPart; // longer rows are read again and again by wide_row
+constexpr int kMostParts = (1 << 19) / kPart; // longer rows go to long_kernel
 
 // 16 bytes of logits. A row may start anywhere, so what it is read through claims no alignment.
 template <typename T> struct Vec {
@@ -442,90 +524,106 @@ template <typename T> struct Vec {
     typedef type unaligned __attribute__((aligned(sizeof(T))));
 };
 
-// A wave reads a part in kLoads loads of 64 vectors; the 16 lanes of a quarter hold a segment in 16 / kSegs * kLoads of
-// them, which is one load of 2-byte logits and two of 4-byte ones.
+// Up to N logits from p on, -inf beyond the first `len`.
+template <typename T> __device__ __forceinline__ typename Vec<T>::type read_vec(const T *p, int len) {
+    if (len >= Vec<T>::N)
+        return *reinterpret_cast<const typename Vec<T>::unaligned *>(p);
+    typename Vec<T>::type q(T(-INFINITY));
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N; ++i)
+        if (i < len)
+            q[i] = p[i];
+    return q;
+}
+
+// A wave reads a part in kLoads loads of 64 vectors; the 16 lanes of a quarter hold a segment in kSame of them: one of
+// 2-byte logits, two of 4-byte ones.
 template <typename T> struct Part {
     static constexpr int N = Vec<T>::N, kLoads = kPart / kWave / N, kSame = kLoads / 4;
     // the lane's first element of a load
     static __device__ __forceinline__ int at(int load, int lane) { return (load * kWave + lane) * N; }
-    static __device__ __forceinline__ void read(const T *x, int len, int lane, float (&v)[kLoads * N]) {
-        typename Vec<T>::type q[kLoads];
+    static __device__ __forceinline__ void read(const T *x, int len, int lane, typename Vec<T>::type (&q)[kLoads]) {
         if (len >= kPart) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j)
                 q[j] = *reinterpret_cast<const typename Vec<T>::unaligned *>(x + at(j, lane));
         } else {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                q[j] = typename Vec<T>::type(T(-INFINITY));
-                if (at(j, lane) + N <= len)
-                    q[j] = *reinterpret_cast<const typename Vec<T>::unaligned *>(x + at(j, lane));
-                else
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (at(j, lane) + i < len)
-                            q[j][i] = x[at(j, lane) + i];
-            }
+            for (int j = 0; j < kLoads; ++j)
+                q[j] = read_vec(x + at(j, lane), len - at(j, lane));
         }
-#pragma unroll
-        for (int k = 0; k < kLoads * N; ++k)
-            v[k] = float(q[k / N][k % N]);
     }
 };
 
+// A row that pick_kernel leaves to the two kernels behind it.
+struct WideRow {
+    int64_t row;
+    float top, least;
+    uint64_t total;
+    uint64_t last;  // the entry of the last kept token, where `bin` is kFine
+    uint64_t left;  // otherwise it is in this bin, where the count (by_mass: the weights) reaches this
+    int bin, members;
+    bool by_mass;
+    unsigned arrived[2], listed;
+};
+
+// What the kernels leave for the next ones.
 struct Digest {
-    uint64_t *mass; // [n][parts]: weights relative to the part's own largest logit
-    float *top;     // [n][parts]
-    float *seg;     // [n][parts][kSegs]
+    double *mass;      // [n][parts]: weights relative to the part's own largest logit, in units
+    float *top;        // [n][parts]
+    float *seg;        // [n][parts][kSegs]
+    unsigned *wide;    // the number of rows left
+    WideRow *rows;     // [n]
+    // where several workgroups share a row:
+    uint64_t *bins;    // [kSlices][kFine]
+    unsigned *members; // [kSlices][kFine]
+    uint64_t *kept;    // [kSlices / 2][kMostParts]: weights above the bin
+    uint64_t *list;    // [kSlices / 2][kList]: the bin's entries
     int parts;
 };
 
-// Whether the weights of a whole row are asked for: for its log-probabilities, or because nothing but top_p, or nothing
-// at all, cuts it off.
-__device__ __forceinline__ bool needs_mass(const Args &a, const Params &p) {
-    return a.logp || a.log_kept || (p.top_k == a.V && p.least == -INFINITY);
-}
-
-template <int kCtrl> __device__ __forceinline__ float row_larger(float v) {
-    return larger(v, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), kCtrl, 0xf, 0xf, true)));
-}
-
+// A wave takes a part of a row.
 template <typename T>
 __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Digest g) {
     using P = Part<T>;
     constexpr int kN = P::kLoads * P::N;
     const int lane = threadIdx.x % kWave;
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *g.wide = 0;
     const int64_t items = a.n * g.parts;
     for (int64_t item = blockIdx.x * int64_t(4) + threadIdx.x / kWave; item < items; item += gridDim.x * int64_t(4)) {
         const int64_t row = item / g.parts;
         const int part = int(item - row * g.parts);
-        const Params p = params_of(a, row);
-        float v[kN];
-        P::read(logits + row * a.stride + part * kPart, a.V - part * kPart, lane, v);
-        float m = -INFINITY, mine = -INFINITY;
+        typename Vec<T>::type q[P::kLoads];
+        P::read(logits + row * a.stride + part * kPart, a.V - part * kPart, lane, q);
+        float v[kN], m = -INFINITY, mine = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kN; ++k)
+            v[k] = float(q[k / P::N][k % P::N]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float top = -INFINITY;
+            constexpr int kSome = P::kSame * P::N;
+            float top = v[i * kSome];
 #pragma unroll
-            for (int k = 0; k < P::kSame * P::N; ++k)
-                top = larger(top, v[i * P::kSame * P::N + k]);
-            top = row_larger<0x128>(top); // rotations by 8, 4, 2 and 1 among 16 lanes
-            top = row_larger<0x124>(top);
-            top = row_larger<0x122>(top);
-            top = row_larger<0x121>(top);
+            for (int k = 1; k < kSome; ++k)
+                top = larger(top, v[i * kSome + k]);
+            top = moved_larger<0x128>(top); // rotations by 8, 4, 2 and 1 among 16 lanes
+            top = moved_larger<0x124>(top);
+            top = moved_larger<0x122>(top);
+            top = moved_larger<0x121>(top);
             mine = lane % 16 == i ? top : mine;
             m = larger(m, top);
         }
-        m = larger(m, __shfl_xor(m, 16));
-        m = larger(m, __shfl_xor(m, 32));
+        m = wave_max(m);
         if (lane % 16 < 4)
             g.seg[item * kSegs + lane % 16 * 4 + lane / 16] = mine;
-        uint64_t mass = 0;
-        if (needs_mass(a, p) && p.scale != 0.0 && m < INFINITY && m > -INFINITY) {
-            const Row r(m, p, a.shift);
+        double mass = 0.0;
+        const double scale = scale_of(a, row);
+        if (needs_mass(a, row) && scale != 0.0 && m < INFINITY && m > -INFINITY) {
+            const Row r(m, scale, a.shift);
 #pragma unroll
             for (int k = 0; k < kN; ++k)
-                mass += r.weight(v[k]);
+                mass += r.power(v[k]);
             mass = wave_sum(mass);
         }
         if (lane == 0) {
@@ -538,264 +636,61 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kPick = 512;
 constexpr int kList = 2048; // candidates
-constexpr int kFine = 1024; // bins of wide_row
-using PickBlock = Block<kPick>;
+constexpr int kFine = 1024; // bins
 
-struct PickShared {
-    uint64_t list[kList];
-    union {
-        struct {
-            uint64_t mass[kFine];
-            uint32_t count[kFine];
-        };
-        struct {
-            uint64_t part_mass[kMostParts];
-            uint32_t part_ties[kMostParts];
-        };
-        uint16_t segs[kMostParts * kSegs];
-    };
-    PickBlock::Shared block;
-    uint64_t found_mass, found_left;
-    uint32_t found_key;
-    int found, n;
-    bool spoiled;
-    int ge[2][PickBlock::kWaves];
-};
-
-// The token among the logits of one part, at which the running sum of weights (relative to r.m) passes `target`. Keys above
-// the place's count, and the first `spare` of its own.
-template <typename T>
-__device__ void pick_in_part(const Args &a, int64_t row, const T *x, int part, const Row &weights, const Row &r, Place place,
-                             uint64_t target, uint64_t kept, uint64_t total, PickShared &s) {
-    constexpr int kEach = kPart / kPick;
+// The token among the logits of one part, as far into the sum of its kept weights there as `ask` is in `of`.
+template <typename T, int kT>
+__device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T *x, int part, const Row &own, const Row &r, Last last,
+                                             uint64_t ask, uint64_t of, uint64_t kept, uint64_t total, typename Block<kT>::Shared &s) {
+    constexpr int kEach = kPart / kT;
     const int from = part * kPart + threadIdx.x * kEach;
     float v[kEach];
-    uint64_t ties = 0, unused;
+    uint64_t w[kEach], mine = 0, all;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
+    for (int i = 0; i < kEach; ++i)
         v[i] = from + i < a.V ? float(x[from + i]) : -INFINITY;
-        ties += from + i < a.V && key_of(v[i]) == place.key;
-    }
-    uint64_t rank = PickBlock::before(ties, unused, s.block);
-    uint64_t w[kEach], mine = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        const uint32_t k = key_of(v[i]);
-        const bool tie = k == place.key;
-        w[i] = from + i < a.V && (k > place.key || (tie && rank < place.spare)) ? weights.weight(v[i]) : 0;
-        rank += tie;
+        w[i] = last.keeps(v[i], from + i) ? own.weight(v[i]) : 0;
         mine += w[i];
     }
-    uint64_t all;
-    uint64_t sum = PickBlock::before(mine, all, s.block);
+    uint64_t sum = Block<kT>::before(mine, all, s);
+    const uint64_t target = all == of ? ask : std::min(uint64_t(double(ask) / double(of) * double(all)), all - 1);
+    int token = -1;
+    float at = 0.0f;
     if (sum <= target && target < sum + mine)
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            if (sum <= target && target < sum + w[i])
-                finish_row(a, row, r, from + i, v[i], kept, total);
+            if (sum <= target && target < sum + w[i]) {
+                token = from + i;
+                at = v[i];
+            }
             sum += w[i];
         }
+    if (token >= 0)
+        finish_row(a, row, r, token, at, kept, total);
 }
 
-// The bin of a logit by its distance from the largest, which never decreases as logits do; kFine: its weight is 0. Halves,
-// because the distance itself may be no float.
-struct Bins {
-    float half, step;
-    __device__ __forceinline__ Bins(const Row &r)
-        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 31.5f), 3.402823466e38f)) {}
-    __device__ __forceinline__ int of(float x) const {
-        const float d = (half - x * 0.5f) * step;
-        return d < float(kFine) ? int(d) : kFine;
-    }
+constexpr int kPick = 256;
+using PickBlock = Block<kPick>;
+
+struct PickShared {
+    uint64_t list[kList], weights[kList];
+    uint16_t segs[kMostParts * kSegs];
+    unsigned count[kPick];
+    PickBlock::Shared block;
+    uint64_t found_mass, found_left;
+    float found_top;
+    int found, n;
+    int ge[2][PickBlock::kWaves];
 };
 
-// Where the count (kByMass: the weights) from the top reaches `target`, which it does within the bins; `above` receives the
-// weights above the place's key.
-template <bool kByMass, typename T>
-__device__ Place place_in_bins(const Args &a, const T *x, const Row &r, const Bins &bins, uint64_t target, uint64_t &above, PickShared &s) {
-    constexpr int kEach = kFine / kPick;
-    uint64_t mine = 0, mine_mass = 0, all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int b = threadIdx.x * kEach + i;
-        mine += kByMass ? s.mass[b] : s.count[b];
-        mine_mass += s.mass[b];
-    }
-    uint64_t sum = PickBlock::before(mine, all, s.block);
-    uint64_t sum_mass = kByMass ? sum : PickBlock::before(mine_mass, all, s.block);
-    if (sum < target && target <= sum + mine)
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int b = threadIdx.x * kEach + i;
-            const uint64_t here = kByMass ? s.mass[b] : s.count[b];
-            if (sum < target && target <= sum + here) {
-                s.found = b;
-                s.found_left = target - sum;
-                s.found_mass = sum_mass;
-            }
-            sum += here;
-            sum_mass += s.mass[b];
-        }
-    if (threadIdx.x == 0)
-        s.n = 0;
-    __syncthreads();
-    const int bin = s.found;
-    const uint64_t left = s.found_left;
-    const uint32_t members = s.count[bin];
-    above = s.found_mass;
-    if (members > kList) { // a great many near equals: place_of overwrites the bins
-        __syncthreads();
-        s.spoiled = true;
-        return PickBlock::place_of<kByMass>(x, a.V, r, target, above, s.mass, s.count, s.block);
-    }
-    for (int i = threadIdx.x; i < a.V; i += kPick) {
-        const float v = float(x[i]);
-        const uint32_t k = key_of(v);
-        if (k >= r.floor && bins.of(v) == bin)
-            s.list[atomicAdd(&s.n, 1)] = entry_of(k, i);
-    }
-    __syncthreads();
-    const int n = power_of_two(int(members));
-    for (int i = int(members) + threadIdx.x; i < n; i += kPick)
-        s.list[i] = 0;
-    sort_down<kPick>(s.list, n);
-    // the place is that of an entry: its key, and how many entries of this key there are down to it
-    constexpr int kSome = kList / kPick;
-    const int share = std::max(n / kPick, 1);
-    uint64_t w[kSome];
-    mine = 0;
-    mine_mass = 0;
-#pragma unroll
-    for (int i = 0; i < kSome; ++i) {
-        const int at = threadIdx.x * share + i;
-        const bool in = i < share && at < int(members);
-        w[i] = in ? r.key_weight(uint32_t(s.list[at] >> 32)) : 0;
-        mine += kByMass ? w[i] : in;
-        mine_mass += w[i];
-    }
-    sum = PickBlock::before(mine, all, s.block);
-    sum_mass = kByMass ? sum : PickBlock::before(mine_mass, all, s.block);
-    if (sum < left && left <= sum + mine)
-#pragma unroll
-        for (int i = 0; i < kSome; ++i) {
-            const int at = threadIdx.x * share + i;
-            const uint64_t here = kByMass ? w[i] : uint64_t(i < share && at < int(members));
-            if (sum < left && left <= sum + here)
-                s.found = at;
-            sum += here;
-        }
-    __syncthreads();
-    const int at = s.found;
-    Place p{uint32_t(s.list[at] >> 32), 0};
-    // entries of the key before this one, and the weights before the first of them
-    uint64_t same = 0, over = 0;
-#pragma unroll
-    for (int i = 0; i < kSome; ++i) {
-        const int k = threadIdx.x * share + i;
-        if (i < share && k <= at) {
-            const bool tie = uint32_t(s.list[k] >> 32) == p.key;
-            same += tie;
-            over += tie ? 0 : w[i];
-        }
-    }
-    p.spare = PickBlock::sum(same, s.block);
-    above += PickBlock::sum(over, s.block);
-    __syncthreads();
-    return p;
-}
-
-// Counts and weights of the logits in each bin.
-template <typename T>
-__device__ void fill_bins(const Args &a, const T *x, const Row &r, const Bins &bins, PickShared &s) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kFine; i += kPick)
-        s.mass[i] = s.count[i] = 0;
-    s.spoiled = false;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.V; i += kPick) {
-        const float v = float(x[i]);
-        const int bin = bins.of(v);
-        if (bin < kFine && key_of(v) >= r.floor) {
-            atomicAdd(&s.count[bin], 1u);
-            atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[bin]), (unsigned long long)r.weight(v));
-        }
-    }
-    __syncthreads();
-}
-
-// A row whose kept tokens are too many for a list: weights and counts in bins of the distance from the largest logit, the
-// bin of the last kept token looked through, and the kept weights of every part of the row.
-template <typename T>
-__device__ void wide_row(const Args &a, int64_t row, const T *x, const Row &r, const Params &p, uint64_t total, PickShared &s) {
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    Place place{r.floor ? r.floor - 1 : 0, 0};
-    if (p.top_k < a.V || p.fraction < kOne) {
-        const Bins bins(r);
-        fill_bins(a, x, r, bins, s);
-        uint64_t there = 0, inside = 0, above;
-        for (int i = tid; i < kFine; i += kPick) {
-            there += s.count[i];
-            inside += s.mass[i];
-        }
-        there = PickBlock::sum(there, s.block);
-        inside = PickBlock::sum(inside, s.block);
-        if (uint64_t(p.top_k) < there) { // otherwise what it cuts off has no weight
-            place = place_in_bins<false>(a, x, r, bins, uint64_t(p.top_k), above, s);
-            inside = above + place.spare * r.key_weight(place.key);
-            if (p.fraction < kOne && s.spoiled)
-                fill_bins(a, x, r, bins, s);
-        }
-        if (p.fraction < kOne)
-            place = place_in_bins<true>(a, x, r, bins, std::max(share_up(inside, p.fraction), uint64_t(1)), above, s);
-    }
-    // the kept weights of the parts, and how many of the place's own key each has
-    __syncthreads();
-    const int parts = (a.V + kPart - 1) / kPart;
-    const uint64_t level = place.spare ? r.key_weight(place.key) : 0;
-    for (int q = wave; q < parts; q += PickBlock::kWaves) {
-        float v[kPart / kWave];
-        Part<T>::read(x + q * kPart, a.V - q * kPart, lane, v);
-        uint64_t mass = 0;
-        uint32_t ties = 0;
-#pragma unroll
-        for (int k = 0; k < kPart / kWave; ++k) {
-            const uint32_t key = key_of(v[k]);
-            mass += key > place.key ? r.weight(v[k]) : 0;
-            ties += key == place.key;
-        }
-        mass = wave_sum(mass);
-        ties = wave_sum(ties);
-        if (lane == 0) {
-            s.part_mass[q] = mass;
-            s.part_ties[q] = ties;
-        }
-    }
-    __syncthreads();
-    static_assert(kMostParts <= kPick, "a part a thread");
-    uint64_t all_ties, kept;
-    const uint64_t ties = tid < parts ? s.part_ties[tid] : 0;
-    const uint64_t ties_before = PickBlock::before(ties, all_ties, s.block);
-    const uint64_t spare = place.spare > ties_before ? place.spare - ties_before : 0;
-    const uint64_t mine = tid < parts ? s.part_mass[tid] + std::min(ties, spare) * level : 0;
-    const uint64_t sum = PickBlock::before(mine, kept, s.block);
-    const uint64_t target = share_down(kept, p.at);
-    if (sum <= target && target < sum + mine) {
-        s.found = tid;
-        s.found_left = target - sum;
-        s.found_mass = spare;
-    }
-    __syncthreads();
-    place.spare = s.found_mass;
-    pick_in_part(a, row, x, s.found, r, r, place, s.found_left, kept, total, s);
-}
-
 // The number of segments whose largest logit has a key of at least k.
-__device__ __forceinline__ int segments_from(const uint32_t (&keys)[kMostParts * kSegs / kPick], int segs, uint32_t k, int step, PickShared &s) {
+template <int kKeys> __device__ __forceinline__ int segments_from(const uint32_t (&keys)[kKeys], int segs, uint32_t k, int step, PickShared &s) {
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < kMostParts * kSegs / kPick; ++i)
+    for (int i = 0; i < kKeys; ++i)
         if (i * kPick < segs)
             n += __builtin_popcountll(__ballot(keys[i] >= k));
     if (threadIdx.x % kWave == 0)
@@ -810,129 +705,212 @@ __device__ __forceinline__ int segments_from(const uint32_t (&keys)[kMostParts *
 // The token from s.list[0, n), which holds every token down to some place of the order. `whole`: all that min_p and top_k
 // leave is among them; otherwise `total` is the weight of all that top_p is a share of. False where the list ends before the
 // last kept token does.
-template <typename T>
-__device__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total, PickShared &s) {
-    constexpr int kEach = kList / kPick;
-    const int padded = power_of_two(n), tid = threadIdx.x;
+//
+// Up to 256 entries, a thread each: every thread reads the others', in no order, and adds what comes before its own, which is
+// faster than sorting them (two times 36 dependent steps).
+__device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
+                                              PickShared &s) {
+    const int tid = threadIdx.x;
+    const uint64_t mine = tid < n ? s.list[tid] : 0;
+    const uint64_t w = tid < n ? r.key_weight(key_in(mine)) : 0;
+    if (tid < n)
+        s.weights[tid] = w;
     __syncthreads();
-    for (int i = n + tid; i < padded; i += kPick)
-        s.list[i] = 0;
-    sort_down<kPick>(s.list, padded);
-    int many = std::min(n, p.top_k), share = std::max(padded / kPick, 1);
-    uint64_t w[kEach], mine = 0, kept;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int at = tid * share + i;
-        w[i] = i < share && at < many ? r.key_weight(uint32_t(s.list[at] >> 32)) : 0;
-        mine += w[i];
-    }
-    uint64_t sum = PickBlock::before(mine, kept, s.block);
-    if (p.fraction < kOne) {
-        const uint64_t target = std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1));
-        if (kept < target)
-            return false;
-        if (sum < target && target <= sum + mine)
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                if (sum < target && target <= sum + w[i]) {
-                    s.found = tid * share + i + 1;
-                    s.found_mass = sum + w[i];
-                }
-                sum += w[i];
+    bool keep = tid < n;
+    uint64_t before = 0;
+    int rank = 0;
+    if (p.top_k < n || p.fraction < kOne) {
+        if (keep)
+#pragma unroll 8
+            for (int i = 0; i < n; ++i) {
+                const bool ahead = s.list[i] > mine;
+                before += ahead ? s.weights[i] : 0;
+                rank += ahead;
             }
-        __syncthreads();
-        many = s.found;
-        kept = s.found_mass;
-    }
-    const uint64_t target = share_down(kept, p.at);
-    // in the order of the vocabulary
-    const int sorted = power_of_two(many);
-    for (int i = tid; i < sorted; i += kPick) {
-        const uint64_t e = s.list[i];
-        s.list[i] = i < many ? ~(uint64_t(uint32_t(index_of(e))) << 32 | e >> 32) : 0;
-    }
-    sort_down<kPick>(s.list, sorted);
-    share = std::max(sorted / kPick, 1);
-    mine = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int at = tid * share + i;
-        w[i] = i < share && at < many ? r.key_weight(uint32_t(~s.list[at])) : 0;
-        mine += w[i];
-    }
-    uint64_t unused;
-    sum = PickBlock::before(mine, unused, s.block);
-    if (sum <= target && target < sum + mine)
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            if (sum <= target && target < sum + w[i]) {
-                const uint64_t e = ~s.list[tid * share + i];
-                finish_row(a, row, r, int(e >> 32), float_of(uint32_t(e)), kept, total);
-            }
-            sum += w[i];
+        keep = keep && rank < p.top_k;
+        uint64_t kept = PickBlock::sum(keep ? w : 0, s.block);
+        if (p.fraction < kOne) {
+            const uint64_t target = std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1));
+            if (kept < target)
+                return false;
+            keep = keep && before < target;
         }
+    }
+    const uint64_t kept = PickBlock::sum(keep ? w : 0, s.block);
+    if (tid < n)
+        s.weights[tid] = keep ? w : 0;
+    __syncthreads();
+    before = 0;
+    if (keep)
+#pragma unroll 8
+        for (int i = 0; i < n; ++i)
+            before += uint32_t(s.list[i]) > uint32_t(mine) ? s.weights[i] : 0; // indices before this one's
+    const uint64_t target = share_down(kept, p.at);
+    if (keep && before <= target && target < before + w)
+        finish_row(a, row, r, index_of(mine), float_of(key_in(mine)), kept, total);
     return true;
 }
 
+__device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
+                                               PickShared &s) {
+    const int tid = threadIdx.x;
+    int many = std::min(n, p.top_k), length = n;
+    uint64_t kept = 0;
+    // first in the order of the logits, for the last kept one, then in the order of the vocabulary, for the token
+#pragma unroll 1
+    for (int pass = 0;; ++pass) {
+        const int padded = power_of_two(length), share = std::max(padded / kPick, 1);
+        __syncthreads();
+        for (int i = length + tid; i < padded; i += kPick)
+            s.list[i] = 0;
+        sort_down<kPick>(s.list, padded);
+        const int from = tid * share, to = std::min(from + share, many);
+        uint64_t mine = 0, all;
+#pragma unroll 1
+        for (int i = from; i < to; ++i) {
+            const uint64_t e = s.list[i], w = r.key_weight(pass ? uint32_t(~e) : key_in(e));
+            s.weights[i] = w;
+            mine += w;
+        }
+        uint64_t sum = PickBlock::before(mine, all, s.block), target = 0;
+        if (pass)
+            target = share_down(kept, p.at) + 1; // sums are whole numbers: past it is to reach the next one
+        else {
+            kept = all;
+            if (p.fraction < kOne) {
+                target = std::max(share_up(whole ? all : total, p.fraction), uint64_t(1));
+                if (all < target)
+                    return false;
+            }
+        }
+        if (pass || p.fraction < kOne) {
+            if (sum < target && target <= sum + mine)
+#pragma unroll 1
+                for (int i = from; i < to; ++i) {
+                    sum += s.weights[i];
+                    if (sum >= target) {
+                        s.found = i + 1;
+                        s.found_mass = sum;
+                        break;
+                    }
+                }
+            __syncthreads();
+        }
+        if (pass) {
+            if (tid == 0) {
+                const uint64_t e = ~s.list[s.found - 1];
+                finish_row(a, row, r, int(e >> 32), float_of(uint32_t(e)), kept, total);
+            }
+            return true;
+        }
+        if (p.fraction < kOne) {
+            many = s.found;
+            kept = s.found_mass;
+        }
+        length = many;
+        for (int i = tid; i < many; i += kPick) {
+            const uint64_t e = s.list[i];
+            s.list[i] = ~(uint64_t(uint32_t(index_of(e))) << 32 | key_in(e));
+        }
+    }
+}
+
+// A key that the largest logits of at least `want` segments reach, and not many more: from a histogram of their distances
+// from the largest of all, as far as weights reach, or, where a bin of it holds too many, by halving.
+template <int kKeys>
+__device__ __forceinline__ uint32_t key_reached(const uint32_t (&keys)[kKeys], int segs, int want, float m, const Row &r, PickShared &s) {
+    const int tid = threadIdx.x, most = 2 * want + 64;
+    const float range = fminf(32.0f / float(r.scale), 64.0f); // of which bins of an even width are made
+    const float step = kPick / range;
+    __syncthreads();
+    s.count[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i)
+        if (i * kPick < segs) {
+            const float d = (m - float_of(keys[i])) * step;
+            if (d < float(kPick) && i * kPick + tid < segs)
+                atomicAdd(&s.count[int(d)], 1u);
+        }
+    __syncthreads();
+    const uint64_t mine = s.count[tid];
+    uint64_t all;
+    const uint64_t sum = PickBlock::before(mine, all, s.block);
+    if (tid == 0)
+        s.found = -1;
+    __syncthreads();
+    if (sum < uint64_t(want) && uint64_t(want) <= sum + mine && sum + mine <= uint64_t(most))
+        s.found = tid;
+    __syncthreads();
+    uint32_t from = 0, to = key_of(m) + 1;
+    if (s.found >= 0) {
+        // a little below the bin's end, whatever the roundings on the way
+        const float end = m - float(s.found + 1) / step;
+        return key_of(end - 1e-6f * fmaxf(fabsf(end), fabsf(m)));
+    }
+    for (int at = 0; to - from > 1; ++at) {
+        const uint32_t k = from + (to - from) / 2;
+        const int n = segments_from(keys, segs, k, at, s);
+        if (n >= want)
+            from = k;
+        else
+            to = k;
+        if (n >= want && n <= want + want / 8 + 8)
+            break;
+    }
+    return from;
+}
+
+// A workgroup takes a row.
 template <typename T>
-__global__ void __launch_bounds__(kPick) pick_kernel(const T *logits, Args a, Digest g) {
+__global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3))) pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ PickShared s;
     constexpr int kKeys = kMostParts * kSegs / kPick;
+    static_assert(kMostParts <= kPick, "a part a thread");
     const int tid = threadIdx.x, segs = g.parts * kSegs;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const Params p = params_of(a, row);
         const T *x = logits + row * a.stride;
         const float top = tid < g.parts ? g.top[row * g.parts + tid] : -INFINITY;
-        const uint64_t part_mass = tid < g.parts ? g.mass[row * g.parts + tid] : 0;
+        const double part_mass = tid < g.parts ? g.mass[row * g.parts + tid] : 0.0;
+        const Params p = params_of(a, row);
         const float m = PickBlock::max(top, s.block);
         if (p.scale == 0.0 || !(m < INFINITY) || m == -INFINITY) {
             finish_without(a, row, p.scale == 0.0 || m != -INFINITY);
             continue;
         }
-        Row r(m, p, a.shift);
+        const Row r(m, p.scale, a.shift);
         // the parts' weights, relative to the row's largest logit
-        const uint64_t mine = part_mass ? uint64_t(rint(double(part_mass) * power_of(fmax(double(top) - r.m, r.far), r.c, 0))) : 0;
+        const uint64_t mine = uint64_t(rint(part_mass * power_of(fmax(double(top) - r.m, r.far), r.c, 0)));
         uint64_t total;
         const uint64_t sum = PickBlock::before(mine, total, s.block);
         if (p.top_k == a.V && p.fraction == kOne && p.least == -INFINITY) {
             const uint64_t target = share_down(total, p.at);
             if (sum <= target && target < sum + mine) {
                 s.found = tid;
-                s.found_key = key_of(top);
-                // as far into the part's own sum
-                s.found_left = mine == part_mass ? target - sum : std::min(uint64_t(double(target - sum) / double(mine) * double(part_mass)), part_mass - 1);
+                s.found_top = top;
+                s.found_left = target - sum;
+                s.found_mass = mine;
             }
             __syncthreads();
-            const Row own(float_of(s.found_key), p, a.shift);
-            pick_in_part(a, row, x, s.found, own, r, Place{0, 0}, s.found_left, total, total, s);
+            const Row own(s.found_top, p.scale, a.shift);
+            pick_in_part<T, kPick>(a, row, x, s.found, own, r, Last(0), s.found_left, s.found_mass, total, total, s.block);
             __syncthreads();
             continue;
         }
-        r.floor = floor_key(r.m, p.scale, p.least, key_of(m));
-        int want = 0;
-        if (p.top_k < a.V)
-            want = p.top_k <= segs / 2 ? p.top_k : 0;
-        else if (r.floor == 0)
-            want = std::min(segs / 2, 128);
-        bool wide = want == 0 && r.floor == 0, whole = true;
-        uint32_t low = r.floor;
         uint32_t keys[kKeys];
 #pragma unroll
         for (int i = 0; i < kKeys; ++i)
             keys[i] = i * kPick + tid < segs ? key_of(g.seg[row * segs + i * kPick + tid]) : 0;
+        uint32_t low = floor_key(r.m, p.scale, p.least, key_of(m));
+        const float least = low ? float_of(low) : -INFINITY;
+        int want = 0;
+        if (p.top_k < a.V)
+            want = p.top_k <= segs / 2 ? p.top_k : 0;
+        else if (low == 0)
+            want = std::min(segs / 2, 128);
+        bool wide = want == 0 && low == 0, whole = true;
         if (want) {
-            // the largest key (or one not far below it) that the largest logits of `want` segments have
-            uint32_t from = 0, to = key_of(m) + 1;
-            for (int step = 0; to - from > 1; ++step) {
-                const uint32_t k = from + (to - from) / 2;
-                const int n = segments_from(keys, segs, k, step, s);
-                if (n >= want)
-                    from = k;
-                else
-                    to = k;
-                if (n >= want && n <= want + want / 8 + 8)
-                    break;
-            }
+            const uint32_t from = key_reached(keys, segs, want, m, r, s);
             whole = p.top_k < a.V || from <= low;
             low = std::max(low, from);
         }
@@ -953,113 +931,439 @@ __global__ void __launch_bounds__(kPick) pick_kernel(const T *logits, Args a, Di
 #pragma unroll
                 for (int j = 0; j < Part<T>::kSame; ++j) {
                     const int at = seg / kSegs * kPart + Part<T>::at(load + j, quarter * 16 + tid % 16);
+                    const typename Vec<T>::type q = read_vec(x + at, a.V - at);
 #pragma unroll
-                    for (int k = 0; k < Part<T>::N; ++k)
-                        if (at + k < a.V) {
-                            const uint32_t key = key_of(float(x[at + k]));
-                            if (key >= low) {
-                                const int to = atomicAdd(&s.n, 1);
-                                if (to < kList)
-                                    s.list[to] = entry_of(key, at + k);
-                            }
+                    for (int k = 0; k < Part<T>::N; ++k) {
+                        const uint32_t key = key_of(float(q[k]));
+                        if (key >= low && at + k < a.V) {
+                            const int to = atomicAdd(&s.n, 1);
+                            if (to < kList)
+                                s.list[to] = entry_of(key, at + k);
                         }
+                    }
                 }
             }
             __syncthreads();
             const int n = s.n;
-            wide = n > kList || !pick_from_list<T>(a, row, r, p, n, whole, total, s);
+            wide = n > kList ||
+                   !(n <= kPick ? pick_from_few(a, row, r, p, n, whole, total, s) : pick_from_list(a, row, r, p, n, whole, total, s));
         }
-        if (wide)
-            wide_row(a, row, x, r, p, total, s);
+        if (wide && tid == 0) {
+            WideRow &w = g.rows[atomicAdd(g.wide, 1u)];
+            w.row = row;
+            w.top = m;
+            w.least = least;
+            w.total = total;
+            w.arrived[0] = w.arrived[1] = w.listed = 0;
+        }
         __syncthreads();
     }
 }
 
-// Rows too long for a digest's sums: read once for the largest logit, once for the weights, and then by wide_row's means.
+// ------------------------------------------------------------------------------------------------
+// rows of which more tokens are kept than a list holds
+// ------------------------------------------------------------------------------------------------
+constexpr int kWide = 512;
+constexpr int kSlices = 512, kMostShares = 16;
+using WideBlock = Block<kWide>;
+
+// Workgroups that share a row, so that a few wide rows have many and many have one each.
+__device__ __forceinline__ int shares_of(unsigned wide, int parts) {
+    return wide > kSlices / 2 ? 1 : std::max(1, std::min(std::min(int(kSlices / wide), kMostShares), parts / 4));
+}
+
+struct WideShared {
+    uint64_t mass[kFine];
+    uint32_t count[kFine];
+    uint64_t list[kList];
+    uint64_t kept[kMostParts];
+    WideBlock::Shared block;
+    uint64_t found_mass, found_left;
+    int found, n;
+    bool last;
+};
+
+// The bin of a logit by its distance from the largest, which never decreases as logits do; kFine: its weight is 0. Halves,
+// because the distance itself may be no float.
+struct Bins {
+    float half, step;
+    __device__ __forceinline__ Bins(const Row &r)
+        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 31.5f), 3.402823466e38f)) {}
+    __device__ __forceinline__ int of(float x) const {
+        const float d = (half - x * 0.5f) * step;
+        return d < float(kFine) ? int(d) : kFine;
+    }
+};
+
+// Calls f(logit, index) for a share of a row's vectors.
+template <typename T, typename F> __device__ __forceinline__ void for_share(const T *x, int V, int share, int shares, F &&f) {
+    constexpr int N = Vec<T>::N;
+    const int vecs = (V + N - 1) / N, each = (vecs + shares - 1) / shares, end = std::min(vecs, (share + 1) * each);
+    for (int i = share * each + int(threadIdx.x); i < end; i += kWide) {
+        const typename Vec<T>::type q = read_vec(x + i * N, V - i * N);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            f(float(q[k]), i * N + k);
+    }
+}
+
+// Counts and weights of a share of the logits in each bin.
+template <typename T>
+__device__ __forceinline__ void fill_bins(const T *x, int V, int share, int shares, const Row &r, const Bins &bins, float least, WideShared &s) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kFine; i += kWide)
+        s.mass[i] = s.count[i] = 0;
+    __syncthreads();
+    for_share(x, V, share, shares, [&](float v, int) {
+        const int bin = bins.of(v);
+        if (bin < kFine && v >= least) {
+            atomicAdd(&s.count[bin], 1u);
+            atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[bin]), (unsigned long long)r.weight(v));
+        }
+    });
+    __syncthreads();
+}
+
+// The bin in which the count (by_mass: the weights) from the top reaches `target`, which it does within the bins; `left`
+// receives what is left of the target there, `above` the weights of the bins above.
+__device__ __forceinline__ int bin_of(bool by_mass, uint64_t target, uint64_t &left, uint64_t &above, WideShared &s) {
+    constexpr int kEach = kFine / kWide;
+    uint64_t mine = 0, mine_mass = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int b = threadIdx.x * kEach + i;
+        mine += by_mass ? s.mass[b] : s.count[b];
+        mine_mass += s.mass[b];
+    }
+    uint64_t sum = WideBlock::before(mine, all, s.block);
+    uint64_t sum_mass = WideBlock::before(mine_mass, all, s.block);
+    if (sum < target && target <= sum + mine)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int b = threadIdx.x * kEach + i;
+            const uint64_t here = by_mass ? s.mass[b] : s.count[b];
+            if (sum < target && target <= sum + here) {
+                s.found = b;
+                s.found_left = target - sum;
+                s.found_mass = sum_mass;
+            }
+            sum += here;
+            sum_mass += s.mass[b];
+        }
+    __syncthreads();
+    left = s.found_left;
+    above = s.found_mass;
+    return s.found;
+}
+
+// Sorts the n entries of a bin and finds the one at which their count (by_mass: their weights) reaches `left`; `inside`
+// receives the weights down to it.
+__device__ __forceinline__ int place_in_list(bool by_mass, uint64_t left, int n, const Row &r, uint64_t &inside, WideShared &s) {
+    const int padded = power_of_two(n), share = std::max(padded / kWide, 1), tid = threadIdx.x;
+    __syncthreads();
+    for (int i = n + tid; i < padded; i += kWide)
+        s.list[i] = 0;
+    sort_down<kWide>(s.list, padded);
+    const int from = tid * share, to = std::min(from + share, n);
+    uint64_t mine = 0, mine_mass = 0, all;
+#pragma unroll 1
+    for (int i = from; i < to; ++i) {
+        const uint64_t w = r.key_weight(key_in(s.list[i]));
+        mine += by_mass ? w : 1;
+        mine_mass += w;
+    }
+    uint64_t sum = WideBlock::before(mine, all, s.block);
+    uint64_t sum_mass = WideBlock::before(mine_mass, all, s.block);
+    if (sum < left && left <= sum + mine)
+#pragma unroll 1
+        for (int i = from; i < to; ++i) {
+            const uint64_t w = r.key_weight(key_in(s.list[i]));
+            sum += by_mass ? w : 1;
+            sum_mass += w;
+            if (sum >= left) {
+                s.found = i;
+                s.found_mass = sum_mass;
+                break;
+            }
+        }
+    __syncthreads();
+    inside = s.found_mass;
+    return s.found;
+}
+
+// Whether this workgroup is the last of `shares` to come here; what the others wrote before is then seen.
+__device__ __forceinline__ bool is_last(unsigned *arrived, int shares, WideShared &s) {
+    if (shares == 1)
+        return true;
+    __builtin_amdgcn_s_waitcnt(0); // every wave's stores have reached the cache
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence(); // for the whole workgroup, which shares its caches: a fence of every wave's own took ten times as long
+        s.last = atomicAdd(arrived, 1u) == unsigned(shares - 1);
+        if (s.last)
+            __threadfence();
+    }
+    __syncthreads();
+    return s.last;
+}
+
+// Where the last kept token is: counts and weights in bins of the distance from the largest logit say in which.
+template <typename T>
+__global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4))) wide_place_kernel(const T *logits, Args a, Digest g) {
+    __shared__ WideShared s;
+    const int tid = threadIdx.x;
+    const unsigned wide = *g.wide;
+    if (wide == 0)
+        return;
+    const int shares = shares_of(wide, g.parts);
+    const int64_t items = int64_t(wide) * shares;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t slot = item / shares;
+        WideRow &w = g.rows[slot];
+        const int64_t row = w.row;
+        const Params p = params_of(a, row);
+        const T *x = logits + row * a.stride;
+        const float least = w.least;
+        const Row r(w.top, p.scale, a.shift);
+        const Bins bins(r);
+        uint64_t last = least == -INFINITY ? 0 : entry_of(key_of(least), -1), left = 0, above;
+        int bin = kFine, members = 0;
+        bool by_mass = false;
+        if (p.top_k < a.V || p.fraction < kOne) {
+            fill_bins(x, a.V, int(item - slot * shares), shares, r, bins, least, s);
+            if (shares > 1) {
+                for (int i = tid; i < kFine; i += kWide) {
+                    g.bins[item * kFine + i] = s.mass[i];
+                    g.members[item * kFine + i] = s.count[i];
+                }
+                if (!is_last(&w.arrived[0], shares, s))
+                    continue;
+                for (int i = tid; i < kFine; i += kWide) {
+                    uint64_t mass = 0;
+                    uint32_t count = 0;
+                    for (int k = 0; k < shares; ++k) {
+                        mass += g.bins[(slot * shares + k) * kFine + i];
+                        count += g.members[(slot * shares + k) * kFine + i];
+                    }
+                    s.mass[i] = mass;
+                    s.count[i] = count;
+                }
+                __syncthreads();
+            }
+            uint64_t there = 0, inside = 0;
+            for (int i = tid; i < kFine; i += kWide) {
+                there += s.count[i];
+                inside += s.mass[i];
+            }
+            there = WideBlock::sum(there, s.block);
+            inside = WideBlock::sum(inside, s.block);
+            const bool cut = uint64_t(p.top_k) < there; // otherwise what it cuts off has no weight
+            if (cut) {
+                bin = bin_of(false, uint64_t(p.top_k), left, above, s);
+                members = int(s.count[bin]);
+            }
+            if (cut && p.fraction < kOne) { // what top_p is a share of has to be known
+                if (members > kList)
+                    last = WideBlock::place_of<false>(x, a.V, r, least, uint64_t(p.top_k), inside, s.mass, s.count, s.block);
+                else {
+                    __syncthreads();
+                    if (tid == 0)
+                        s.n = 0;
+                    __syncthreads();
+                    for_share(x, a.V, 0, 1, [&](float v, int i) {
+                        if (bins.of(v) == bin && v >= least)
+                            s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), i);
+                    });
+                    __syncthreads();
+                    place_in_list(false, left, members, r, inside, s);
+                    inside += above;
+                    __syncthreads();
+                }
+                if (members > kList)
+                    fill_bins(x, a.V, 0, 1, r, bins, least, s);
+            }
+            if (p.fraction < kOne) {
+                by_mass = true;
+                bin = bin_of(true, std::max(share_up(inside, p.fraction), uint64_t(1)), left, above, s);
+                members = int(s.count[bin]);
+            }
+            if (members > kList) { // a great many near equals
+                __syncthreads();
+                const uint64_t target = by_mass ? std::max(share_up(inside, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
+                uint64_t unused;
+                last = by_mass ? WideBlock::place_of<true>(x, a.V, r, least, target, unused, s.mass, s.count, s.block)
+                               : WideBlock::place_of<false>(x, a.V, r, least, target, unused, s.mass, s.count, s.block);
+                bin = kFine;
+            }
+        }
+        if (tid == 0) {
+            w.last = last;
+            w.left = left;
+            w.bin = bin;
+            w.members = members;
+            w.by_mass = by_mass;
+        }
+        __syncthreads();
+    }
+}
+
+// The kept weights of every part, the bin's entries, and the token.
+template <typename T>
+__global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4))) wide_pick_kernel(const T *logits, Args a, Digest g) {
+    __shared__ WideShared s;
+    using P = Part<T>;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const unsigned wide = *g.wide;
+    if (wide == 0)
+        return;
+    const int shares = shares_of(wide, g.parts);
+    const int64_t items = int64_t(wide) * shares;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t slot = item / shares;
+        WideRow &w = g.rows[slot];
+        const int64_t row = w.row;
+        const Params p = params_of(a, row);
+        const T *x = logits + row * a.stride;
+        const Row r(w.top, p.scale, a.shift);
+        const Bins bins(r);
+        const float least = w.least;
+        const int bin = w.bin;
+        const bool exact = bin == kFine;
+        const Last last(w.last);
+        uint64_t *list = shares > 1 ? g.list + slot * kList : s.list;
+        uint64_t *kept_of = shares > 1 ? g.kept + slot * kMostParts : s.kept;
+        if (tid == 0)
+            s.n = 0;
+        __syncthreads();
+        for (int part = int(item - slot * shares) + wave * shares; part < g.parts; part += shares * WideBlock::kWaves) {
+            uint64_t mass = 0;
+#pragma unroll 1
+            for (int j = 0; j < P::kLoads; ++j) {
+                const int at = part * kPart + P::at(j, lane);
+                const typename Vec<T>::type q = read_vec(x + at, a.V - at);
+#pragma unroll
+                for (int k = 0; k < P::N; ++k) {
+                    const float v = float(q[k]);
+                    const int mine = bins.of(v);
+                    const bool in = v >= least;
+                    if (exact ? last.keeps(v, at + k) : in && mine < bin)
+                        mass += r.weight(v);
+                    if (!exact && in && mine == bin) {
+                        const int to = shares > 1 ? int(atomicAdd(&w.listed, 1u)) : atomicAdd(&s.n, 1);
+                        list[to] = entry_of(key_of(v), at + k);
+                    }
+                }
+            }
+            mass = wave_sum(mass);
+            if (lane == 0)
+                kept_of[part] = mass;
+        }
+        if (!is_last(&w.arrived[1], shares, s))
+            continue;
+        __syncthreads();
+        uint64_t end = w.last;
+        if (shares > 1 && tid < g.parts)
+            s.kept[tid] = kept_of[tid];
+        if (!exact) {
+            const int n = w.members;
+            if (shares > 1)
+                for (int i = tid; i < n; i += kWide)
+                    s.list[i] = list[i];
+            uint64_t unused;
+            const int at = place_in_list(w.by_mass, w.left, n, r, unused, s);
+            end = s.list[at];
+            for (int i = tid; i <= at; i += kWide)
+                atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(s.list[i]) / kPart]), (unsigned long long)r.key_weight(key_in(s.list[i])));
+        }
+        __syncthreads();
+        uint64_t kept;
+        const uint64_t mine = tid < g.parts ? s.kept[tid] : 0;
+        const uint64_t sum = WideBlock::before(mine, kept, s.block);
+        const uint64_t target = share_down(kept, p.at);
+        if (sum <= target && target < sum + mine) {
+            s.found = tid;
+            s.found_left = target - sum;
+            s.found_mass = mine;
+        }
+        __syncthreads();
+        pick_in_part<T, kWide>(a, row, x, s.found, r, r, Last(end), s.found_left, s.found_mass, kept, w.total, s.block);
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// rows too long for a digest
+// ------------------------------------------------------------------------------------------------
 constexpr int kLong = 1024;
+
+// A workgroup reads the row once for its largest logit, once for its weights, five times for each place and twice for the
+// token.
 template <typename T>
 __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
     using B = Block<kLong>;
     __shared__ B::Shared s;
     __shared__ uint64_t mass[kBins];
     __shared__ uint32_t count[kBins];
-    __shared__ uint64_t part[B::kWaves], ties[B::kWaves];
+    __shared__ uint64_t part[B::kWaves];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const Params p = params_of(a, row);
         const T *x = logits + row * a.stride;
         float m = -INFINITY;
-        for (int i = tid; i < a.V; i += kLong)
+        for (int64_t i = tid; i < a.V; i += kLong)
             m = larger(m, float(x[i]));
         m = B::max(m, s);
         if (p.scale == 0.0 || !(m < INFINITY) || m == -INFINITY) {
             finish_without(a, row, p.scale == 0.0 || m != -INFINITY);
             continue;
         }
-        Row r(m, p, a.shift);
-        r.floor = floor_key(r.m, p.scale, p.least, key_of(m));
-        uint64_t total = 0, inside = 0, there = 0, above;
-        for (int i = tid; i < a.V; i += kLong) {
+        const Row r(m, p.scale, a.shift);
+        const uint32_t floor = floor_key(r.m, p.scale, p.least, key_of(m));
+        const float least = floor ? float_of(floor) : -INFINITY;
+        uint64_t total = 0, inside = 0, there = 0, unused;
+        for (int64_t i = tid; i < a.V; i += kLong) {
             const float v = float(x[i]);
             const uint64_t w = r.weight(v);
-            const bool in = key_of(v) >= r.floor;
             total += w;
-            inside += in ? w : 0;
-            there += in;
+            inside += v >= least ? w : 0;
+            there += v >= least;
         }
         total = B::sum(total, s);
         inside = B::sum(inside, s);
         there = B::sum(there, s);
-        Place place{r.floor ? r.floor - 1 : 0, 0};
-        if (uint64_t(p.top_k) < there) {
-            place = B::template place_of<false>(x, a.V, r, uint64_t(p.top_k), above, mass, count, s);
-            inside = above + place.spare * r.key_weight(place.key);
-        }
+        uint64_t end = floor ? entry_of(floor, -1) : 0;
+        if (uint64_t(p.top_k) < there)
+            end = B::template place_of<false>(x, a.V, r, least, uint64_t(p.top_k), inside, mass, count, s);
         if (p.fraction < kOne)
-            place = B::template place_of<true>(x, a.V, r, std::max(share_up(inside, p.fraction), uint64_t(1)), above, mass, count, s);
-        // waves take stretches of the vocabulary; a token's equals before it decide whether it is kept
-        const int each = (a.V + kLong - 1) / kLong * kWave;
-        const int from = int(std::min(int64_t(wave) * each, int64_t(a.V))), to = int(std::min(int64_t(from) + each, int64_t(a.V)));
-        const uint64_t level = place.spare ? r.key_weight(place.key) : 0;
-        uint64_t my_mass = 0, my_ties = 0;
-        for (int64_t i = int64_t(from) + lane; i < to; i += kWave) {
+            end = B::template place_of<true>(x, a.V, r, least, std::max(share_up(inside, p.fraction), uint64_t(1)), unused, mass, count, s);
+        const Last last(end);
+        // waves take stretches of the vocabulary
+        const int64_t each = int64_t((a.V - 1) / kLong + 1) * kWave;
+        const int64_t from = std::min(wave * each, int64_t(a.V)), to = std::min(from + each, int64_t(a.V));
+        uint64_t mine = 0;
+        for (int64_t i = from + lane; i < to; i += kWave) {
             const float v = float(x[i]);
-            const uint32_t k = key_of(v);
-            my_mass += k > place.key ? r.weight(v) : 0;
-            my_ties += k == place.key;
+            mine += last.keeps(v, int(i)) ? r.weight(v) : 0;
         }
-        my_mass = wave_sum(my_mass);
-        my_ties = wave_sum(my_ties);
+        mine = wave_sum(mine);
         __syncthreads();
-        if (lane == 0) {
-            part[wave] = my_mass;
-            ties[wave] = my_ties;
-        }
+        if (lane == 0)
+            part[wave] = mine;
         __syncthreads();
-        uint64_t kept = 0, sum = 0, equal = 0, rank = 0;
+        uint64_t kept = 0, sum = 0;
         for (int w = 0; w < B::kWaves; ++w) {
-            if (w == wave) {
-                sum = kept;
-                rank = equal;
-            }
-            kept += part[w] + std::min(ties[w], place.spare - std::min(equal, place.spare)) * level;
-            equal += ties[w];
+            sum = w == wave ? kept : sum;
+            kept += part[w];
         }
         const uint64_t target = share_down(kept, p.at);
-        const bool mine = sum <= target;
-        for (int64_t i = int64_t(from) + lane; i - lane < to && sum <= target; i += kWave) {
-            const bool in = i < to;
-            const float v = in ? float(x[i]) : -INFINITY;
-            const uint32_t k = key_of(v);
-            const uint64_t tied = __ballot(in && k == place.key);
-            const uint64_t my_rank = rank + __builtin_popcountll(tied & ((uint64_t(1) << lane) - 1));
-            const bool keep = in && (k > place.key || (k == place.key && my_rank < place.spare));
-            const uint64_t with = sum + wave_scan(keep ? r.weight(v) : 0);
+        const bool first = sum <= target;
+        for (int64_t i = from + lane; i - lane < to && sum <= target; i += kWave) {
+            const float v = i < to ? float(x[i]) : -INFINITY;
+            const uint64_t with = sum + wave_scan(i < to && last.keeps(v, int(i)) ? r.weight(v) : 0);
             const uint64_t past = __ballot(with > target);
-            if (mine && past && lane == __builtin_ctzll(past))
+            if (first && past && lane == __builtin_ctzll(past))
                 finish_row(a, row, r, int(i), v, kept, total);
-            rank += __builtin_popcountll(tied);
-            sum = __shfl(with, kWave - 1);
+            sum = last_lane(with);
         }
         __syncthreads();
     }
@@ -1067,21 +1371,51 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
 
 // How rows of V tokens are taken.
 struct Plan {
-    int group; // of small_kernel; 0: a digest
-    int parts; // 0 and no group: long_kernel
+    int group, own; // of small_kernel; 0: a digest
+    int parts;      // 0 and no group: long_kernel
 };
 
 Plan plan_of(int64_t V) {
-    if (V <= kOwn * kWave)
-        return {kWave, 0};
-    if (V <= kOwn * 256)
-        return {256, 0};
-    if (V < int64_t(kMostParts) * kPart)
-        return {0, int((V + kPart - 1) / kPart)};
-    return {0, 0};
+    if (V <= 4 * kWave)
+        return {kWave, 4, 0};
+    if (V <= 8 * kWave)
+        return {kWave, 8, 0};
+    if (V <= 8 * 256)
+        return {256, 8, 0};
+    if (V >= int64_t(kMostParts) * kPart)
+        return {0, 0, 0};
+    return {0, 0, int((V + kPart - 1) / kPart)};
 }
 
-constexpr int64_t kPartBytes = sizeof(uint64_t) + sizeof(float) * (1 + kSegs);
+// What the kernels leave for the next ones, behind each other in the workspace.
+struct Space {
+    char *at;
+    int64_t bytes = 0;
+    template <typename T> T *take(int64_t count) {
+        T *p = reinterpret_cast<T *>(at + bytes);
+        bytes += (count * int64_t(sizeof(T)) + 15) / 16 * 16;
+        return p;
+    }
+};
+
+// Its bytes, and where its parts are in a workspace at `at`.
+int64_t lay_out(const Plan &p, int64_t n, char *at, Digest &g) {
+    Space s{at};
+    g.parts = p.parts;
+    if (!p.parts)
+        return 0;
+    g.wide = s.take<unsigned>(1);
+    g.rows = s.take<WideRow>(n);
+    g.mass = s.take<double>(n * p.parts);
+    g.top = s.take<float>(n * p.parts);
+    g.seg = s.take<float>(n * p.parts * kSegs);
+    const int64_t slices = std::min<int64_t>(n * kMostShares, kSlices), slots = std::min<int64_t>(n, kSlices / 2);
+    g.bins = s.take<uint64_t>(slices * kFine);
+    g.members = s.take<unsigned>(slices * kFine);
+    g.kept = s.take<uint64_t>(slots * kMostParts);
+    g.list = s.take<uint64_t>(slots * kList);
+    return s.bytes;
+}
 
 int size_of(int32_t dtype) { return dtype == TREE_ENS_F32 ? 4 : 2; }
 
@@ -1094,7 +1428,7 @@ int check_sizes(int32_t dtype, int64_t n, int64_t V) {
         return set_error(TREE_ENS_E_ARG, "dtype must be TREE_ENS_F32, TREE_ENS_BF16 or TREE_ENS_F16");
     if (n < 0 || V < 1 || V > INT32_MAX)
         return set_error(TREE_ENS_E_ARG, "n_tokens must be >= 0 and n_vocab in [1, INT32_MAX]");
-    if (n > INT64_MAX / kPartBytes / kMostParts)
+    if (n > INT64_MAX / 1024 / kMostParts)
         return set_error(TREE_ENS_E_ARG, "n_tokens must be within memory");
     return TREE_ENS_OK;
 }
@@ -1110,7 +1444,9 @@ int tree_ens_sample_workspace(int32_t dtype, int64_t n_tokens, int64_t n_vocab, 
     *bytes = 0;
     if (int rc = check_sizes(dtype, n_tokens, n_vocab))
         return rc;
-    *bytes = n_tokens * plan_of(n_vocab).parts * kPartBytes;
+    Digest g;
+    if (n_tokens > 0)
+        *bytes = lay_out(plan_of(n_vocab), n_tokens, nullptr, g);
     return TREE_ENS_OK;
 }
 
@@ -1141,7 +1477,8 @@ int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_t
         misaligned(logp, 4) || misaligned(log_kept, 4))
         return set_error(TREE_ENS_E_ARG, "a row's parameters, logp or log_kept is misaligned");
     const Plan plan = plan_of(n_vocab);
-    if (const int64_t need = n_tokens * plan.parts * kPartBytes) {
+    Digest g;
+    if (const int64_t need = lay_out(plan, n_tokens, static_cast<char *>(workspace), g)) {
         if (!workspace || workspace_bytes < need)
             return set_error(TREE_ENS_E_ARG, "workspace is NULL or smaller than " + std::to_string(need) + " bytes");
         if (misaligned(workspace, 16))
@@ -1158,19 +1495,18 @@ int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_t
     const auto launch = [&](auto *type) {
         using T = std::decay_t<decltype(*type)>;
         const T *x = static_cast<const T *>(logits);
-        if (plan.group == kWave)
-            hipLaunchKernelGGL((small_kernel<T, kWave>), rows, dim3(kWave), 0, s, x, a);
-        else if (plan.group)
-            hipLaunchKernelGGL((small_kernel<T, 256>), rows, dim3(256), 0, s, x, a);
-        else if (plan.parts) {
-            Digest g;
-            g.parts = plan.parts;
-            g.mass = static_cast<uint64_t *>(workspace);
-            g.top = reinterpret_cast<float *>(g.mass + n_tokens * plan.parts);
-            g.seg = g.top + n_tokens * plan.parts;
+        if (plan.group) {
+            const auto kernel = plan.group == 256 ? small_kernel<T, 256, 8> : plan.own == 8 ? small_kernel<T, kWave, 8> : small_kernel<T, kWave, 4>;
+            hipLaunchKernelGGL(kernel, rows, dim3(unsigned(plan.group)), 0, s, x, a);
+        } else if (plan.parts) {
             const int64_t blocks = (n_tokens * plan.parts + 3) / 4;
             hipLaunchKernelGGL(scan_kernel<T>, dim3(unsigned(std::min(blocks, kMaxBlocks))), dim3(256), 0, s, x, a, g);
             hipLaunchKernelGGL(pick_kernel<T>, rows, dim3(kPick), 0, s, x, a, g);
+            if (!row_top_k && !row_top_p && !row_min_p && a.top_k == 0 && top_p == 1.0f && min_p == 0.0f)
+                return; // no row is cut off
+            const dim3 wide(unsigned(std::min<int64_t>(n_tokens * kMostShares, 2 * kSlices)));
+            hipLaunchKernelGGL(wide_place_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
+            hipLaunchKernelGGL(wide_pick_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
         } else
             hipLaunchKernelGGL(long_kernel<T>, rows, dim3(kLong), 0, s, x, a);
     };
