@@ -164,8 +164,8 @@ __device__ __forceinline__ float larger(float a, float b) { return __builtin_ele
 template <int kCtrl, int kRows, bool kOwn = false> __device__ __forceinline__ unsigned moved(unsigned v) {
     return unsigned(__builtin_amdgcn_update_dpp(kOwn ? int(v) : 0, int(v), kCtrl, kRows, 0xf, false));
 }
-template <int kCtrl, int kRows> __device__ __forceinline__ uint64_t moved(uint64_t v) {
-    return uint64_t(moved<kCtrl, kRows>(unsigned(v >> 32))) << 32 | moved<kCtrl, kRows>(unsigned(v));
+template <int kCtrl, int kRows, bool kOwn = false> __device__ __forceinline__ uint64_t moved(uint64_t v) {
+    return uint64_t(moved<kCtrl, kRows, kOwn>(unsigned(v >> 32))) << 32 | moved<kCtrl, kRows, kOwn>(unsigned(v));
 }
 template <int kCtrl, int kRows> __device__ __forceinline__ double moved(double v) {
     return __longlong_as_double(moved<kCtrl, kRows>(uint64_t(__double_as_longlong(v))));
@@ -191,14 +191,20 @@ template <typename V> __device__ __forceinline__ V wave_sum(V v) { return last_l
 template <int kCtrl, int kRows = 0xf> __device__ __forceinline__ float moved_larger(float v) {
     return larger(v, __uint_as_float(moved<kCtrl, kRows, true>(__float_as_uint(v))));
 }
-__device__ __forceinline__ float wave_max(float v) {
+template <int kCtrl, int kRows = 0xf> __device__ __forceinline__ uint64_t moved_larger(uint64_t v) {
+    return std::max(v, moved<kCtrl, kRows, true>(v));
+}
+__device__ __forceinline__ float last_lane(float v) {
+    return __uint_as_float(unsigned(__builtin_amdgcn_readlane(int(__float_as_uint(v)), kWave - 1)));
+}
+template <typename V> __device__ __forceinline__ V wave_max(V v) {
     v = moved_larger<0x111>(v);
     v = moved_larger<0x112>(v);
     v = moved_larger<0x114>(v);
     v = moved_larger<0x118>(v);
     v = moved_larger<0x142, 0xa>(v);
     v = moved_larger<0x143, 0xc>(v);
-    return __uint_as_float(unsigned(__builtin_amdgcn_readlane(int(__float_as_uint(v)), kWave - 1)));
+    return last_lane(v);
 }
 
 __device__ __forceinline__ void store_row(const Args &a, int64_t row, int64_t token, float logp, float log_kept) {
@@ -379,38 +385,94 @@ template <int kT> struct Block {
 };
 
 // ------------------------------------------------------------------------------------------------
-// sorting in LDS
+// lists of entries in LDS
 // ------------------------------------------------------------------------------------------------
-// Waits for the other threads of what shares stretches of `stride` pairs: a wave's LDS accesses are in order.
-template <int kT> __device__ __forceinline__ void sort_wait(int stride) {
-    if (kT > kWave && stride > kWave)
-        __syncthreads();
-    else {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
+enum class Order { kLogits, kVocabulary };
+
+// An entry as the order has it, the first one the largest: by index where the halves are changed over.
+template <Order kOrder> __device__ __forceinline__ uint64_t ordered(uint64_t entry) {
+    return kOrder == Order::kLogits ? entry : entry << 32 | entry >> 32;
 }
 
-// Sorts n (a power of two) entries, the largest first. Pairs of a stride up to 64 lie in the 128 entries that one wave
-// takes, and need no barrier between the steps.
-template <int kT> __device__ void sort_down(uint64_t *v, int n) {
-    __syncthreads();
-    for (int k = 2; k <= n; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            for (int p = threadIdx.x; p < n / 2; p += kT) {
-                const int i = 2 * p - (p & (j - 1));
-                const uint64_t a = v[i], b = v[i + j];
-                if ((a < b) == ((i & k) == 0)) {
-                    v[i] = b;
-                    v[i + j] = a;
+template <int kT> struct List {
+    using B = Block<kT>;
+    struct Shared {
+        uint64_t mass[kT];
+        uint32_t count[kT];
+        uint64_t high[B::kWaves], low[B::kWaves];
+        uint64_t left, above, entry;
+        uint32_t digit;
+    };
+
+    // The entry of list[0, n) at which the count (by_mass: the weights) of those of at least `least` reaches `target`, which it
+    // does; `inside` receives the weights down to it. By bins of the range that the entries have, as many as there are
+    // threads, and then of the range of the bin that holds it, until it is alone: two or three times, whatever the entries.
+    template <Order kOrder>
+    static __device__ __forceinline__ uint64_t find(bool by_mass, uint64_t target, const uint64_t *list, int n, uint64_t least, const Row &r,
+                                                    uint64_t &inside, Shared &s, typename B::Shared &block) {
+        const int tid = threadIdx.x;
+        uint64_t high = 0, low = ~uint64_t(0);
+        for (int i = tid; i < n; i += kT)
+            if (list[i] >= least) {
+                high = std::max(high, ordered<kOrder>(list[i]));
+                low = std::min(low, ordered<kOrder>(list[i]));
+            }
+        high = wave_max(high);
+        low = ~wave_max(~low);
+        if constexpr (B::kWaves > 1) {
+            __syncthreads();
+            if (tid % kWave == 0) {
+                s.high[tid / kWave] = high;
+                s.low[tid / kWave] = low;
+            }
+            __syncthreads();
+            for (int w = 0; w < B::kWaves; ++w) {
+                high = std::max(high, s.high[w]);
+                low = std::min(low, s.low[w]);
+            }
+        }
+        uint64_t above = 0;
+        for (;;) {
+            const uint64_t span = high - low;
+            const int shift = span < kT ? 0 : 64 - __builtin_clzll(span) - (31 - __builtin_clz(kT));
+            __syncthreads();
+            s.mass[tid] = s.count[tid] = 0;
+            __syncthreads();
+            for (int i = tid; i < n; i += kT) {
+                const uint64_t e = ordered<kOrder>(list[i]);
+                if (list[i] >= least && e <= high && e >= low) {
+                    const int bin = int((high - e) >> shift);
+                    atomicAdd(&s.count[bin], 1u);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[bin]), (unsigned long long)r.key_weight(key_in(list[i])));
                 }
             }
-            sort_wait<kT>(std::max(j, j > 1 ? j / 2 : k));
+            __syncthreads();
+            const uint64_t mass = s.mass[tid], mine = by_mass ? mass : s.count[tid];
+            uint64_t unused;
+            const uint64_t mass_before = B::before(mass, unused, block), before = by_mass ? mass_before : B::before(mine, unused, block);
+            if (before < target && target <= before + mine) {
+                s.digit = tid;
+                s.left = target - before;
+                s.above = mass_before;
+            }
+            __syncthreads();
+            const int bin = int(s.digit);
+            target = s.left;
+            above += s.above;
+            high -= uint64_t(bin) << shift;
+            low = high - std::min(high - low, (uint64_t(1) << shift) - 1);
+            if (s.count[bin] == 1 || shift == 0) {
+                inside = above + s.mass[bin];
+                break;
+            }
         }
-    __syncthreads();
-}
-
-__device__ __forceinline__ int power_of_two(int n) { return n <= 2 ? 2 : 1 << (32 - __builtin_clz(unsigned(n - 1))); }
+        for (int i = tid; i < n; i += kT)
+            if (list[i] >= least && ordered<kOrder>(list[i]) <= high && ordered<kOrder>(list[i]) >= low)
+                s.entry = list[i];
+        __syncthreads();
+        return s.entry;
+    }
+};
 
 // ------------------------------------------------------------------------------------------------
 // short rows
@@ -418,9 +480,10 @@ __device__ __forceinline__ int power_of_two(int n) { return n <= 2 ? 2 : 1 << (3
 template <typename T, int kT, int kOwn>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn == 4 ? 4 : 3))) small_kernel(const T *logits, Args a) {
     using B = Block<kT>;
+    using L = List<kT>;
     __shared__ typename B::Shared s;
+    __shared__ typename L::Shared find;
     __shared__ uint64_t list[kOwn * kT];
-    __shared__ uint64_t last;
     const int tid = threadIdx.x, each = (a.V + kT - 1) / kT, from = tid * each;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *x = logits + row * a.stride;
@@ -447,43 +510,24 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
         total = B::sum(total, s);
         uint64_t lowest = entry_of(floor, -1); // entries from here on are kept
         if (p.top_k < a.V || p.fraction < kOne) {
-            const int n = power_of_two(a.V);
             __syncthreads();
-            if (tid == 0)
-                last = 0;
-            for (int i = a.V + tid; i < n; i += kT)
-                list[i] = 0;
+            uint64_t inside = 0, there = 0;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i)
                 if (i < each && from + i < a.V) {
-                    const uint32_t k = key_of(v[i]);
-                    list[from + i] = k >= floor ? entry_of(k, from + i) : 0;
+                    const uint64_t e = entry_of(key_of(v[i]), from + i);
+                    list[from + i] = e;
+                    inside += e >= lowest ? w[i] : 0;
+                    there += e >= lowest;
                 }
-            sort_down<kT>(list, n);
-            const int share = std::max(n / kT, 1);
-            uint64_t sorted[kOwn], mine = 0;
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) {
-                const int at = tid * share + i;
-                const uint64_t e = i < share && at < std::min(n, p.top_k) ? list[at] : 0;
-                sorted[i] = e ? r.key_weight(key_in(e)) : 0;
-                mine += sorted[i];
-            }
-            uint64_t all;
-            uint64_t sum = B::before(mine, all, s);
-            if (p.fraction < kOne) {
-                const uint64_t target = std::max(share_up(all, p.fraction), uint64_t(1));
-                if (sum < target && target <= sum + mine)
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        if (sum < target && target <= sum + sorted[i])
-                            last = list[tid * share + i];
-                        sum += sorted[i];
-                    }
-            } else if (tid == 0)
-                last = list[p.top_k - 1]; // 0 where min_p keeps fewer
+            inside = B::sum(inside, s);
+            there = B::sum(there, s);
             __syncthreads();
-            lowest = std::max(lowest, last);
+            if (uint64_t(p.top_k) < there)
+                lowest = L::template find<Order::kLogits>(false, uint64_t(p.top_k), list, a.V, lowest, r, inside, find, s);
+            uint64_t unused;
+            if (p.fraction < kOne)
+                lowest = L::template find<Order::kLogits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, r, unused, find, s);
         }
         uint64_t mine = 0;
 #pragma unroll
@@ -536,6 +580,18 @@ template <typename T> __device__ __forceinline__ typename Vec<T>::type read_vec(
     return q;
 }
 
+// The N logits from element `at` on of a row of at least N, or its last ones; `first` receives the first one's index. Those
+// before `at` are replaced by -inf.
+template <typename T> __device__ __forceinline__ typename Vec<T>::type read_at(const T *x, int V, int at, int &first) {
+    first = std::min(at, V - Vec<T>::N);
+    typename Vec<T>::type q = *reinterpret_cast<const typename Vec<T>::unaligned *>(x + first);
+    if (first < at)
+#pragma unroll
+        for (int i = 0; i < Vec<T>::N; ++i)
+            q[i] = first + i < at ? T(-INFINITY) : q[i];
+    return q;
+}
+
 // A wave reads a part in kLoads loads of 64 vectors; the 16 lanes of a quarter hold a segment in kSame of them: one of
 // 2-byte logits, two of 4-byte ones.
 template <typename T> struct Part {
@@ -578,7 +634,7 @@ struct Digest {
     uint64_t *bins;    // [kSlices][kFine]
     unsigned *members; // [kSlices][kFine]
     uint64_t *kept;    // [kSlices / 2][kMostParts]: weights above the bin
-    uint64_t *list;    // [kSlices / 2][kList]: the bin's entries
+    uint64_t *list;    // [kSlices / 2][kMembers]: the bin's entries
     int parts;
 };
 
@@ -636,7 +692,8 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kList = 2048; // candidates
+constexpr int kList = 1024; // candidates of pick_kernel
+constexpr int kMembers = 2048; // of a bin
 constexpr int kFine = 1024; // bins
 
 // The token among the logits of one part, as far into the sum of its kept weights there as `ask` is in `of`.
@@ -675,10 +732,20 @@ __device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T
 constexpr int kPick = 256;
 using PickBlock = Block<kPick>;
 
+struct Weighed {
+    uint64_t entry, weight;
+};
+constexpr int kAhead = 8;
+
 struct PickShared {
-    uint64_t list[kList], weights[kList];
+    uint64_t list[kList];
+    union {
+        Weighed weighed[kPick + kAhead];
+        List<kPick>::Shared find;
+    };
+    uint32_t keys[kMostParts * kSegs]; // of the segments' largest logits; thread t has every kPick-th from t on
     uint16_t segs[kMostParts * kSegs];
-    unsigned count[kPick];
+    uint64_t bins[kPick];
     PickBlock::Shared block;
     uint64_t found_mass, found_left;
     float found_top;
@@ -687,12 +754,11 @@ struct PickShared {
 };
 
 // The number of segments whose largest logit has a key of at least k.
-template <int kKeys> __device__ __forceinline__ int segments_from(const uint32_t (&keys)[kKeys], int segs, uint32_t k, int step, PickShared &s) {
+__device__ __forceinline__ int segments_from(int segs, uint32_t k, int step, PickShared &s) {
     int n = 0;
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i)
-        if (i * kPick < segs)
-            n += __builtin_popcountll(__ballot(keys[i] >= k));
+    for (int i = threadIdx.x; i < segs; i += kPick)
+        n += s.keys[i] >= k;
+    n = int(wave_sum(uint64_t(n)));
     if (threadIdx.x % kWave == 0)
         s.ge[step & 1][threadIdx.x / kWave] = n;
     __syncthreads();
@@ -702,155 +768,126 @@ template <int kKeys> __device__ __forceinline__ int segments_from(const uint32_t
     return n;
 }
 
+// Calls f for s.weighed[0, n), of which there is room for kAhead more: that many are on their way from LDS at a time.
+template <typename F> __device__ __forceinline__ void for_entries(const PickShared &s, int n, F &&f) {
+    for (int i = 0; i < n; i += kAhead) {
+        Weighed o[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            o[k] = s.weighed[i + k];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k < n)
+                f(o[k]);
+    }
+}
+
 // The token from s.list[0, n), which holds every token down to some place of the order. `whole`: all that min_p and top_k
 // leave is among them; otherwise `total` is the weight of all that top_p is a share of. False where the list ends before the
 // last kept token does.
-//
-// Up to 256 entries, a thread each: every thread reads the others', in no order, and adds what comes before its own, which is
-// faster than sorting them (two times 36 dependent steps).
+__device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
+                                               PickShared &s) {
+    using L = List<kPick>;
+    uint64_t kept = 0, end = 0, unused;
+    for (int i = threadIdx.x; i < n; i += kPick)
+        kept += r.key_weight(key_in(s.list[i]));
+    kept = PickBlock::sum(kept, s.block);
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) { // top_k, then top_p of what it leaves
+        if (pass ? p.fraction == kOne : p.top_k >= n)
+            continue;
+        const uint64_t target = pass ? std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
+        if (pass && kept < target)
+            return false;
+        end = L::find<Order::kLogits>(pass, target, s.list, n, end, r, kept, s.find, s.block);
+    }
+    // sums are whole numbers: past the random share of them is to reach the next one
+    const uint64_t token = L::find<Order::kVocabulary>(true, share_down(kept, p.at) + 1, s.list, n, end, r, unused, s.find, s.block);
+    if (threadIdx.x == 0)
+        finish_row(a, row, r, index_of(token), float_of(key_in(token)), kept, total);
+    return true;
+}
+
+// The same of up to 256 entries, a thread each: every thread reads the others', in no order, and adds what comes before its own.
 __device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
                                               PickShared &s) {
     const int tid = threadIdx.x;
-    const uint64_t mine = tid < n ? s.list[tid] : 0;
-    const uint64_t w = tid < n ? r.key_weight(key_in(mine)) : 0;
-    if (tid < n)
-        s.weights[tid] = w;
-    __syncthreads();
+    const bool busy = tid - tid % kWave < n; // a lane of the wave has an entry
     bool keep = tid < n;
-    uint64_t before = 0;
-    int rank = 0;
+    const uint64_t mine = keep ? s.list[tid] : 0;
+    const uint64_t w = keep ? r.key_weight(key_in(mine)) : 0;
+    if (keep)
+        s.weighed[tid] = {mine, w};
+    if (tid == 0)
+        s.n = 0;
+    __syncthreads();
     if (p.top_k < n || p.fraction < kOne) {
-        if (keep)
-#pragma unroll 8
-            for (int i = 0; i < n; ++i) {
-                const bool ahead = s.list[i] > mine;
-                before += ahead ? s.weights[i] : 0;
-                rank += ahead;
-            }
+        uint64_t before = 0;
+        int rank = 0;
+        if (busy)
+            for_entries(s, n, [&](const Weighed &o) {
+                before += o.entry > mine ? o.weight : 0;
+                rank += o.entry > mine;
+            });
         keep = keep && rank < p.top_k;
-        uint64_t kept = PickBlock::sum(keep ? w : 0, s.block);
         if (p.fraction < kOne) {
-            const uint64_t target = std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1));
-            if (kept < target)
+            const uint64_t inside = PickBlock::sum(keep ? w : 0, s.block);
+            const uint64_t target = std::max(share_up(whole ? inside : total, p.fraction), uint64_t(1));
+            if (inside < target)
                 return false;
             keep = keep && before < target;
         }
     }
-    const uint64_t kept = PickBlock::sum(keep ? w : 0, s.block);
-    if (tid < n)
-        s.weights[tid] = keep ? w : 0;
-    __syncthreads();
-    before = 0;
+    const uint64_t kept = PickBlock::sum(keep ? w : 0, s.block), target = share_down(kept, p.at);
     if (keep)
-#pragma unroll 8
-        for (int i = 0; i < n; ++i)
-            before += uint32_t(s.list[i]) > uint32_t(mine) ? s.weights[i] : 0; // indices before this one's
-    const uint64_t target = share_down(kept, p.at);
+        s.weighed[atomicAdd(&s.n, 1)] = {mine, w};
+    __syncthreads();
+    uint64_t before = 0;
+    if (busy)
+        for_entries(s, s.n, [&](const Weighed &o) {
+            before += uint32_t(o.entry) > uint32_t(mine) ? o.weight : 0; // indices before this one's
+        });
     if (keep && before <= target && target < before + w)
         finish_row(a, row, r, index_of(mine), float_of(key_in(mine)), kept, total);
     return true;
 }
 
-__device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
-                                               PickShared &s) {
+// A key down to which the segments' largest logits are `target` at least (by_mass: have at least that weight), and not many
+// more: from bins of their distance from the largest of all, as far as weights reach, or, where one of those holds too many,
+// by halving. 0 where their weights are less than that.
+__device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, int segs, float m, const Row &r, PickShared &s) {
     const int tid = threadIdx.x;
-    int many = std::min(n, p.top_k), length = n;
-    uint64_t kept = 0;
-    // first in the order of the logits, for the last kept one, then in the order of the vocabulary, for the token
-#pragma unroll 1
-    for (int pass = 0;; ++pass) {
-        const int padded = power_of_two(length), share = std::max(padded / kPick, 1);
-        __syncthreads();
-        for (int i = length + tid; i < padded; i += kPick)
-            s.list[i] = 0;
-        sort_down<kPick>(s.list, padded);
-        const int from = tid * share, to = std::min(from + share, many);
-        uint64_t mine = 0, all;
-#pragma unroll 1
-        for (int i = from; i < to; ++i) {
-            const uint64_t e = s.list[i], w = r.key_weight(pass ? uint32_t(~e) : key_in(e));
-            s.weights[i] = w;
-            mine += w;
-        }
-        uint64_t sum = PickBlock::before(mine, all, s.block), target = 0;
-        if (pass)
-            target = share_down(kept, p.at) + 1; // sums are whole numbers: past it is to reach the next one
-        else {
-            kept = all;
-            if (p.fraction < kOne) {
-                target = std::max(share_up(whole ? all : total, p.fraction), uint64_t(1));
-                if (all < target)
-                    return false;
-            }
-        }
-        if (pass || p.fraction < kOne) {
-            if (sum < target && target <= sum + mine)
-#pragma unroll 1
-                for (int i = from; i < to; ++i) {
-                    sum += s.weights[i];
-                    if (sum >= target) {
-                        s.found = i + 1;
-                        s.found_mass = sum;
-                        break;
-                    }
-                }
-            __syncthreads();
-        }
-        if (pass) {
-            if (tid == 0) {
-                const uint64_t e = ~s.list[s.found - 1];
-                finish_row(a, row, r, int(e >> 32), float_of(uint32_t(e)), kept, total);
-            }
-            return true;
-        }
-        if (p.fraction < kOne) {
-            many = s.found;
-            kept = s.found_mass;
-        }
-        length = many;
-        for (int i = tid; i < many; i += kPick) {
-            const uint64_t e = s.list[i];
-            s.list[i] = ~(uint64_t(uint32_t(index_of(e))) << 32 | key_in(e));
-        }
-    }
-}
-
-// A key that the largest logits of at least `want` segments reach, and not many more: from a histogram of their distances
-// from the largest of all, as far as weights reach, or, where a bin of it holds too many, by halving.
-template <int kKeys>
-__device__ __forceinline__ uint32_t key_reached(const uint32_t (&keys)[kKeys], int segs, int want, float m, const Row &r, PickShared &s) {
-    const int tid = threadIdx.x, most = 2 * want + 64;
-    const float range = fminf(32.0f / float(r.scale), 64.0f); // of which bins of an even width are made
-    const float step = kPick / range;
+    const float step = kPick / fminf(32.0f / float(r.scale), 64.0f);
     __syncthreads();
-    s.count[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i)
-        if (i * kPick < segs) {
-            const float d = (m - float_of(keys[i])) * step;
-            if (d < float(kPick) && i * kPick + tid < segs)
-                atomicAdd(&s.count[int(d)], 1u);
-        }
-    __syncthreads();
-    const uint64_t mine = s.count[tid];
-    uint64_t all;
-    const uint64_t sum = PickBlock::before(mine, all, s.block);
+    s.bins[tid] = 0;
     if (tid == 0)
         s.found = -1;
     __syncthreads();
-    if (sum < uint64_t(want) && uint64_t(want) <= sum + mine && sum + mine <= uint64_t(most))
+#pragma unroll 1
+    for (int i = tid; i < segs; i += kPick) {
+        const float x = float_of(s.keys[i]), d = (m - x) * step;
+        if (d < float(kPick))
+            atomicAdd(reinterpret_cast<unsigned long long *>(&s.bins[int(d)]), by_mass ? (unsigned long long)r.weight(x) : 1ull);
+    }
+    __syncthreads();
+    const uint64_t mine = s.bins[tid];
+    uint64_t all;
+    const uint64_t sum = PickBlock::before(mine, all, s.block);
+    if (sum < target && target <= sum + mine && (by_mass || sum + mine <= 2 * target + 64))
         s.found = tid;
     __syncthreads();
-    uint32_t from = 0, to = key_of(m) + 1;
     if (s.found >= 0) {
         // a little below the bin's end, whatever the roundings on the way
         const float end = m - float(s.found + 1) / step;
         return key_of(end - 1e-6f * fmaxf(fabsf(end), fabsf(m)));
     }
+    if (by_mass)
+        return 0;
+    uint32_t from = 0, to = key_of(m) + 1;
+    const int want = int(target);
     for (int at = 0; to - from > 1; ++at) {
         const uint32_t k = from + (to - from) / 2;
-        const int n = segments_from(keys, segs, k, at, s);
+        const int n = segments_from(segs, k, at, s);
         if (n >= want)
             from = k;
         else
@@ -858,14 +895,13 @@ __device__ __forceinline__ uint32_t key_reached(const uint32_t (&keys)[kKeys], i
         if (n >= want && n <= want + want / 8 + 8)
             break;
     }
-    return from;
+    return std::max(from, key_of(-INFINITY));
 }
 
 // A workgroup takes a row.
 template <typename T>
-__global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3))) pick_kernel(const T *logits, Args a, Digest g) {
+__global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4))) pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ PickShared s;
-    constexpr int kKeys = kMostParts * kSegs / kPick;
     static_assert(kMostParts <= kPick, "a part a thread");
     const int tid = threadIdx.x, segs = g.parts * kSegs;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -873,6 +909,11 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
         const float top = tid < g.parts ? g.top[row * g.parts + tid] : -INFINITY;
         const double part_mass = tid < g.parts ? g.mass[row * g.parts + tid] : 0.0;
         const Params p = params_of(a, row);
+        const bool cut = p.top_k < a.V || p.fraction < kOne || p.least != -INFINITY;
+        if (cut)
+#pragma unroll 4
+            for (int i = tid; i < segs; i += kPick)
+                s.keys[i] = key_of(g.seg[row * segs + i]);
         const float m = PickBlock::max(top, s.block);
         if (p.scale == 0.0 || !(m < INFINITY) || m == -INFINITY) {
             finish_without(a, row, p.scale == 0.0 || m != -INFINITY);
@@ -883,7 +924,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
         const uint64_t mine = uint64_t(rint(part_mass * power_of(fmax(double(top) - r.m, r.far), r.c, 0)));
         uint64_t total;
         const uint64_t sum = PickBlock::before(mine, total, s.block);
-        if (p.top_k == a.V && p.fraction == kOne && p.least == -INFINITY) {
+        if (!cut) {
             const uint64_t target = share_down(total, p.at);
             if (sum <= target && target < sum + mine) {
                 s.found = tid;
@@ -897,22 +938,18 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             __syncthreads();
             continue;
         }
-        uint32_t keys[kKeys];
-#pragma unroll
-        for (int i = 0; i < kKeys; ++i)
-            keys[i] = i * kPick + tid < segs ? key_of(g.seg[row * segs + i * kPick + tid]) : 0;
         uint32_t low = floor_key(r.m, p.scale, p.least, key_of(m));
         const float least = low ? float_of(low) : -INFINITY;
-        int want = 0;
-        if (p.top_k < a.V)
-            want = p.top_k <= segs / 2 ? p.top_k : 0;
-        else if (low == 0)
-            want = std::min(segs / 2, 128);
-        bool wide = want == 0 && low == 0, whole = true;
-        if (want) {
-            const uint32_t from = key_reached(keys, segs, want, m, r, s);
-            whole = p.top_k < a.V || from <= low;
-            low = std::max(low, from);
+        bool wide = false, whole = true;
+        if (p.top_k < a.V) {
+            if (p.top_k <= segs / 2)
+                low = std::max(low, key_reached(false, uint64_t(p.top_k), segs, m, r, s));
+            else
+                wide = low == 0;
+        } else if (low == 0) {
+            low = key_reached(true, std::max(share_up(total, p.fraction), uint64_t(1)), segs, m, r, s);
+            whole = false;
+            wide = low == 0;
         }
         if (!wide) {
             // segments that have a candidate, and their candidates
@@ -920,26 +957,35 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             if (tid == 0)
                 s.found = s.n = 0;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kKeys; ++i)
-                if (i * kPick + tid < segs && keys[i] >= low)
-                    s.segs[atomicAdd(&s.found, 1)] = uint16_t(i * kPick + tid);
+            for (int i = tid; i < segs; i += kPick)
+                if (s.keys[i] >= low)
+                    s.segs[atomicAdd(&s.found, 1)] = uint16_t(i);
             __syncthreads();
             const int many = s.found;
-            for (int i = tid / 16; i < many; i += kPick / 16) {
-                const int seg = s.segs[i], quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
+            const float lowest = float_of(low);
+            // a quarter of a wave has four loads on their way at a time
+            for (int i = tid / 16; i < many; i += kPick / 16 * (4 / Part<T>::kSame)) {
+                typename Vec<T>::type q[4];
+                int at[4], first[4];
 #pragma unroll
-                for (int j = 0; j < Part<T>::kSame; ++j) {
-                    const int at = seg / kSegs * kPart + Part<T>::at(load + j, quarter * 16 + tid % 16);
-                    const typename Vec<T>::type q = read_vec(x + at, a.V - at);
+                for (int j = 0; j < 4; ++j) {
+                    const int k = i + j / Part<T>::kSame * (kPick / 16);
+                    const int seg = k < many ? s.segs[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
+                    at[j] = k < many ? seg / kSegs * kPart + Part<T>::at(load + j % Part<T>::kSame, quarter * 16 + tid % 16) : a.V;
+                    q[j] = read_at(x, a.V, at[j], first[j]);
+                }
 #pragma unroll
-                    for (int k = 0; k < Part<T>::N; ++k) {
-                        const uint32_t key = key_of(float(q[k]));
-                        if (key >= low && at + k < a.V) {
-                            const int to = atomicAdd(&s.n, 1);
-                            if (to < kList)
-                                s.list[to] = entry_of(key, at + k);
-                        }
+                for (int j = 0; j < 4; ++j) {
+                    unsigned hits = 0;
+#pragma unroll
+                    for (int k = 0; k < Part<T>::N; ++k)
+                        hits |= float(q[j][k]) >= lowest ? 1u << k : 0;
+                    hits &= ~0u << (at[j] - first[j]);
+                    while (hits) {
+                        const int k = __builtin_ctz(hits), to = atomicAdd(&s.n, 1);
+                        hits &= hits - 1;
+                        if (to < kList)
+                            s.list[to] = entry_of(key_of(float(x[first[j] + k])), first[j] + k);
                     }
                 }
             }
@@ -975,9 +1021,10 @@ __device__ __forceinline__ int shares_of(unsigned wide, int parts) {
 struct WideShared {
     uint64_t mass[kFine];
     uint32_t count[kFine];
-    uint64_t list[kList];
+    uint64_t list[kMembers];
     uint64_t kept[kMostParts];
     WideBlock::Shared block;
+    List<kWide>::Shared find;
     uint64_t found_mass, found_left;
     int found, n;
     bool last;
@@ -995,15 +1042,24 @@ struct Bins {
     }
 };
 
-// Calls f(logit, index) for a share of a row's vectors.
+// Calls f(logit, index) for a share of a row's vectors, some of the last of them twice, with -inf.
 template <typename T, typename F> __device__ __forceinline__ void for_share(const T *x, int V, int share, int shares, F &&f) {
     constexpr int N = Vec<T>::N;
     const int vecs = (V + N - 1) / N, each = (vecs + shares - 1) / shares, end = std::min(vecs, (share + 1) * each);
-    for (int i = share * each + int(threadIdx.x); i < end; i += kWide) {
-        const typename Vec<T>::type q = read_vec(x + i * N, V - i * N);
+    constexpr int kLoads = 4; // on their way at a time
+    for (int i = share * each + int(threadIdx.x); i < end; i += kLoads * kWide) {
+        typename Vec<T>::type q[kLoads];
+        int first[kLoads];
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            f(float(q[k]), i * N + k);
+        for (int j = 0; j < kLoads; ++j)
+            if (i + j * kWide < end)
+                q[j] = read_at(x, V, (i + j * kWide) * N, first[j]);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            if (i + j * kWide < end)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    f(float(q[j][k]), first[j] + k);
     }
 }
 
@@ -1056,41 +1112,6 @@ __device__ __forceinline__ int bin_of(bool by_mass, uint64_t target, uint64_t &l
     return s.found;
 }
 
-// Sorts the n entries of a bin and finds the one at which their count (by_mass: their weights) reaches `left`; `inside`
-// receives the weights down to it.
-__device__ __forceinline__ int place_in_list(bool by_mass, uint64_t left, int n, const Row &r, uint64_t &inside, WideShared &s) {
-    const int padded = power_of_two(n), share = std::max(padded / kWide, 1), tid = threadIdx.x;
-    __syncthreads();
-    for (int i = n + tid; i < padded; i += kWide)
-        s.list[i] = 0;
-    sort_down<kWide>(s.list, padded);
-    const int from = tid * share, to = std::min(from + share, n);
-    uint64_t mine = 0, mine_mass = 0, all;
-#pragma unroll 1
-    for (int i = from; i < to; ++i) {
-        const uint64_t w = r.key_weight(key_in(s.list[i]));
-        mine += by_mass ? w : 1;
-        mine_mass += w;
-    }
-    uint64_t sum = WideBlock::before(mine, all, s.block);
-    uint64_t sum_mass = WideBlock::before(mine_mass, all, s.block);
-    if (sum < left && left <= sum + mine)
-#pragma unroll 1
-        for (int i = from; i < to; ++i) {
-            const uint64_t w = r.key_weight(key_in(s.list[i]));
-            sum += by_mass ? w : 1;
-            sum_mass += w;
-            if (sum >= left) {
-                s.found = i;
-                s.found_mass = sum_mass;
-                break;
-            }
-        }
-    __syncthreads();
-    inside = s.found_mass;
-    return s.found;
-}
-
 // Whether this workgroup is the last of `shares` to come here; what the others wrote before is then seen.
 __device__ __forceinline__ bool is_last(unsigned *arrived, int shares, WideShared &s) {
     if (shares == 1)
@@ -1138,15 +1159,25 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 }
                 if (!is_last(&w.arrived[0], shares, s))
                     continue;
-                for (int i = tid; i < kFine; i += kWide) {
-                    uint64_t mass = 0;
-                    uint32_t count = 0;
+                {
+                    static_assert(kFine == 2 * kWide, "two bins a thread");
+                    uint64_t mass[2] = {0, 0};
+                    uint32_t count[2] = {0, 0};
+#pragma unroll 8
                     for (int k = 0; k < shares; ++k) {
-                        mass += g.bins[(slot * shares + k) * kFine + i];
-                        count += g.members[(slot * shares + k) * kFine + i];
+                        const int64_t at = (slot * shares + k) * kFine + 2 * tid;
+                        const ulonglong2 m = *reinterpret_cast<const ulonglong2 *>(g.bins + at);
+                        const uint2 c = *reinterpret_cast<const uint2 *>(g.members + at);
+                        mass[0] += m.x;
+                        mass[1] += m.y;
+                        count[0] += c.x;
+                        count[1] += c.y;
                     }
-                    s.mass[i] = mass;
-                    s.count[i] = count;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        s.mass[2 * tid + i] = mass[i];
+                        s.count[2 * tid + i] = count[i];
+                    }
                 }
                 __syncthreads();
             }
@@ -1163,7 +1194,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 members = int(s.count[bin]);
             }
             if (cut && p.fraction < kOne) { // what top_p is a share of has to be known
-                if (members > kList)
+                if (members > kMembers)
                     last = WideBlock::place_of<false>(x, a.V, r, least, uint64_t(p.top_k), inside, s.mass, s.count, s.block);
                 else {
                     __syncthreads();
@@ -1175,11 +1206,11 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                             s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), i);
                     });
                     __syncthreads();
-                    place_in_list(false, left, members, r, inside, s);
+                    List<kWide>::find<Order::kLogits>(false, left, s.list, members, 0, r, inside, s.find, s.block);
                     inside += above;
                     __syncthreads();
                 }
-                if (members > kList)
+                if (members > kMembers)
                     fill_bins(x, a.V, 0, 1, r, bins, least, s);
             }
             if (p.fraction < kOne) {
@@ -1187,7 +1218,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 bin = bin_of(true, std::max(share_up(inside, p.fraction), uint64_t(1)), left, above, s);
                 members = int(s.count[bin]);
             }
-            if (members > kList) { // a great many near equals
+            if (members > kMembers) { // a great many near equals
                 __syncthreads();
                 const uint64_t target = by_mass ? std::max(share_up(inside, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
                 uint64_t unused;
@@ -1230,33 +1261,40 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
         const int bin = w.bin;
         const bool exact = bin == kFine;
         const Last last(w.last);
-        uint64_t *list = shares > 1 ? g.list + slot * kList : s.list;
-        uint64_t *kept_of = shares > 1 ? g.kept + slot * kMostParts : s.kept;
+        uint64_t *list = g.list + slot * kMembers, *kept_of = g.kept + slot * kMostParts; // where the row is shared
         if (tid == 0)
             s.n = 0;
         __syncthreads();
         for (int part = int(item - slot * shares) + wave * shares; part < g.parts; part += shares * WideBlock::kWaves) {
             uint64_t mass = 0;
-#pragma unroll 1
-            for (int j = 0; j < P::kLoads; ++j) {
-                const int at = part * kPart + P::at(j, lane);
-                const typename Vec<T>::type q = read_vec(x + at, a.V - at);
+            typename Vec<T>::type q[P::kLoads];
+            int at[P::kLoads];
+#pragma unroll
+            for (int j = 0; j < P::kLoads; ++j)
+                q[j] = read_at(x, a.V, part * kPart + P::at(j, lane), at[j]);
+#pragma unroll
+            for (int j = 0; j < P::kLoads; ++j)
 #pragma unroll
                 for (int k = 0; k < P::N; ++k) {
-                    const float v = float(q[k]);
+                    const float v = float(q[j][k]);
                     const int mine = bins.of(v);
                     const bool in = v >= least;
-                    if (exact ? last.keeps(v, at + k) : in && mine < bin)
+                    if (exact ? last.keeps(v, at[j] + k) : in && mine < bin)
                         mass += r.weight(v);
-                    if (!exact && in && mine == bin) {
-                        const int to = shares > 1 ? int(atomicAdd(&w.listed, 1u)) : atomicAdd(&s.n, 1);
-                        list[to] = entry_of(key_of(v), at + k);
-                    }
+                    if (!exact && in && mine == bin)
+                        s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), at[j] + k);
                 }
-            }
             mass = wave_sum(mass);
             if (lane == 0)
-                kept_of[part] = mass;
+                (shares > 1 ? kept_of : s.kept)[part] = mass;
+        }
+        if (shares > 1) {
+            __syncthreads();
+            if (tid == 0)
+                s.found = int(atomicAdd(&w.listed, unsigned(s.n)));
+            __syncthreads();
+            for (int i = tid; i < s.n; i += kWide)
+                list[s.found + i] = s.list[i];
         }
         if (!is_last(&w.arrived[1], shares, s))
             continue;
@@ -1270,10 +1308,11 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 for (int i = tid; i < n; i += kWide)
                     s.list[i] = list[i];
             uint64_t unused;
-            const int at = place_in_list(w.by_mass, w.left, n, r, unused, s);
-            end = s.list[at];
-            for (int i = tid; i <= at; i += kWide)
-                atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(s.list[i]) / kPart]), (unsigned long long)r.key_weight(key_in(s.list[i])));
+            __syncthreads();
+            end = List<kWide>::find<Order::kLogits>(w.by_mass, w.left, s.list, n, 0, r, unused, s.find, s.block);
+            for (int i = tid; i < n; i += kWide)
+                if (s.list[i] >= end)
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(s.list[i]) / kPart]), (unsigned long long)r.key_weight(key_in(s.list[i])));
         }
         __syncthreads();
         uint64_t kept;
@@ -1413,7 +1452,7 @@ int64_t lay_out(const Plan &p, int64_t n, char *at, Digest &g) {
     g.bins = s.take<uint64_t>(slices * kFine);
     g.members = s.take<unsigned>(slices * kFine);
     g.kept = s.take<uint64_t>(slots * kMostParts);
-    g.list = s.take<uint64_t>(slots * kList);
+    g.list = s.take<uint64_t>(slots * kMembers);
     return s.bytes;
 }
 
