@@ -7,9 +7,11 @@ first call raises ``TreeEnsLibraryMissing`` (build it with ``__graft_entry__.bui
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import re
+from operator import attrgetter
 from typing import Optional
 
 import numpy as np
@@ -32,6 +34,8 @@ TREE_ENS_CODEGEN = 2  # also compile a kernel specialised for the model (hiprtc)
 TREE_ENS_F32, TREE_ENS_BF16, TREE_ENS_F16 = range(3)  # types of logits
 TREE_ENS_SEQ_MEAN = 1  # a sequence counts with the mean over its tokens, not the sum
 TREE_ENS_CENTER_ONLY = 2  # advantages are not divided by the standard deviation
+
+_dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 
 _CODE_NAMES = {0: "OK", -1: "E_ARG", -2: "E_MODEL", -3: "E_SHAPE", -4: "E_DEVICE", -5: "E_NOMEM"}
 
@@ -673,27 +677,33 @@ def _dense(t) -> bool:
     return True
 
 
-def _check_grads(grads):
-    """(device, addresses, counts and dtype codes as C arrays) of a sequence of dense device tensors."""
+def _check_grads(grads, name="grads"):
+    """(device, tensors, their addresses, counts and dtype codes in arrays) of a sequence of dense device tensors. One
+    reading of all tensors for each of their properties costs a third of a loop over them."""
     import torch
     grads = list(grads)
-    if not grads or not all(isinstance(t, torch.Tensor) for t in grads):
-        raise TypeError("grads must be a sequence of one tensor or more")
-    dev, codes = grads[0].device, _dtype_codes()
-    if dev.type != "cuda" or any(t.device != dev for t in grads):
-        raise TypeError("grads must be CUDA (HIP) tensors of one device")
-    if not all(t.dtype in codes for t in grads) or not all(_dense(t) for t in grads):
-        raise TypeError("grads must be float32, bfloat16 or float16 tensors without gaps between their elements")
-    n = len(grads)
-    return dev, grads, ((ctypes.c_void_p * n)(*[t.data_ptr() for t in grads]), (ctypes.c_int64 * n)(*[t.numel() for t in grads]),
-                        (ctypes.c_int32 * n)(*[codes[t.dtype] for t in grads]))
+    if not grads or not all(issubclass(kind, torch.Tensor) for kind in set(map(type, grads))):
+        raise TypeError(f"{name} must be a sequence of one tensor or more")
+    Tensor, codes = torch.Tensor, _dtype_codes()
+    dtypes = list(map(_dtype_of, grads))
+    kinds = set(dtypes)
+    if not kinds <= codes.keys() or not (all(map(Tensor.is_contiguous, grads)) or all(map(_dense, grads))):
+        raise TypeError(f"{name} must be float32, bfloat16 or float16 tensors without gaps between their elements")
+    if not grads[0].is_cuda or len(set(map(Tensor.get_device, grads))) != 1:
+        raise TypeError(f"{name} must be CUDA (HIP) tensors of one device")
+    kinds = array.array("i", map(codes.__getitem__, dtypes) if len(kinds) > 1 else [codes[dtypes[0]]] * len(grads))
+    return grads[0].device, grads, array.array("q", map(Tensor.data_ptr, grads)), array.array("q", map(Tensor.numel, grads)), kinds
+
+
+def _address(values):
+    return values.buffer_info()[0]
 
 
 def tree_ens_grad_norm(grads, norm=None, stream=None):
     """The 2-norm of the elements of all tensors of ``grads`` together, such as ``[p.grad for p in parameters]``: a float32
     scalar on their device (``norm``, if given). Types may be mixed; tensors are dense, in any order of their dimensions."""
     import torch
-    dev, grads, (ptrs, counts, codes) = _check_grads(grads)
+    dev, grads, ptrs, counts, codes = _check_grads(grads)
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
         with elsewhere:
@@ -704,8 +714,8 @@ def tree_ens_grad_norm(grads, norm=None, stream=None):
         _check_norm(norm, dev)
     lib = load_library()
     _keep, work, size = _workspace(lib, dev, "tree_ens_grad_norm_workspace", len(grads))
-    _check(lib.tree_ens_grad_norm(_stream_on(dev), len(grads), ptrs, counts, codes, norm.data_ptr(), work, size),
-           "tree_ens_grad_norm")
+    _check(lib.tree_ens_grad_norm(_stream_on(dev), len(grads), _address(ptrs), _address(counts), _address(codes),
+           norm.data_ptr(), work, size), "tree_ens_grad_norm")
     return norm
 
 
@@ -719,23 +729,22 @@ def tree_ens_grad_clip(grads, norm, max_norm: float, eps: float = 1e-6, out=None
     """``grads`` times min(1, max_norm / (norm + eps)), each rounded once to its type, in place or into the tensors of
     ``out`` (of the same shapes, strides and types; they may be some of the same tensors): the tensors written. ``norm`` as
     tree_ens_grad_norm gives it, or over all processes' shards."""
-    dev, grads, (ptrs, counts, codes) = _check_grads(grads)
+    dev, grads, ptrs, counts, codes = _check_grads(grads)
     _check_norm(norm, dev)
-    out = grads if out is None else list(out)
-    if len(out) != len(grads):
-        raise TypeError(f"out must hold {len(grads)} tensors, not {len(out)}")
     to = ptrs
-    if out is not grads:
-        if any(o.shape != t.shape or o.dtype != t.dtype or o.device != dev or (o.stride() != t.stride() and t.numel() > 1)
-               for o, t in zip(out, grads)):
+    if out is None:
+        out = grads
+    else:
+        out_dev, out, to, _, out_codes = _check_grads(out, "out")
+        if out_dev != dev or out_codes != codes or list(map(_shape_of, out)) != list(map(_shape_of, grads)) or \
+                any(a.stride() != b.stride() for a, b in zip(out, grads) if not (a.is_contiguous() and b.is_contiguous())):
             raise TypeError("out must hold tensors of the gradients' shapes, strides, types and device")
-        to = (ctypes.c_void_p * len(out))(*[o.data_ptr() for o in out])
     elsewhere = _elsewhere(dev, stream)
     if elsewhere is not None:
         with elsewhere:
             return tree_ens_grad_clip(grads, norm, max_norm, eps, out)
-    _check(load_library().tree_ens_grad_clip(_stream_on(dev), len(grads), ptrs, counts, codes, norm.data_ptr(), float(max_norm),
-           float(eps), to), "tree_ens_grad_clip")
+    _check(load_library().tree_ens_grad_clip(_stream_on(dev), len(grads), _address(ptrs), _address(counts), _address(codes),
+           norm.data_ptr(), float(max_norm), float(eps), _address(to)), "tree_ens_grad_clip")
     return out
 
 

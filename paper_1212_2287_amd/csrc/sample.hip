@@ -78,10 +78,16 @@ __device__ __forceinline__ int top_k_of(const Args &a, int64_t row) {
 }
 __device__ __forceinline__ float min_p_of(const Args &a, int64_t row) { return a.row_min_p ? a.row_min_p[row] : a.min_p; }
 
-// Whether the weights of a whole row are asked for: for its log-probabilities, or because nothing but top_p, or nothing
-// at all, cuts it off.
-__device__ __forceinline__ bool needs_mass(const Args &a, int64_t row) {
-    return a.logp || a.log_kept || (top_k_of(a, row) == a.V && !(min_p_of(a, row) > 0.0f));
+__device__ __forceinline__ bool wants_logp(const Args &a) { return a.logp || a.log_kept; }
+
+// What the weights of a whole row are for: they decide on tokens where nothing but top_p, or nothing at all, cuts it off, and are
+// exact then; otherwise log-probabilities ask for what is not kept, for which single precision does.
+enum class Mass { kNone, kExact, kQuick };
+__device__ __forceinline__ Mass mass_of(const Args &a, int64_t row) {
+    if (top_k_of(a, row) == a.V && !(min_p_of(a, row) > 0.0f))
+        return Mass::kExact;
+    // below this scale a distance that is no float could have a weight
+    return !wants_logp(a) ? Mass::kNone : scale_of(a, row) < 0x1p-100 ? Mass::kExact : Mass::kQuick;
 }
 
 __device__ __forceinline__ Params params_of(const Args &a, int64_t row) {
@@ -143,6 +149,16 @@ __device__ __forceinline__ uint32_t floor_key(double m, double scale, double lea
         return 0;
     uint32_t low = key_of(-INFINITY); // not enough (the difference from a float's is never 0), `top` is
     const int lane = threadIdx.x % kWave;
+    // within a few roundings of m + least / scale, as a rule
+    const uint32_t near = key_of(fmaxf(float(m + least * __builtin_amdgcn_rcp(scale)), -3e38f));
+    if (near - low > kWave && near + kWave < top) {
+        const uint64_t yes = __ballot((double(float_of(near - kWave / 2 + lane)) - m) * scale >= least);
+        const int first = yes ? __builtin_ctzll(yes) : kWave;
+        if (first < kWave)
+            top = near - kWave / 2 + first;
+        if (first > 0)
+            low = near - kWave / 2 + first - 1;
+    }
     while (top - low > 1) {
         const uint64_t span = top - low;
         const uint32_t k = low + uint32_t(span * uint64_t(lane + 1) / (kWave + 1));
@@ -223,18 +239,46 @@ struct Row {
         : m(double(top)), scale(scale_), c(scale_ * kLog2e), far(-64.0 * __builtin_amdgcn_rcp(scale_)), shift(shift_) {}
     // The weight in units, not rounded. Masked logits are taken at `far`, where it is less than half of one.
     __device__ __forceinline__ double power(float x) const { return power_of(fmax(double(x) - m, far), c, shift); }
+    __device__ __forceinline__ double share(float x) const { return power_of(fmax(double(x) - m, far), c, 0); } // of the largest
     __device__ __forceinline__ uint64_t weight(float x) const { return whole_of(power(x)); }
     __device__ __forceinline__ uint64_t key_weight(uint32_t k) const { return weight(float_of(k)); }
 };
 
-// The token's log-probability and the logarithm of the kept share, which is 0 exactly where everything is kept.
-__device__ __forceinline__ void finish_row(const Args &a, int64_t row, const Row &r, int token, float x, uint64_t kept, uint64_t total) {
+// A sum of weights of at most 1, in whole numbers of 2^-51 for those of 2^-28 and more and of 2^-79 for others: exact in any order,
+// and in proportion to itself, as what is not kept has to be.
+struct Fine {
+    uint64_t high = 0, low = 0;
+    __device__ __forceinline__ void add(double w) {
+        high += w >= 0x1p-28 ? whole_of(w * 0x1p51) : 0;
+        low += w >= 0x1p-28 ? 0 : whole_of(w * 0x1p79);
+    }
+    __device__ __forceinline__ double units(int shift) const { return ldexp(double(high), shift - 51) + ldexp(double(low), shift - 79); }
+};
+
+// Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts.
+struct Quick {
+    float m, c, rest;
+    __device__ __forceinline__ Quick(float top, double scale) : m(top) {
+        const double exact = scale * kLog2e;
+        c = float(fmin(exact, 3.402823466e38));
+        rest = float(exact - double(c));
+        rest = exact > 3.402823466e38 ? 0.0f : rest;
+    }
+    __device__ __forceinline__ float power(float x) const {
+        const float d = fmaxf(x - m, -3.402823466e38f); // masked logits too: times 0 they would be NaN
+        return __builtin_amdgcn_exp2f(fmaf(d, c, d * rest));
+    }
+};
+
+// The token, its log-probability, and the logarithm of the kept share from the weights kept and not kept (in units): the
+// latter by itself, however small it is, and 0 exactly where there is nothing of it.
+__device__ __forceinline__ void finish_row(const Args &a, int64_t row, const Row &r, int token, float x, double kept, double dropped) {
     a.tokens[row] = token;
     if (a.logp)
-        a.logp[row] = float((double(x) - r.m) * r.scale - log_of(double(total)) + r.shift * 0.6931471805599453);
+        a.logp[row] = float((double(x) - r.m) * r.scale - log_of(kept + dropped) + r.shift * 0.6931471805599453);
     if (a.log_kept) {
-        const double dropped = total > kept ? double(total - kept) / double(total) : 0.0;
-        a.log_kept[row] = float(dropped < 0x1p-16 ? -fma(dropped, fma(dropped, 1.0 / 3, 0.5) * dropped, dropped) : log_of(1.0 - dropped));
+        const double d = dropped / (kept + dropped);
+        a.log_kept[row] = float(d < 0x1p-16 ? -fma(d, fma(d, 1.0 / 3, 0.5) * d, d) : log_of(1.0 - d));
     }
 }
 __device__ __forceinline__ void finish_without(const Args &a, int64_t row, bool bad) {
@@ -263,6 +307,7 @@ template <int kT> struct Block {
     static constexpr int kWaves = kT / kWave;
     struct Shared {
         uint64_t part[kWaves];
+        double real[kWaves];
         float max[kWaves];
         uint64_t left;
         uint32_t digit;
@@ -280,6 +325,20 @@ template <int kT> struct Block {
         v = 0;
         for (int w = 0; w < kWaves; ++w)
             v += s.part[w];
+        return v;
+    }
+    static __device__ __forceinline__ Fine sum(Fine v, Shared &s) { return {sum(v.high, s), sum(v.low, s)}; }
+    static __device__ __forceinline__ double sum(double v, Shared &s) {
+        v = wave_sum(v);
+        if constexpr (kWaves == 1)
+            return v;
+        __syncthreads();
+        if (threadIdx.x % kWave == 0)
+            s.real[threadIdx.x / kWave] = v;
+        __syncthreads();
+        v = 0.0;
+        for (int w = 0; w < kWaves; ++w)
+            v += s.real[w];
         return v;
     }
 
@@ -501,13 +560,10 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
         }
         const Row r(m, p.scale, a.shift);
         const uint32_t floor = floor_key(r.m, p.scale, p.least, key_of(m));
-        uint64_t w[kOwn], total = 0;
+        uint64_t w[kOwn];
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
+        for (int i = 0; i < kOwn; ++i)
             w[i] = i < each && from + i < a.V ? r.weight(v[i]) : 0;
-            total += w[i];
-        }
-        total = B::sum(total, s);
         uint64_t lowest = entry_of(floor, -1); // entries from here on are kept
         if (p.top_k < a.V || p.fraction < kOne) {
             __syncthreads();
@@ -530,12 +586,18 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
                 lowest = L::template find<Order::kLogits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, r, unused, find, s);
         }
         uint64_t mine = 0;
+        double lost = 0.0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            if (entry_of(key_of(v[i]), from + i) < lowest)
+            if (entry_of(key_of(v[i]), from + i) < lowest) {
                 w[i] = 0;
+                if (wants_logp(a) && v[i] > -INFINITY)
+                    lost += r.power(v[i]);
+            }
             mine += w[i];
         }
+        if (wants_logp(a) && lowest)
+            lost = B::sum(lost, s);
         uint64_t kept;
         uint64_t sum = B::before(mine, kept, s);
         const uint64_t target = share_down(kept, p.at);
@@ -551,7 +613,7 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
                 sum += w[i];
             }
         if (token >= 0)
-            finish_row(a, row, r, token, at, kept, total);
+            finish_row(a, row, r, token, at, double(kept), lost);
     }
 }
 
@@ -615,7 +677,6 @@ template <typename T> struct Part {
 struct WideRow {
     int64_t row;
     float top, least;
-    uint64_t total;
     uint64_t last;  // the entry of the last kept token, where `bin` is kFine
     uint64_t left;  // otherwise it is in this bin, where the count (by_mass: the weights) reaches this
     int bin, members;
@@ -634,6 +695,7 @@ struct Digest {
     uint64_t *bins;    // [kSlices][kFine]
     unsigned *members; // [kSlices][kFine]
     uint64_t *kept;    // [kSlices / 2][kMostParts]: weights above the bin
+    double *lost;      // [kSlices / 2][kMostParts]: and below it
     uint64_t *list;    // [kSlices / 2][kMembers]: the bin's entries
     int parts;
 };
@@ -675,11 +737,20 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
             g.seg[item * kSegs + lane % 16 * 4 + lane / 16] = mine;
         double mass = 0.0;
         const double scale = scale_of(a, row);
-        if (needs_mass(a, row) && scale != 0.0 && m < INFINITY && m > -INFINITY) {
-            const Row r(m, scale, a.shift);
+        const Mass kind = mass_of(a, row);
+        if (kind != Mass::kNone && scale != 0.0 && m < INFINITY && m > -INFINITY) {
+            if (kind == Mass::kExact) {
+                const Row r(m, scale, a.shift);
 #pragma unroll
-            for (int k = 0; k < kN; ++k)
-                mass += r.power(v[k]);
+                for (int k = 0; k < kN; ++k)
+                    mass += r.power(v[k]);
+            } else {
+                const Quick w(m, scale);
+#pragma unroll
+                for (int k = 0; k < kN; ++k)
+                    mass += double(w.power(v[k]));
+                mass = ldexp(mass, a.shift);
+            }
             mass = wave_sum(mass);
         }
         if (lane == 0) {
@@ -699,7 +770,7 @@ constexpr int kFine = 1024; // bins
 // The token among the logits of one part, as far into the sum of its kept weights there as `ask` is in `of`.
 template <typename T, int kT>
 __device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T *x, int part, const Row &own, const Row &r, Last last,
-                                             uint64_t ask, uint64_t of, uint64_t kept, uint64_t total, typename Block<kT>::Shared &s) {
+                                             uint64_t ask, uint64_t of, uint64_t kept, double dropped, typename Block<kT>::Shared &s) {
     constexpr int kEach = kPart / kT;
     const int from = part * kPart + threadIdx.x * kEach;
     float v[kEach];
@@ -726,10 +797,10 @@ __device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T
             sum += w[i];
         }
     if (token >= 0)
-        finish_row(a, row, r, token, at, kept, total);
+        finish_row(a, row, r, token, at, double(kept), dropped);
 }
 
-constexpr int kPick = 256;
+constexpr int kPick = 256, kFew = 256;
 using PickBlock = Block<kPick>;
 
 struct Weighed {
@@ -740,24 +811,27 @@ constexpr int kAhead = 8;
 struct PickShared {
     uint64_t list[kList];
     union {
-        Weighed weighed[kPick + kAhead];
+        Weighed weighed[kFew + kAhead];
         List<kPick>::Shared find;
     };
-    uint32_t keys[kMostParts * kSegs]; // of the segments' largest logits; thread t has every kPick-th from t on
-    uint16_t segs[kMostParts * kSegs];
     uint64_t bins[kPick];
+    float tops[kPick];      // of the parts
+    uint64_t listed[kPick]; // weights of a part's tokens in the list, in 2^-51 of its largest
     PickBlock::Shared block;
     uint64_t found_mass, found_left;
     float found_top;
     int found, n;
     int ge[2][PickBlock::kWaves];
 };
+// Behind it in LDS, for as many segments as there are: the keys of their largest logits, of which thread t has every kPick-th
+// from t on, and a list of some of the segments.
+constexpr int kSegBytes = kSegs * int(sizeof(uint32_t) + sizeof(uint16_t)); // of a part
 
 // The number of segments whose largest logit has a key of at least k.
-__device__ __forceinline__ int segments_from(int segs, uint32_t k, int step, PickShared &s) {
+__device__ __forceinline__ int segments_from(const uint32_t *keys, int segs, uint32_t k, int step, PickShared &s) {
     int n = 0;
     for (int i = threadIdx.x; i < segs; i += kPick)
-        n += s.keys[i] >= k;
+        n += keys[i] >= k;
     n = int(wave_sum(uint64_t(n)));
     if (threadIdx.x % kWave == 0)
         s.ge[step & 1][threadIdx.x / kWave] = n;
@@ -783,10 +857,10 @@ template <typename F> __device__ __forceinline__ void for_entries(const PickShar
 }
 
 // The token from s.list[0, n), which holds every token down to some place of the order. `whole`: all that min_p and top_k
-// leave is among them; otherwise `total` is the weight of all that top_p is a share of. False where the list ends before the
-// last kept token does.
+// leave is among them; otherwise `total` is the weight of all that top_p is a share of. `rest`: the weights of the tokens
+// beyond the list. False where the list ends before the last kept token does.
 __device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
-                                               PickShared &s) {
+                                               double rest, PickShared &s) {
     using L = List<kPick>;
     uint64_t kept = 0, end = 0, unused;
     for (int i = threadIdx.x; i < n; i += kPick)
@@ -801,17 +875,35 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const
             return false;
         end = L::find<Order::kLogits>(pass, target, s.list, n, end, r, kept, s.find, s.block);
     }
+    Fine lost;
+    if (wants_logp(a) && end) {
+        for (int i = threadIdx.x; i < n; i += kPick)
+            if (s.list[i] < end)
+                lost.add(r.share(float_of(key_in(s.list[i]))));
+        lost = PickBlock::sum(lost, s.block);
+    }
     // sums are whole numbers: past the random share of them is to reach the next one
     const uint64_t token = L::find<Order::kVocabulary>(true, share_down(kept, p.at) + 1, s.list, n, end, r, unused, s.find, s.block);
     if (threadIdx.x == 0)
-        finish_row(a, row, r, index_of(token), float_of(key_in(token)), kept, total);
+        finish_row(a, row, r, index_of(token), float_of(key_in(token)), double(kept), rest + lost.units(r.shift));
     return true;
 }
 
-// The same of up to 256 entries, a thread each: every thread reads the others', in no order, and adds what comes before its own.
+// The same of up to kT entries, by the first kT threads, one each: every thread reads the others', in no order, and adds what comes
+// before its own. A wave needs no barriers for it.
+template <int kT>
 __device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
-                                              PickShared &s) {
+                                              double rest, PickShared &s) {
     const int tid = threadIdx.x;
+    typename Block<kT>::Shared &block = reinterpret_cast<typename Block<kT>::Shared &>(s.block);
+    const auto wait = [] {
+        if constexpr (kT > kWave)
+            __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
     const bool busy = tid - tid % kWave < n; // a lane of the wave has an entry
     bool keep = tid < n;
     const uint64_t mine = keep ? s.list[tid] : 0;
@@ -820,7 +912,7 @@ __device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const 
         s.weighed[tid] = {mine, w};
     if (tid == 0)
         s.n = 0;
-    __syncthreads();
+    wait();
     if (p.top_k < n || p.fraction < kOne) {
         uint64_t before = 0;
         int rank = 0;
@@ -831,31 +923,38 @@ __device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const 
             });
         keep = keep && rank < p.top_k;
         if (p.fraction < kOne) {
-            const uint64_t inside = PickBlock::sum(keep ? w : 0, s.block);
+            const uint64_t inside = Block<kT>::sum(keep ? w : 0, block);
             const uint64_t target = std::max(share_up(whole ? inside : total, p.fraction), uint64_t(1));
             if (inside < target)
                 return false;
             keep = keep && before < target;
         }
     }
-    const uint64_t kept = PickBlock::sum(keep ? w : 0, s.block), target = share_down(kept, p.at);
+    const uint64_t kept = Block<kT>::sum(keep ? w : 0, block), target = share_down(kept, p.at);
+    Fine lost;
+    if (wants_logp(a)) {
+        if (tid < n && !keep)
+            lost.add(r.share(float_of(key_in(mine))));
+        lost = Block<kT>::sum(lost, block);
+    }
     if (keep)
         s.weighed[atomicAdd(&s.n, 1)] = {mine, w};
-    __syncthreads();
+    wait();
     uint64_t before = 0;
     if (busy)
         for_entries(s, s.n, [&](const Weighed &o) {
             before += uint32_t(o.entry) > uint32_t(mine) ? o.weight : 0; // indices before this one's
         });
     if (keep && before <= target && target < before + w)
-        finish_row(a, row, r, index_of(mine), float_of(key_in(mine)), kept, total);
+        finish_row(a, row, r, index_of(mine), float_of(key_in(mine)), double(kept), rest + lost.units(r.shift));
     return true;
 }
 
 // A key down to which the segments' largest logits are `target` at least (by_mass: have at least that weight), and not many
 // more: from bins of their distance from the largest of all, as far as weights reach, or, where one of those holds too many,
 // by halving. 0 where their weights are less than that.
-__device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, int segs, float m, const Row &r, PickShared &s) {
+__device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, const uint32_t *keys, int segs, float m, const Row &r,
+                                                PickShared &s) {
     const int tid = threadIdx.x;
     const float step = kPick / fminf(32.0f / float(r.scale), 64.0f);
     __syncthreads();
@@ -865,7 +964,7 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, i
     __syncthreads();
 #pragma unroll 1
     for (int i = tid; i < segs; i += kPick) {
-        const float x = float_of(s.keys[i]), d = (m - x) * step;
+        const float x = float_of(keys[i]), d = (m - x) * step;
         if (d < float(kPick))
             atomicAdd(reinterpret_cast<unsigned long long *>(&s.bins[int(d)]), by_mass ? (unsigned long long)r.weight(x) : 1ull);
     }
@@ -887,7 +986,7 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, i
     const int want = int(target);
     for (int at = 0; to - from > 1; ++at) {
         const uint32_t k = from + (to - from) / 2;
-        const int n = segments_from(segs, k, at, s);
+        const int n = segments_from(keys, segs, k, at, s);
         if (n >= want)
             from = k;
         else
@@ -902,8 +1001,10 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, i
 template <typename T>
 __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4))) pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ PickShared s;
+    extern __shared__ uint32_t keys[];
     static_assert(kMostParts <= kPick, "a part a thread");
     const int tid = threadIdx.x, segs = g.parts * kSegs;
+    uint16_t *some = reinterpret_cast<uint16_t *>(keys + segs); // of the segments
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *x = logits + row * a.stride;
         const float top = tid < g.parts ? g.top[row * g.parts + tid] : -INFINITY;
@@ -913,7 +1014,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
         if (cut)
 #pragma unroll 4
             for (int i = tid; i < segs; i += kPick)
-                s.keys[i] = key_of(g.seg[row * segs + i]);
+                keys[i] = key_of(g.seg[row * segs + i]);
         const float m = PickBlock::max(top, s.block);
         if (p.scale == 0.0 || !(m < INFINITY) || m == -INFINITY) {
             finish_without(a, row, p.scale == 0.0 || m != -INFINITY);
@@ -921,7 +1022,8 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
         }
         const Row r(m, p.scale, a.shift);
         // the parts' weights, relative to the row's largest logit
-        const uint64_t mine = uint64_t(rint(part_mass * power_of(fmax(double(top) - r.m, r.far), r.c, 0)));
+        const double factor = power_of(fmax(double(top) - r.m, r.far), r.c, 0);
+        const uint64_t mine = uint64_t(rint(part_mass * factor));
         uint64_t total;
         const uint64_t sum = PickBlock::before(mine, total, s.block);
         if (!cut) {
@@ -934,7 +1036,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
             }
             __syncthreads();
             const Row own(s.found_top, p.scale, a.shift);
-            pick_in_part<T, kPick>(a, row, x, s.found, own, r, Last(0), s.found_left, s.found_mass, total, total, s.block);
+            pick_in_part<T, kPick>(a, row, x, s.found, own, r, Last(0), s.found_left, s.found_mass, total, 0.0, s.block);
             __syncthreads();
             continue;
         }
@@ -943,11 +1045,11 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
         bool wide = false, whole = true;
         if (p.top_k < a.V) {
             if (p.top_k <= segs / 2)
-                low = std::max(low, key_reached(false, uint64_t(p.top_k), segs, m, r, s));
+                low = std::max(low, key_reached(false, uint64_t(p.top_k), keys, segs, m, r, s));
             else
                 wide = low == 0;
         } else if (low == 0) {
-            low = key_reached(true, std::max(share_up(total, p.fraction), uint64_t(1)), segs, m, r, s);
+            low = key_reached(true, std::max(share_up(total, p.fraction), uint64_t(1)), keys, segs, m, r, s);
             whole = false;
             wide = low == 0;
         }
@@ -956,10 +1058,12 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
             __syncthreads();
             if (tid == 0)
                 s.found = s.n = 0;
+            s.tops[tid] = top;
+            s.listed[tid] = 0;
             __syncthreads();
             for (int i = tid; i < segs; i += kPick)
-                if (s.keys[i] >= low)
-                    s.segs[atomicAdd(&s.found, 1)] = uint16_t(i);
+                if (keys[i] >= low)
+                    some[atomicAdd(&s.found, 1)] = uint16_t(i);
             __syncthreads();
             const int many = s.found;
             const float lowest = float_of(low);
@@ -970,7 +1074,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int k = i + j / Part<T>::kSame * (kPick / 16);
-                    const int seg = k < many ? s.segs[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
+                    const int seg = k < many ? some[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
                     at[j] = k < many ? seg / kSegs * kPart + Part<T>::at(load + j % Part<T>::kSame, quarter * 16 + tid % 16) : a.V;
                     q[j] = read_at(x, a.V, at[j], first[j]);
                 }
@@ -991,15 +1095,37 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
             }
             __syncthreads();
             const int n = s.n;
-            wide = n > kList ||
-                   !(n <= kPick ? pick_from_few(a, row, r, p, n, whole, total, s) : pick_from_list(a, row, r, p, n, whole, total, s));
+            wide = n > kList;
+            double rest = 0.0;
+            if (!wide && wants_logp(a)) {
+                // what a part has beside the list's tokens, whose weights are those that its sum was made of: what is left of
+                // the roundings of a sum counts as nothing
+                const bool quick = mass_of(a, row) == Mass::kQuick;
+                for (int i = tid; i < n; i += kPick) {
+                    const int part = index_of(s.list[i]) / kPart;
+                    const float v = float_of(key_in(s.list[i])), own = s.tops[part];
+                    const double w = quick ? ldexp(double(Quick(own, p.scale).power(v)), 51)
+                                           : power_of(fmax(double(v) - double(own), r.far), r.c, 51);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.listed[part]), (unsigned long long)whole_of(w));
+                }
+                __syncthreads();
+                if (tid < g.parts) {
+                    const double left = part_mass - ldexp(double(s.listed[tid]), a.shift - 51);
+                    rest = left > part_mass * 0x1p-44 ? left * factor : 0.0;
+                }
+                rest = PickBlock::sum(rest, s.block);
+            }
+            if (!wide && n <= kWave)
+                wide = __syncthreads_or(tid < kWave && !pick_from_few<kWave>(a, row, r, p, n, whole, total, rest, s));
+            else if (!wide)
+                wide = !(n <= kFew ? pick_from_few<kFew>(a, row, r, p, n, whole, total, rest, s)
+                                   : pick_from_list(a, row, r, p, n, whole, total, rest, s));
         }
         if (wide && tid == 0) {
             WideRow &w = g.rows[atomicAdd(g.wide, 1u)];
             w.row = row;
             w.top = m;
             w.least = least;
-            w.total = total;
             w.arrived[0] = w.arrived[1] = w.listed = 0;
         }
         __syncthreads();
@@ -1023,6 +1149,7 @@ struct WideShared {
     uint32_t count[kFine];
     uint64_t list[kMembers];
     uint64_t kept[kMostParts];
+    double lost[kMostParts];
     WideBlock::Shared block;
     List<kWide>::Shared find;
     uint64_t found_mass, found_left;
@@ -1030,12 +1157,12 @@ struct WideShared {
     bool last;
 };
 
-// The bin of a logit by its distance from the largest, which never decreases as logits do; kFine: its weight is 0. Halves,
-// because the distance itself may be no float.
+// The bin of a logit by its distance from the largest, which never decreases as logits do; kFine: beyond 63 in units of the
+// exponent, where neither what is kept nor what is not is felt any more. Halves, because the distance itself may be no float.
 struct Bins {
     float half, step;
     __device__ __forceinline__ Bins(const Row &r)
-        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 31.5f), 3.402823466e38f)) {}
+        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 63.0f), 3.402823466e38f)) {}
     __device__ __forceinline__ int of(float x) const {
         const float d = (half - x * 0.5f) * step;
         return d < float(kFine) ? int(d) : kFine;
@@ -1188,7 +1315,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             }
             there = WideBlock::sum(there, s.block);
             inside = WideBlock::sum(inside, s.block);
-            const bool cut = uint64_t(p.top_k) < there; // otherwise what it cuts off has no weight
+            const bool cut = uint64_t(p.top_k) < there; // otherwise what it cuts off is beyond the bins
             if (cut) {
                 bin = bin_of(false, uint64_t(p.top_k), left, above, s);
                 members = int(s.count[bin]);
@@ -1262,11 +1389,14 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
         const bool exact = bin == kFine;
         const Last last(w.last);
         uint64_t *list = g.list + slot * kMembers, *kept_of = g.kept + slot * kMostParts; // where the row is shared
+        double *lost_of = g.lost + slot * kMostParts;
+        const bool wants = wants_logp(a);
         if (tid == 0)
             s.n = 0;
         __syncthreads();
         for (int part = int(item - slot * shares) + wave * shares; part < g.parts; part += shares * WideBlock::kWaves) {
             uint64_t mass = 0;
+            double lost = 0.0;
             typename Vec<T>::type q[P::kLoads];
             int at[P::kLoads];
 #pragma unroll
@@ -1279,14 +1409,21 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                     const float v = float(q[j][k]);
                     const int mine = bins.of(v);
                     const bool in = v >= least;
-                    if (exact ? last.keeps(v, at[j] + k) : in && mine < bin)
-                        mass += r.weight(v);
+                    const bool keep = exact ? last.keeps(v, at[j] + k) : in && mine < bin;
                     if (!exact && in && mine == bin)
                         s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), at[j] + k);
+                    else if (keep || wants) {
+                        const double w = r.power(v);
+                        mass += keep ? whole_of(w) : 0;
+                        lost += keep || v == -INFINITY ? 0.0 : w;
+                    }
                 }
             mass = wave_sum(mass);
-            if (lane == 0)
+            lost = wave_sum(lost);
+            if (lane == 0) {
                 (shares > 1 ? kept_of : s.kept)[part] = mass;
+                (shares > 1 ? lost_of : s.lost)[part] = lost;
+            }
         }
         if (shares > 1) {
             __syncthreads();
@@ -1300,8 +1437,11 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             continue;
         __syncthreads();
         uint64_t end = w.last;
-        if (shares > 1 && tid < g.parts)
+        if (shares > 1 && tid < g.parts) {
             s.kept[tid] = kept_of[tid];
+            s.lost[tid] = lost_of[tid];
+        }
+        Fine below; // of the bin's entries that are not kept
         if (!exact) {
             const int n = w.members;
             if (shares > 1)
@@ -1310,14 +1450,19 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             uint64_t unused;
             __syncthreads();
             end = List<kWide>::find<Order::kLogits>(w.by_mass, w.left, s.list, n, 0, r, unused, s.find, s.block);
-            for (int i = tid; i < n; i += kWide)
-                if (s.list[i] >= end)
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(s.list[i]) / kPart]), (unsigned long long)r.key_weight(key_in(s.list[i])));
+            for (int i = tid; i < n; i += kWide) {
+                const uint64_t e = s.list[i];
+                if (e >= end)
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(e) / kPart]), (unsigned long long)r.key_weight(key_in(e)));
+                else
+                    below.add(r.share(float_of(key_in(e))));
+            }
         }
         __syncthreads();
         uint64_t kept;
         const uint64_t mine = tid < g.parts ? s.kept[tid] : 0;
         const uint64_t sum = WideBlock::before(mine, kept, s.block);
+        const double dropped = WideBlock::sum(tid < g.parts ? s.lost[tid] : 0.0, s.block) + WideBlock::sum(below, s.block).units(a.shift);
         const uint64_t target = share_down(kept, p.at);
         if (sum <= target && target < sum + mine) {
             s.found = tid;
@@ -1325,7 +1470,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             s.found_mass = mine;
         }
         __syncthreads();
-        pick_in_part<T, kWide>(a, row, x, s.found, r, r, Last(end), s.found_left, s.found_mass, kept, w.total, s.block);
+        pick_in_part<T, kWide>(a, row, x, s.found, r, r, Last(end), s.found_left, s.found_mass, kept, dropped, s.block);
         __syncthreads();
     }
 }
@@ -1359,15 +1504,12 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
         const Row r(m, p.scale, a.shift);
         const uint32_t floor = floor_key(r.m, p.scale, p.least, key_of(m));
         const float least = floor ? float_of(floor) : -INFINITY;
-        uint64_t total = 0, inside = 0, there = 0, unused;
+        uint64_t inside = 0, there = 0, unused;
         for (int64_t i = tid; i < a.V; i += kLong) {
             const float v = float(x[i]);
-            const uint64_t w = r.weight(v);
-            total += w;
-            inside += v >= least ? w : 0;
+            inside += v >= least ? r.weight(v) : 0;
             there += v >= least;
         }
-        total = B::sum(total, s);
         inside = B::sum(inside, s);
         there = B::sum(there, s);
         uint64_t end = floor ? entry_of(floor, -1) : 0;
@@ -1380,10 +1522,15 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
         const int64_t each = int64_t((a.V - 1) / kLong + 1) * kWave;
         const int64_t from = std::min(wave * each, int64_t(a.V)), to = std::min(from + each, int64_t(a.V));
         uint64_t mine = 0;
+        double lost = 0.0;
         for (int64_t i = from + lane; i < to; i += kWave) {
             const float v = float(x[i]);
-            mine += last.keeps(v, int(i)) ? r.weight(v) : 0;
+            const bool keep = last.keeps(v, int(i));
+            const double w = r.power(v);
+            mine += keep ? whole_of(w) : 0;
+            lost += keep || v == -INFINITY ? 0.0 : w;
         }
+        lost = B::sum(lost, s);
         mine = wave_sum(mine);
         __syncthreads();
         if (lane == 0)
@@ -1401,7 +1548,7 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
             const uint64_t with = sum + wave_scan(i < to && last.keeps(v, int(i)) ? r.weight(v) : 0);
             const uint64_t past = __ballot(with > target);
             if (first && past && lane == __builtin_ctzll(past))
-                finish_row(a, row, r, int(i), v, kept, total);
+                finish_row(a, row, r, int(i), v, double(kept), lost);
             sum = last_lane(with);
         }
         __syncthreads();
@@ -1452,6 +1599,7 @@ int64_t lay_out(const Plan &p, int64_t n, char *at, Digest &g) {
     g.bins = s.take<uint64_t>(slices * kFine);
     g.members = s.take<unsigned>(slices * kFine);
     g.kept = s.take<uint64_t>(slots * kMostParts);
+    g.lost = s.take<double>(slots * kMostParts);
     g.list = s.take<uint64_t>(slots * kMembers);
     return s.bytes;
 }
@@ -1540,10 +1688,10 @@ int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_t
         } else if (plan.parts) {
             const int64_t blocks = (n_tokens * plan.parts + 3) / 4;
             hipLaunchKernelGGL(scan_kernel<T>, dim3(unsigned(std::min(blocks, kMaxBlocks))), dim3(256), 0, s, x, a, g);
-            hipLaunchKernelGGL(pick_kernel<T>, rows, dim3(kPick), 0, s, x, a, g);
+            hipLaunchKernelGGL(pick_kernel<T>, rows, dim3(kPick), unsigned(plan.parts * kSegBytes), s, x, a, g);
             if (!row_top_k && !row_top_p && !row_min_p && a.top_k == 0 && top_p == 1.0f && min_p == 0.0f)
                 return; // no row is cut off
-            const dim3 wide(unsigned(std::min<int64_t>(n_tokens * kMostShares, 2 * kSlices)));
+            const dim3 wide(unsigned(std::min<int64_t>(n_tokens * kMostShares, kSlices)));
             hipLaunchKernelGGL(wide_place_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
             hipLaunchKernelGGL(wide_pick_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
         } else

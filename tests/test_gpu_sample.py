@@ -1,8 +1,10 @@
 """GPU sampling through the C ABI, against the float64 oracle on the same (already rounded) logits.
 
 Tokens are equal. Weights are off by 2^-39 of themselves and half a unit (2^-45, for fewer than 2^19 tokens) at most, so
-the total, at least 1, by 2^-39 + 2^-45 V relative, and logp by as much beside its own rounding, 2^-24 of it; the dropped
-weights and the total by the same relative to the total, so log_kept by twice that over the share that is kept."""
+what is kept, at least 1, by 2^-39 + 2^-45 V relative; what is not kept is added as it is, in single precision where top_k or
+min_p cuts: of u = 2^-24 a weight exp(z) is then off by 3 u |z| (the distance, its product, the exponent) and 4 u (exp2), and
+the |z| that count are below 48, so the share D that is not kept by 152 u. logp and the logarithm of the share kept are off by
+as much, the latter over the share kept, beside their own rounding, u of them."""
 from __future__ import annotations
 
 from fractions import Fraction
@@ -55,8 +57,9 @@ def _check(got, want, V, what):
     tokens, logp, log_kept = (g.cpu().numpy() for g in got)
     assert np.array_equal(tokens, want[0]), (what, np.nonzero(tokens != want[0])[0][:5], tokens[:5], want[0][:5])
     off = 2.0 ** -39 + 2.0 ** -45 * max(V, 1) * max(1.0, V / 2 ** 18)
-    for name, a, b, e in (("logp", logp, want[1], off + U * np.abs(want[1])),
-                          ("log_kept", log_kept, want[2], 2 * off / np.exp(want[2]) + U * np.abs(want[2]))):
+    quick = 152 * U * -np.expm1(want[2])
+    for name, a, b, e in (("logp", logp, want[1], off + quick + U * np.abs(want[1])),
+                          ("log_kept", log_kept, want[2], (2 * off + quick) / np.exp(want[2]) + U * np.abs(want[2]))):
         fine = np.isfinite(b)
         assert np.array_equal(a[~fine], b[~fine], equal_nan=True), (what, name)
         err = np.abs(a[fine].astype(np.float64) - b[fine]) - e[fine]
@@ -190,6 +193,31 @@ def test_even_random_numbers_give_the_distribution(T, V):
     p[order] = w[order] / w[order].sum()
     assert np.abs(np.bincount(tokens.cpu().numpy(), minlength=V) - n * p).max() <= 1 + 1e-6
     assert isinstance(tokens, torch.Tensor) and tokens.dtype == torch.int64
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [60, 900, 2_500, 70_000])
+def test_shares_not_kept_however_small(T, dtype, V):
+    """Rows of which almost nothing is dropped, down to 1e-13 of the probability, and then nothing at all: the logarithm of the
+    share kept is right in proportion. Single precision: 152 u of it; what is left of a sum whose tokens are taken out of it again
+    counts as nothing up to 2^-44, which a row of 35 parts may do in each."""
+    n = 12
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 1, (n, V))
+    x[np.arange(n), rng.integers(0, V, n)] = np.linspace(12, 32, n)
+    x[:, rng.permutation(V)[:20]] += 6.0
+    d = _dev(x).to(_torch_dtype(dtype))
+    x, u = d.double().cpu().numpy(), rng.random(n)
+    for params in (dict(top_k=1), dict(top_k=15), dict(top_k=V - V // 8), dict(min_p=_f32(1e-3)), dict(top_p=0.5), dict(top_k=V // 2, top_p=0.75)):
+        want = O.sample(x, u, **params)
+        tokens, logp, log_kept = (t.double().cpu().numpy() for t in T.tree_ens_sample(d, _dev(u), **params))
+        assert np.array_equal(tokens, want[0])
+        assert (np.abs(log_kept - want[2]) <= 153 * U * np.abs(want[2]) + 40 * 2.0 ** -44).all(), (params, log_kept, want[2])
+        assert (np.abs(logp - want[1]) <= 153 * U * -np.expm1(want[2]) + U * np.abs(want[1]) + 2.0 ** -39 + 2.0 ** -45 * V).all()
+    # masked beyond the first: nothing has a weight that is not kept
+    d[:, 10:] = -float("inf")
+    for params in (dict(top_k=10), dict(top_k=11), dict(min_p=_f32(1e-30)), dict(top_k=min(V, 500), min_p=_f32(1e-30))):
+        assert not T.tree_ens_sample(d, _dev(u), **params)[2].any(), params
 
 
 @pytest.mark.parametrize("V", [700, 9_000])
