@@ -51,13 +51,21 @@ struct Params {
 
 constexpr uint64_t kOne = uint64_t(1) << 53;
 
+// a / b to about 2^-50, in a third of an exact division's instructions.
+__device__ __forceinline__ double ratio(double a, double b) {
+    double r = __builtin_amdgcn_rcp(b);
+    r = fma(fma(-b, r, 1.0), r, r);
+    r = fma(fma(-b, r, 1.0), r, r);
+    return a * r;
+}
+
 // The natural logarithm of a number of at least 2^-1000, to about 2^-45: of the exponent, and 2 atanh of (m - 1) / (m + 1) for
 // the rest m, within sqrt(2) of 1, by its series. A few dozen instructions where the library's has hundreds, which a
 // workgroup that comes by once has to fetch first.
 __device__ __forceinline__ double log_of(double x) {
     const int high = __double2hiint(x), n = (high - 0x3fe6a09e) >> 20; // 0x3fe6a09e...: sqrt(1/2)
     const double m = __hiloint2double(high - (n << 20), __double2loint(x));
-    const double q = (m - 1.0) / (m + 1.0), y = q * q;
+    const double q = ratio(m - 1.0, m + 1.0), y = q * q;
     double p = 1.0 / 15;
     p = fma(p, y, 1.0 / 13);
     p = fma(p, y, 1.0 / 11);
@@ -277,7 +285,7 @@ __device__ __forceinline__ void finish_row(const Args &a, int64_t row, const Row
     if (a.logp)
         a.logp[row] = float((double(x) - r.m) * r.scale - log_of(kept + dropped) + r.shift * 0.6931471805599453);
     if (a.log_kept) {
-        const double d = dropped / (kept + dropped);
+        const double d = ratio(dropped, kept + dropped);
         a.log_kept[row] = float(d < 0x1p-16 ? -fma(d, fma(d, 1.0 / 3, 0.5) * d, d) : log_of(1.0 - d));
     }
 }
@@ -466,28 +474,31 @@ template <int kT> struct List {
     // The entry of list[0, n) at which the count (by_mass: the weights) of those of at least `least` reaches `target`, which it
     // does; `inside` receives the weights down to it. By bins of the range that the entries have, as many as there are
     // threads, and then of the range of the bin that holds it, until it is alone: two or three times, whatever the entries.
+    // `high` and `low`: bounds of the entries as the order has them, or 0 and 0.
     template <Order kOrder>
-    static __device__ __forceinline__ uint64_t find(bool by_mass, uint64_t target, const uint64_t *list, int n, uint64_t least, const Row &r,
-                                                    uint64_t &inside, Shared &s, typename B::Shared &block) {
+    static __device__ __forceinline__ uint64_t find(bool by_mass, uint64_t target, const uint64_t *list, int n, uint64_t least, uint64_t high,
+                                                    uint64_t low, const Row &r, uint64_t &inside, Shared &s, typename B::Shared &block) {
         const int tid = threadIdx.x;
-        uint64_t high = 0, low = ~uint64_t(0);
-        for (int i = tid; i < n; i += kT)
-            if (list[i] >= least) {
-                high = std::max(high, ordered<kOrder>(list[i]));
-                low = std::min(low, ordered<kOrder>(list[i]));
-            }
-        high = wave_max(high);
-        low = ~wave_max(~low);
-        if constexpr (B::kWaves > 1) {
-            __syncthreads();
-            if (tid % kWave == 0) {
-                s.high[tid / kWave] = high;
-                s.low[tid / kWave] = low;
-            }
-            __syncthreads();
-            for (int w = 0; w < B::kWaves; ++w) {
-                high = std::max(high, s.high[w]);
-                low = std::min(low, s.low[w]);
+        if (high == 0) {
+            low = ~uint64_t(0);
+            for (int i = tid; i < n; i += kT)
+                if (list[i] >= least) {
+                    high = std::max(high, ordered<kOrder>(list[i]));
+                    low = std::min(low, ordered<kOrder>(list[i]));
+                }
+            high = wave_max(high);
+            low = ~wave_max(~low);
+            if constexpr (B::kWaves > 1) {
+                __syncthreads();
+                if (tid % kWave == 0) {
+                    s.high[tid / kWave] = high;
+                    s.low[tid / kWave] = low;
+                }
+                __syncthreads();
+                for (int w = 0; w < B::kWaves; ++w) {
+                    high = std::max(high, s.high[w]);
+                    low = std::min(low, s.low[w]);
+                }
             }
         }
         uint64_t above = 0;
@@ -580,10 +591,10 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
             there = B::sum(there, s);
             __syncthreads();
             if (uint64_t(p.top_k) < there)
-                lowest = L::template find<Order::kLogits>(false, uint64_t(p.top_k), list, a.V, lowest, r, inside, find, s);
+                lowest = L::template find<Order::kLogits>(false, uint64_t(p.top_k), list, a.V, lowest, 0, 0, r, inside, find, s);
             uint64_t unused;
             if (p.fraction < kOne)
-                lowest = L::template find<Order::kLogits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, r, unused, find, s);
+                lowest = L::template find<Order::kLogits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, 0, 0, r, unused, find, s);
         }
         uint64_t mine = 0;
         double lost = 0.0;
@@ -692,11 +703,11 @@ struct Digest {
     unsigned *wide;    // the number of rows left
     WideRow *rows;     // [n]
     // where several workgroups share a row:
-    uint64_t *bins;    // [kSlices][kFine]
-    unsigned *members; // [kSlices][kFine]
-    uint64_t *kept;    // [kSlices / 2][kMostParts]: weights above the bin
-    double *lost;      // [kSlices / 2][kMostParts]: and below it
-    uint64_t *list;    // [kSlices / 2][kMembers]: the bin's entries
+    uint64_t *bins;    // [kShared][kFine]: weights, and
+    unsigned *members; // [kShared][kFine]: the numbers of tokens; set to 0 by pick_kernel
+    uint64_t *kept;    // [kShared][kMostParts]: weights above the bin, and
+    double *lost;      // [kShared][kMostParts]: below it
+    uint64_t *list;    // [kShared][kMembers]: the bin's entries
     int parts;
 };
 
@@ -708,10 +719,14 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
     const int lane = threadIdx.x % kWave;
     if (blockIdx.x == 0 && threadIdx.x == 0)
         *g.wide = 0;
-    const int64_t items = a.n * g.parts;
-    for (int64_t item = blockIdx.x * int64_t(4) + threadIdx.x / kWave; item < items; item += gridDim.x * int64_t(4)) {
-        const int64_t row = item / g.parts;
-        const int part = int(item - row * g.parts);
+    const int each = (g.parts + 3) / 4; // workgroups of a row
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
+    for (int64_t at = blockIdx.x; at < a.n * each; at += gridDim.x) {
+        const int64_t row = at / each;
+        const int part = int(at - row * each) * 4 + wave;
+        if (part >= g.parts)
+            continue;
+        const int64_t item = row * g.parts + part;
         typename Vec<T>::type q[P::kLoads];
         P::read(logits + row * a.stride + part * kPart, a.V - part * kPart, lane, q);
         float v[kN], m = -INFINITY, mine = -INFINITY;
@@ -763,14 +778,22 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kList = 1024; // candidates of pick_kernel
+constexpr int kList = 512;     // candidates of pick_kernel
 constexpr int kMembers = 2048; // of a bin
-constexpr int kFine = 1024; // bins
+constexpr int kFine = 1024;    // bins
+constexpr int kShared = 256;   // wide rows that workgroups may share
+
+// What finish_row takes, from whichever thread finds it.
+struct Outcome {
+    int token;
+    float x;
+    double kept, dropped;
+};
 
 // The token among the logits of one part, as far into the sum of its kept weights there as `ask` is in `of`.
 template <typename T, int kT>
-__device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T *x, int part, const Row &own, const Row &r, Last last,
-                                             uint64_t ask, uint64_t of, uint64_t kept, double dropped, typename Block<kT>::Shared &s) {
+__device__ __forceinline__ void pick_in_part(const Args &a, const T *x, int part, const Row &own, Last last, uint64_t ask, uint64_t of,
+                                             Outcome &out, typename Block<kT>::Shared &s) {
     constexpr int kEach = kPart / kT;
     const int from = part * kPart + threadIdx.x * kEach;
     float v[kEach];
@@ -785,22 +808,18 @@ __device__ __forceinline__ void pick_in_part(const Args &a, int64_t row, const T
     }
     uint64_t sum = Block<kT>::before(mine, all, s);
     const uint64_t target = all == of ? ask : std::min(uint64_t(double(ask) / double(of) * double(all)), all - 1);
-    int token = -1;
-    float at = 0.0f;
     if (sum <= target && target < sum + mine)
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             if (sum <= target && target < sum + w[i]) {
-                token = from + i;
-                at = v[i];
+                out.token = from + i;
+                out.x = v[i];
             }
             sum += w[i];
         }
-    if (token >= 0)
-        finish_row(a, row, r, token, at, double(kept), dropped);
 }
 
-constexpr int kPick = 256, kFew = 256;
+constexpr int kPick = 256;
 using PickBlock = Block<kPick>;
 
 struct Weighed {
@@ -811,7 +830,7 @@ constexpr int kAhead = 8;
 struct PickShared {
     uint64_t list[kList];
     union {
-        Weighed weighed[kFew + kAhead];
+        Weighed weighed[kWave + kAhead];
         List<kPick>::Shared find;
     };
     uint64_t bins[kPick];
@@ -821,6 +840,7 @@ struct PickShared {
     uint64_t found_mass, found_left;
     float found_top;
     int found, n;
+    Outcome out;
     int ge[2][PickBlock::kWaves];
 };
 // Behind it in LDS, for as many segments as there are: the keys of their largest logits, of which thread t has every kPick-th
@@ -859,7 +879,7 @@ template <typename F> __device__ __forceinline__ void for_entries(const PickShar
 // The token from s.list[0, n), which holds every token down to some place of the order. `whole`: all that min_p and top_k
 // leave is among them; otherwise `total` is the weight of all that top_p is a share of. `rest`: the weights of the tokens
 // beyond the list. False where the list ends before the last kept token does.
-__device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
+__device__ __forceinline__ bool pick_from_list(const Args &a, const Row &r, const Params &p, uint32_t low, int n, bool whole, uint64_t total,
                                                double rest, PickShared &s) {
     using L = List<kPick>;
     uint64_t kept = 0, end = 0, unused;
@@ -873,7 +893,8 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const
         const uint64_t target = pass ? std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
         if (pass && kept < target)
             return false;
-        end = L::find<Order::kLogits>(pass, target, s.list, n, end, r, kept, s.find, s.block);
+        end = L::find<Order::kLogits>(pass, target, s.list, n, end, entry_of(key_of(float(r.m)), 0), entry_of(low, -1), r, kept, s.find,
+                                      s.block);
     }
     Fine lost;
     if (wants_logp(a) && end) {
@@ -883,70 +904,61 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, int64_t row, const
         lost = PickBlock::sum(lost, s.block);
     }
     // sums are whole numbers: past the random share of them is to reach the next one
-    const uint64_t token = L::find<Order::kVocabulary>(true, share_down(kept, p.at) + 1, s.list, n, end, r, unused, s.find, s.block);
+    const uint64_t token = L::find<Order::kVocabulary>(true, share_down(kept, p.at) + 1, s.list, n, end, ~uint64_t(0),
+                                                              ordered<Order::kVocabulary>(entry_of(0, a.V - 1)), r, unused, s.find, s.block);
     if (threadIdx.x == 0)
-        finish_row(a, row, r, index_of(token), float_of(key_in(token)), double(kept), rest + lost.units(r.shift));
+        s.out = {index_of(token), float_of(key_in(token)), double(kept), rest + lost.units(r.shift)};
     return true;
 }
 
-// The same of up to kT entries, by the first kT threads, one each: every thread reads the others', in no order, and adds what comes
-// before its own. A wave needs no barriers for it.
-template <int kT>
-__device__ __forceinline__ bool pick_from_few(const Args &a, int64_t row, const Row &r, const Params &p, int n, bool whole, uint64_t total,
-                                              double rest, PickShared &s) {
-    const int tid = threadIdx.x;
-    typename Block<kT>::Shared &block = reinterpret_cast<typename Block<kT>::Shared &>(s.block);
-    const auto wait = [] {
-        if constexpr (kT > kWave)
-            __syncthreads();
-        else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+// The same of up to 64 entries, by the first wave alone and so without barriers: every lane reads the others' entries, in no
+// order, and adds what comes before its own.
+__device__ __forceinline__ bool pick_from_few(const Args &a, const Row &r, const Params &p, int n, bool whole, uint64_t total, double rest,
+                                              PickShared &s) {
+    const int lane = threadIdx.x;
+    const auto wait = [] { // for the wave's own LDS accesses, which are in order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     };
-    const bool busy = tid - tid % kWave < n; // a lane of the wave has an entry
-    bool keep = tid < n;
-    const uint64_t mine = keep ? s.list[tid] : 0;
+    bool keep = lane < n;
+    const uint64_t mine = keep ? s.list[lane] : 0;
     const uint64_t w = keep ? r.key_weight(key_in(mine)) : 0;
     if (keep)
-        s.weighed[tid] = {mine, w};
-    if (tid == 0)
-        s.n = 0;
+        s.weighed[lane] = {mine, w};
     wait();
     if (p.top_k < n || p.fraction < kOne) {
         uint64_t before = 0;
         int rank = 0;
-        if (busy)
-            for_entries(s, n, [&](const Weighed &o) {
-                before += o.entry > mine ? o.weight : 0;
-                rank += o.entry > mine;
-            });
+        for_entries(s, n, [&](const Weighed &o) {
+            before += o.entry > mine ? o.weight : 0;
+            rank += o.entry > mine;
+        });
         keep = keep && rank < p.top_k;
         if (p.fraction < kOne) {
-            const uint64_t inside = Block<kT>::sum(keep ? w : 0, block);
+            const uint64_t inside = wave_sum(keep ? w : 0);
             const uint64_t target = std::max(share_up(whole ? inside : total, p.fraction), uint64_t(1));
             if (inside < target)
                 return false;
             keep = keep && before < target;
         }
+        wait();
+        if (lane < n)
+            s.weighed[lane].weight = keep ? w : 0;
+        wait();
     }
-    const uint64_t kept = Block<kT>::sum(keep ? w : 0, block), target = share_down(kept, p.at);
+    const uint64_t kept = wave_sum(keep ? w : 0), target = share_down(kept, p.at);
     Fine lost;
     if (wants_logp(a)) {
-        if (tid < n && !keep)
+        if (lane < n && !keep)
             lost.add(r.share(float_of(key_in(mine))));
-        lost = Block<kT>::sum(lost, block);
+        lost = {wave_sum(lost.high), wave_sum(lost.low)};
     }
-    if (keep)
-        s.weighed[atomicAdd(&s.n, 1)] = {mine, w};
-    wait();
     uint64_t before = 0;
-    if (busy)
-        for_entries(s, s.n, [&](const Weighed &o) {
-            before += uint32_t(o.entry) > uint32_t(mine) ? o.weight : 0; // indices before this one's
-        });
+    for_entries(s, n, [&](const Weighed &o) {
+        before += uint32_t(o.entry) > uint32_t(mine) ? o.weight : 0; // indices before this one's
+    });
     if (keep && before <= target && target < before + w)
-        finish_row(a, row, r, index_of(mine), float_of(key_in(mine)), double(kept), rest + lost.units(r.shift));
+        s.out = {index_of(mine), float_of(key_in(mine)), double(kept), rest + lost.units(r.shift)};
     return true;
 }
 
@@ -999,7 +1011,7 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, c
 
 // A workgroup takes a row.
 template <typename T>
-__global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4))) pick_kernel(const T *logits, Args a, Digest g) {
+__global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3))) pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ PickShared s;
     extern __shared__ uint32_t keys[];
     static_assert(kMostParts <= kPick, "a part a thread");
@@ -1036,8 +1048,10 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
             }
             __syncthreads();
             const Row own(s.found_top, p.scale, a.shift);
-            pick_in_part<T, kPick>(a, row, x, s.found, own, r, Last(0), s.found_left, s.found_mass, total, 0.0, s.block);
+            pick_in_part<T, kPick>(a, x, s.found, own, Last(0), s.found_left, s.found_mass, s.out, s.block);
             __syncthreads();
+            if (tid == 0)
+                finish_row(a, row, r, s.out.token, s.out.x, double(total), 0.0);
             continue;
         }
         uint32_t low = floor_key(r.m, p.scale, p.least, key_of(m));
@@ -1067,19 +1081,19 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
             __syncthreads();
             const int many = s.found;
             const float lowest = float_of(low);
-            // a quarter of a wave has four loads on their way at a time
-            for (int i = tid / 16; i < many; i += kPick / 16 * (4 / Part<T>::kSame)) {
-                typename Vec<T>::type q[4];
-                int at[4], first[4];
+            constexpr int kLoads = 4; // of a quarter of a wave on their way at a time
+            for (int i = tid / 16; i < many; i += kPick / 16 * (kLoads / Part<T>::kSame)) {
+                typename Vec<T>::type q[kLoads];
+                int at[kLoads], first[kLoads];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kLoads; ++j) {
                     const int k = i + j / Part<T>::kSame * (kPick / 16);
                     const int seg = k < many ? some[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
                     at[j] = k < many ? seg / kSegs * kPart + Part<T>::at(load + j % Part<T>::kSame, quarter * 16 + tid % 16) : a.V;
                     q[j] = read_at(x, a.V, at[j], first[j]);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kLoads; ++j) {
                     unsigned hits = 0;
 #pragma unroll
                     for (int k = 0; k < Part<T>::N; ++k)
@@ -1116,19 +1130,28 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
                 rest = PickBlock::sum(rest, s.block);
             }
             if (!wide && n <= kWave)
-                wide = __syncthreads_or(tid < kWave && !pick_from_few<kWave>(a, row, r, p, n, whole, total, rest, s));
+                wide = __syncthreads_or(tid < kWave && !pick_from_few(a, r, p, n, whole, total, rest, s));
             else if (!wide)
-                wide = !(n <= kFew ? pick_from_few<kFew>(a, row, r, p, n, whole, total, rest, s)
-                                   : pick_from_list(a, row, r, p, n, whole, total, rest, s));
+                wide = !pick_from_list(a, r, p, low, n, whole, total, rest, s);
         }
-        if (wide && tid == 0) {
-            WideRow &w = g.rows[atomicAdd(g.wide, 1u)];
+        __syncthreads();
+        if (!wide) {
+            if (tid == 0)
+                finish_row(a, row, r, s.out.token, s.out.x, s.out.kept, s.out.dropped);
+            continue;
+        }
+        if (tid == 0) {
+            s.found = int(atomicAdd(g.wide, 1u));
+            WideRow &w = g.rows[s.found];
             w.row = row;
             w.top = m;
             w.least = least;
             w.arrived[0] = w.arrived[1] = w.listed = 0;
         }
         __syncthreads();
+        if (s.found < kShared)
+            for (int i = tid; i < kFine; i += kPick)
+                g.bins[int64_t(s.found) * kFine + i] = g.members[int64_t(s.found) * kFine + i] = 0;
     }
 }
 
@@ -1136,12 +1159,12 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(4)))
 // rows of which more tokens are kept than a list holds
 // ------------------------------------------------------------------------------------------------
 constexpr int kWide = 512;
-constexpr int kSlices = 512, kMostShares = 16;
+constexpr int kMostShares = 16;
 using WideBlock = Block<kWide>;
 
 // Workgroups that share a row, so that a few wide rows have many and many have one each.
 __device__ __forceinline__ int shares_of(unsigned wide, int parts) {
-    return wide > kSlices / 2 ? 1 : std::max(1, std::min(std::min(int(kSlices / wide), kMostShares), parts / 4));
+    return wide > kShared ? 1 : std::max(1, std::min(std::min(int(2 * kShared / wide), kMostShares), parts / 4));
 }
 
 struct WideShared {
@@ -1154,6 +1177,7 @@ struct WideShared {
     List<kWide>::Shared find;
     uint64_t found_mass, found_left;
     int found, n;
+    Outcome out;
     bool last;
 };
 
@@ -1239,18 +1263,19 @@ __device__ __forceinline__ int bin_of(bool by_mass, uint64_t target, uint64_t &l
     return s.found;
 }
 
-// Whether this workgroup is the last of `shares` to come here; what the others wrote before is then seen.
+// What workgroups of a row leave for the last of them goes past their caches, each of which belongs to some of them only.
+template <typename V> __device__ __forceinline__ void leave(V *p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V> __device__ __forceinline__ V left_at(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Whether this workgroup is the last of `shares` to come here, so that what the others left is there. Every wave waits for its
+// stores before the arrival is counted; fences, which write back and empty a whole cache, took 40 us of 64 rows in 8 shares.
 __device__ __forceinline__ bool is_last(unsigned *arrived, int shares, WideShared &s) {
     if (shares == 1)
         return true;
-    __builtin_amdgcn_s_waitcnt(0); // every wave's stores have reached the cache
+    __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence(); // for the whole workgroup, which shares its caches: a fence of every wave's own took ten times as long
+    if (threadIdx.x == 0)
         s.last = atomicAdd(arrived, 1u) == unsigned(shares - 1);
-        if (s.last)
-            __threadfence();
-    }
     __syncthreads();
     return s.last;
 }
@@ -1280,31 +1305,18 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
         if (p.top_k < a.V || p.fraction < kOne) {
             fill_bins(x, a.V, int(item - slot * shares), shares, r, bins, least, s);
             if (shares > 1) {
-                for (int i = tid; i < kFine; i += kWide) {
-                    g.bins[item * kFine + i] = s.mass[i];
-                    g.members[item * kFine + i] = s.count[i];
-                }
+                uint64_t *all = g.bins + slot * kFine;
+                unsigned *number = g.members + slot * kFine;
+                for (int i = tid; i < kFine; i += kWide)
+                    if (s.count[i]) {
+                        atomicAdd(number + i, s.count[i]);
+                        atomicAdd(reinterpret_cast<unsigned long long *>(all + i), (unsigned long long)s.mass[i]);
+                    }
                 if (!is_last(&w.arrived[0], shares, s))
                     continue;
-                {
-                    static_assert(kFine == 2 * kWide, "two bins a thread");
-                    uint64_t mass[2] = {0, 0};
-                    uint32_t count[2] = {0, 0};
-#pragma unroll 8
-                    for (int k = 0; k < shares; ++k) {
-                        const int64_t at = (slot * shares + k) * kFine + 2 * tid;
-                        const ulonglong2 m = *reinterpret_cast<const ulonglong2 *>(g.bins + at);
-                        const uint2 c = *reinterpret_cast<const uint2 *>(g.members + at);
-                        mass[0] += m.x;
-                        mass[1] += m.y;
-                        count[0] += c.x;
-                        count[1] += c.y;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        s.mass[2 * tid + i] = mass[i];
-                        s.count[2 * tid + i] = count[i];
-                    }
+                for (int i = tid; i < kFine; i += kWide) {
+                    s.mass[i] = left_at(all + i);
+                    s.count[i] = left_at(number + i);
                 }
                 __syncthreads();
             }
@@ -1333,7 +1345,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                             s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), i);
                     });
                     __syncthreads();
-                    List<kWide>::find<Order::kLogits>(false, left, s.list, members, 0, r, inside, s.find, s.block);
+                    List<kWide>::find<Order::kLogits>(false, left, s.list, members, 0, 0, 0, r, inside, s.find, s.block);
                     inside += above;
                     __syncthreads();
                 }
@@ -1421,8 +1433,13 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             mass = wave_sum(mass);
             lost = wave_sum(lost);
             if (lane == 0) {
-                (shares > 1 ? kept_of : s.kept)[part] = mass;
-                (shares > 1 ? lost_of : s.lost)[part] = lost;
+                if (shares > 1) {
+                    leave(kept_of + part, mass);
+                    leave(lost_of + part, lost);
+                } else {
+                    s.kept[part] = mass;
+                    s.lost[part] = lost;
+                }
             }
         }
         if (shares > 1) {
@@ -1431,25 +1448,25 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 s.found = int(atomicAdd(&w.listed, unsigned(s.n)));
             __syncthreads();
             for (int i = tid; i < s.n; i += kWide)
-                list[s.found + i] = s.list[i];
+                leave(list + s.found + i, s.list[i]);
         }
         if (!is_last(&w.arrived[1], shares, s))
             continue;
         __syncthreads();
         uint64_t end = w.last;
         if (shares > 1 && tid < g.parts) {
-            s.kept[tid] = kept_of[tid];
-            s.lost[tid] = lost_of[tid];
+            s.kept[tid] = left_at(kept_of + tid);
+            s.lost[tid] = left_at(lost_of + tid);
         }
         Fine below; // of the bin's entries that are not kept
         if (!exact) {
             const int n = w.members;
             if (shares > 1)
                 for (int i = tid; i < n; i += kWide)
-                    s.list[i] = list[i];
+                    s.list[i] = left_at(list + i);
             uint64_t unused;
             __syncthreads();
-            end = List<kWide>::find<Order::kLogits>(w.by_mass, w.left, s.list, n, 0, r, unused, s.find, s.block);
+            end = List<kWide>::find<Order::kLogits>(w.by_mass, w.left, s.list, n, 0, 0, 0, r, unused, s.find, s.block);
             for (int i = tid; i < n; i += kWide) {
                 const uint64_t e = s.list[i];
                 if (e >= end)
@@ -1470,8 +1487,10 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             s.found_mass = mine;
         }
         __syncthreads();
-        pick_in_part<T, kWide>(a, row, x, s.found, r, r, Last(end), s.found_left, s.found_mass, kept, dropped, s.block);
+        pick_in_part<T, kWide>(a, x, s.found, r, Last(end), s.found_left, s.found_mass, s.out, s.block);
         __syncthreads();
+        if (tid == 0)
+            finish_row(a, row, r, s.out.token, s.out.x, double(kept), dropped);
     }
 }
 
@@ -1595,9 +1614,9 @@ int64_t lay_out(const Plan &p, int64_t n, char *at, Digest &g) {
     g.mass = s.take<double>(n * p.parts);
     g.top = s.take<float>(n * p.parts);
     g.seg = s.take<float>(n * p.parts * kSegs);
-    const int64_t slices = std::min<int64_t>(n * kMostShares, kSlices), slots = std::min<int64_t>(n, kSlices / 2);
-    g.bins = s.take<uint64_t>(slices * kFine);
-    g.members = s.take<unsigned>(slices * kFine);
+    const int64_t slots = std::min<int64_t>(n, kShared);
+    g.bins = s.take<uint64_t>(slots * kFine);
+    g.members = s.take<unsigned>(slots * kFine);
     g.kept = s.take<uint64_t>(slots * kMostParts);
     g.lost = s.take<double>(slots * kMostParts);
     g.list = s.take<uint64_t>(slots * kMembers);
@@ -1686,12 +1705,12 @@ int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_t
             const auto kernel = plan.group == 256 ? small_kernel<T, 256, 8> : plan.own == 8 ? small_kernel<T, kWave, 8> : small_kernel<T, kWave, 4>;
             hipLaunchKernelGGL(kernel, rows, dim3(unsigned(plan.group)), 0, s, x, a);
         } else if (plan.parts) {
-            const int64_t blocks = (n_tokens * plan.parts + 3) / 4;
+            const int64_t blocks = n_tokens * ((plan.parts + 3) / 4);
             hipLaunchKernelGGL(scan_kernel<T>, dim3(unsigned(std::min(blocks, kMaxBlocks))), dim3(256), 0, s, x, a, g);
             hipLaunchKernelGGL(pick_kernel<T>, rows, dim3(kPick), unsigned(plan.parts * kSegBytes), s, x, a, g);
             if (!row_top_k && !row_top_p && !row_min_p && a.top_k == 0 && top_p == 1.0f && min_p == 0.0f)
                 return; // no row is cut off
-            const dim3 wide(unsigned(std::min<int64_t>(n_tokens * kMostShares, kSlices)));
+            const dim3 wide(unsigned(std::min<int64_t>(n_tokens * kMostShares, 2 * kShared)));
             hipLaunchKernelGGL(wide_place_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
             hipLaunchKernelGGL(wide_pick_kernel<T>, wide, dim3(kWide), 0, s, x, a, g);
         } else
