@@ -6,11 +6,11 @@
 // top-k and top-p are both the search for the place in that order where a running count or a running sum of
 // weights reaches a target.
 //
-// Rows of up to 2,048 tokens go to one workgroup (small_kernel), which sorts them. Of longer rows scan_kernel
-// reads every logit once and leaves a digest: the largest logit of every 128, and the largest and the weights of
-// every 2,048. pick_kernel, a workgroup a row, finds from it the few segments that can hold a kept token, sorts
-// their candidates and takes the token; where nothing is cut off, the digest's weights lead to the 2,048 logits that
-// hold it. Rows whose kept tokens are more than its list holds are read again (wide_row).
+// Rows of up to 2,048 tokens go to one workgroup (small_kernel). Of longer rows scan_kernel reads every logit once and
+// leaves a digest: the largest logit of every 128, and the largest and the weights of every 2,048. pick_kernel, a
+// workgroup a row, finds from it the few segments that can hold a kept token, lists their candidates and takes the
+// token; where nothing is cut off, the digest's weights lead to the 2,048 logits that hold it. Rows whose kept tokens are
+// more than its list holds are read twice more, by wide_place_kernel and wide_pick_kernel, up to 16 workgroups to a row.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1098,7 +1098,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
 #pragma unroll
                     for (int k = 0; k < Part<T>::N; ++k)
                         hits |= float(q[j][k]) >= lowest ? 1u << k : 0;
-                    hits &= ~0u << (at[j] - first[j]);
+                    hits &= at[j] - first[j] < Part<T>::N ? ~0u << (at[j] - first[j]) : 0;
                     while (hits) {
                         const int k = __builtin_ctz(hits), to = atomicAdd(&s.n, 1);
                         hits &= hits - 1;
@@ -1272,7 +1272,7 @@ template <typename V> __device__ __forceinline__ V left_at(const V *p) { return 
 __device__ __forceinline__ bool is_last(unsigned *arrived, int shares, WideShared &s) {
     if (shares == 1)
         return true;
-    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0)
         s.last = atomicAdd(arrived, 1u) == unsigned(shares - 1);

@@ -146,6 +146,24 @@ def test_many_equal_logits(T, V, levels):
             _check(T.tree_ens_sample(d.to(_torch_dtype(dtype)), _dev(u), **given), O.sample(x, u, **params), V, (V, levels, dtype, list(params)))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2_049, 2_055, 4_097, 6_143, 6_145, 50_001, 65_537, 65_541])
+def test_candidates_at_the_ends_of_the_row(T, dtype, V):
+    """The likeliest tokens are the row's first and last ones, which share loads and segments with what lies beyond it."""
+    rng = np.random.default_rng(V)
+    n = 12
+    x = rng.normal(0, 1, (n, V))
+    x[:, :9] += 9.0
+    x[:, -9:] += 9.0
+    x[6:, -3:] = 11.5  # equals
+    d = _dev(np.concatenate([x, np.full((n, 5), 30.0)], 1)).to(_torch_dtype(dtype))[:, :V]  # larger ones beyond
+    x, u = d.double().cpu().numpy(), np.concatenate([rng.random(n - 2), [0.0, 1 - 2.0 ** -53]])
+    for params in (dict(), dict(top_k=1), dict(top_k=17), dict(top_k=60), dict(top_p=0.9), dict(min_p=_f32(0.02)),
+                   dict(top_k=V - 3, top_p=_f32(0.95)), dict(top_p=_f32(0.999)), dict(top_k=V - 1)):
+        params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
+        _check(T.tree_ens_sample(d, _dev(u), **params), O.sample(x, u, **params), V, (V, dtype, params))
+
+
 @pytest.mark.parametrize("dtype,n,V", [("bf16", 40, 300), ("f32", 24, 5_000), ("f16", 16, 60_001)])
 def test_parameters_of_each_row(T, dtype, n, V):
     d, x, u = _logits(dtype, n, V, seed=4)
