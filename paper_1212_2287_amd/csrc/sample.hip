@@ -212,6 +212,30 @@ __device__ __forceinline__ uint64_t last_lane(uint64_t v) {
 __device__ __forceinline__ double last_lane(double v) { return __longlong_as_double(last_lane(uint64_t(__double_as_longlong(v)))); }
 template <typename V> __device__ __forceinline__ V wave_sum(V v) { return last_lane(wave_scan(v)); }
 
+// Over the 16 lanes of a row, by rotations of 8, 4, 2 and 1.
+template <int kCtrl> __device__ __forceinline__ int rotated(int v) { return __builtin_amdgcn_mov_dpp(v, kCtrl, 0xf, 0xf, true); }
+template <int kCtrl> __device__ __forceinline__ float rotated(float v) { return __int_as_float(rotated<kCtrl>(__float_as_int(v))); }
+template <int kCtrl> __device__ __forceinline__ double rotated(double v) {
+    return __hiloint2double(rotated<kCtrl>(__double2hiint(v)), rotated<kCtrl>(__double2loint(v)));
+}
+__device__ __forceinline__ float row_max(float v) {
+    v = larger(v, rotated<0x128>(v));
+    v = larger(v, rotated<0x124>(v));
+    v = larger(v, rotated<0x122>(v));
+    return larger(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ double row_sum(double v) {
+    v += rotated<0x128>(v);
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    return v + rotated<0x121>(v);
+}
+// A row's lanes hold the same: the other rows' too.
+__device__ __forceinline__ float of_row(float v, int row) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * row)); }
+__device__ __forceinline__ double of_row(double v, int row) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 16 * row), __builtin_amdgcn_readlane(__double2loint(v), 16 * row));
+}
+
 template <int kCtrl, int kRows = 0xf> __device__ __forceinline__ float moved_larger(float v) {
     return larger(v, __uint_as_float(moved<kCtrl, kRows, true>(__float_as_uint(v))));
 }
@@ -740,14 +764,11 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 #pragma unroll
             for (int k = 1; k < kSome; ++k)
                 top = larger(top, v[i * kSome + k]);
-            top = moved_larger<0x128>(top); // rotations by 8, 4, 2 and 1 among 16 lanes
-            top = moved_larger<0x124>(top);
-            top = moved_larger<0x122>(top);
-            top = moved_larger<0x121>(top);
+            top = row_max(top);
             mine = lane % 16 == i ? top : mine;
             m = larger(m, top);
         }
-        m = wave_max(m);
+        m = larger(larger(of_row(m, 0), of_row(m, 1)), larger(of_row(m, 2), of_row(m, 3)));
         if (lane % 16 < 4)
             g.seg[item * kSegs + lane % 16 * 4 + lane / 16] = mine;
         double mass = 0.0;
@@ -764,9 +785,10 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 #pragma unroll
                 for (int k = 0; k < kN; ++k)
                     mass += double(w.power(v[k]));
-                mass = ldexp(mass, a.shift);
+                mass *= double(int64_t(1) << a.shift);
             }
-            mass = wave_sum(mass);
+            mass = row_sum(mass);
+            mass = (of_row(mass, 0) + of_row(mass, 1)) + (of_row(mass, 2) + of_row(mass, 3));
         }
         if (lane == 0) {
             g.top[item] = m;
