@@ -402,10 +402,11 @@ int tree_ens_policy_workspace(int64_t n_tokens, int64_t n_seqs, int64_t *bytes);
  * log_kept 0; a row with a NaN or +inf, or without a proper scale, token -1, logp and log_kept NaN
  * (tree_ens_token_logp takes -1 for a row that does not count).
  *
- * Weights are whole numbers of 2^-44 (of more from an n_vocab of 2^19 on: their sum stays below 2^63), taken from a
- * double off by at most 2^-39 of it, so sums are exact in whatever order they are taken, and so is what is
- * decided by them: a row's token depends neither on the rows beside it nor on their number. Tokens of less than
- * half a unit are never sampled.
+ * Sums that decide on tokens are of weights from doubles off by at most 2^-39 of themselves, added exactly or in
+ * an order that is the row's own, so a row's token depends neither on the rows beside it nor on their number.
+ * Weights below half of 2^-44 (of more from an n_vocab of 2^19 on: the sums stay below 2^63) count as 0 where
+ * tokens are kept. Weights that top_k and min_p leave out are added in single precision, by themselves: the share
+ * not kept is off by at most 2^-16 of itself, logp and log_kept by as much of that share, however small it is.
  */
 int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
                     int64_t n_vocab, int64_t row_stride, const double *uniform, float scale,
@@ -421,7 +422,8 @@ int tree_ens_sample_workspace(int32_t dtype, int64_t n_tokens, int64_t n_vocab, 
  *
  *   n_tensors   >= 0.
  *   grads       host, [n_tensors] device pointers, each aligned for its type (NULL where the count is 0).
- *   counts      host, int64 [n_tensors]: elements of each, >= 0, one behind the other in memory.
+ *   counts      host, int64 [n_tensors]: elements of each, >= 0, one behind the other in memory; 2^48 at most
+ *               together.
  *   dtypes      host, int32 [n_tensors]: TREE_ENS_F32, TREE_ENS_BF16 or TREE_ENS_F16.
  *   norm        device, float [1]: 0 where there is no element; inf beyond the largest float.
  * The host arrays are read during the call only. A NaN among the elements makes the norm NaN, an infinity
@@ -440,8 +442,8 @@ int tree_ens_grad_norm_workspace(int64_t n_tensors, int64_t *bytes);
  *   max_norm    finite, >= 0; eps finite, >= 0.
  *   out         host, [n_tensors] device pointers to tensors of the same counts and types. Each may be
  *               the one of `grads` itself; otherwise none of them may overlap another of `out` or any of
- *               `grads` (TREE_ENS_E_ARG).
- * Gradients in place are left alone, and not read, where the factor is 1. A NaN norm makes everything NaN; an
+ *               `grads`, or the norm (TREE_ENS_E_ARG).
+ * A norm and an eps of 0 count as a factor of 1. Gradients in place are left alone, and not read, where the factor is 1. A NaN norm makes everything NaN; an
  * infinite one makes finite elements 0 and the others NaN.
  */
 int tree_ens_grad_clip(void *stream, int64_t n_tensors, const void *const *grads, const int64_t *counts,

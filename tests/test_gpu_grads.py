@@ -151,6 +151,31 @@ def test_limits_of_clipping(T):
     assert nothing.item() == 0.0
 
 
+def test_nothing_to_scale_by(T):
+    """No norm, no norm allowed and no eps: 0 over 0 leaves the zeros."""
+    import torch
+    x = [torch.zeros(300, device="cuda"), torch.zeros(7, device="cuda", dtype=torch.bfloat16)]
+    out = T.tree_ens_grad_clip(x, T.tree_ens_grad_norm(x), 0.0, eps=0.0, out=[torch.ones_like(t) for t in x])
+    assert all(torch.equal(o, t) for o, t in zip(out, x))
+
+
+def test_many_workgroups_sums(T):
+    """More launches' sums than the last kernel has threads times loads."""
+    import torch
+    x = torch.from_numpy(np.random.default_rng(3).normal(0, 1, (700, 50_000)).astype(np.float32)).cuda()
+    _check_norm(T.tree_ens_grad_norm(list(x)), x.double().square().sum().sqrt().item())
+
+
+def test_the_norm_is_not_clipped(T):
+    import torch
+    x = torch.ones(100, device="cuda")
+    with pytest.raises(T.TreeEnsError, match="overlaps"):
+        T.tree_ens_grad_clip([x], x[3:4], 1.0)
+    T.tree_ens_grad_clip([x], x[3:4], 1.0, eps=0.0, out=[torch.empty_like(x)])  # read only
+    norm = T.tree_ens_grad_norm([x], norm=x[5:6])  # written behind all reads
+    assert norm.item() == 10.0 and x[5].item() == 10.0 and x.sum().item() == 109.0
+
+
 def test_shapes_and_orders_of_dimensions(T):
     import torch
     g = torch.Generator(device="cuda").manual_seed(0)

@@ -322,6 +322,23 @@ def test_offsets_past_32_bits(T):
         _check(T.tree_ens_sample(d, _dev(u), top_p=_f32(0.9)), O.sample(x.double().numpy(), u, top_p=_f32(0.9)), V, "far rows")
 
 
+@pytest.mark.parametrize("V,more", [(5, dict(top_p=0.9)), (2_055, dict(top_p=0.9)), (2_055, dict(top_p=0.9, spread=0.1)), (2_055, {})],
+                         ids=["short", "listed", "wide", "all"])
+def test_more_rows_than_workgroups(T, V, more):
+    """More rows than a launch has workgroups: the first and the last ones are as in calls of their own."""
+    import torch
+    n, some = (1 << 20) + 77, 60
+    x = torch.empty(n, V, dtype=torch.bfloat16, device="cuda").normal_(0, more.get("spread", 3.0), generator=torch.Generator("cuda").manual_seed(1))
+    u = torch.rand(n, dtype=torch.float64, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    top_p = _f32(more.get("top_p", 1.0))
+    got = T.tree_ens_sample(x, u, top_p=top_p)
+    assert ((got[0] >= 0) & (got[0] < V)).all() and torch.isfinite(got[1]).all() and (got[2] <= 0).all()
+    for rows in (slice(0, some), slice(n - some, n)):
+        part = [g[rows] for g in got]
+        assert all(torch.equal(a, b) for a, b in zip(part, T.tree_ens_sample(x[rows], u[rows], top_p=top_p)))
+        _check(part, O.sample(x[rows].double().cpu().numpy(), u[rows].cpu().numpy(), top_p=top_p), V, "rows in turn")
+
+
 @pytest.mark.parametrize("n,V", [(3, 60_001), (40, 500)])
 def test_captured_into_a_graph(T, n, V):
     import torch

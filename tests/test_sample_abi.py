@@ -123,6 +123,19 @@ def test_grad_clip_refuses_overlaps(lib, items, out):
     _clip(lib, "overlaps", items, out)
 
 
+def test_grad_clip_refuses_the_norm_among_its_results(lib):
+    for norm in (P, P + 4, P + 12):
+        _clip(lib, "overlaps", [(P, 4, 0)], [P], norm=norm)
+        _clip(lib, "overlaps", [(P + 64, 4, 0)], [P], norm=norm)
+
+
+def test_more_elements_than_numbers_hold(lib):
+    many = [(P, 2**47, 0), (P, 2**47, 1), (P, 1, 0)]
+    _norm(lib, "counts", *many)
+    _clip(lib, "counts", many, [P] * 3)
+    _norm(lib, "counts", *[(P, 2**48, 0)] * 9)
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert lib.tree_ens_sample(*{**SAMPLE, "n": 0, "logits": None, "uniform": None, "tokens": None}.values()) == 0
     assert lib.tree_ens_grad_clip(None, 0, None, None, None, None, 1.0, 1e-6, None) == 0
