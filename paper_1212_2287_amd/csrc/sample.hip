@@ -712,10 +712,10 @@ template <typename T> struct Part {
 struct WideRow {
     int64_t row;
     float top, least;
-    uint64_t last;  // the entry of the last kept token, where `bin` is kFine
+    uint64_t last;  // the entry of the last kept token, where `bin` is kNoBin
     uint64_t left;  // otherwise it is in this bin, where the count (by_mass: the weights) reaches this
     int bin, members;
-    bool by_mass;
+    bool by_mass, fine; // fine: the bin is one of kFine of a bin
     unsigned arrived[2], listed;
 };
 
@@ -1203,15 +1203,20 @@ struct WideShared {
     bool last;
 };
 
-// The bin of a logit by its distance from the largest, which never decreases as logits do; kFine: beyond 63 in units of the
+// The bin of a logit by its distance from the largest, which never decreases as logits do; kNoBin: beyond 63 in units of the
 // exponent, where neither what is kept nor what is not is felt any more. Halves, because the distance itself may be no float.
+// Fine ones are kFine to each of the others, exactly, since a power of two scales the distance.
+constexpr int kNoBin = kFine * kFine;
 struct Bins {
-    float half, step;
-    __device__ __forceinline__ Bins(const Row &r)
-        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 63.0f), 3.402823466e38f)) {}
+    float half, step, end;
+    __device__ __forceinline__ Bins(const Row &r, bool fine = false)
+        : half(float(r.m) * 0.5f), step(fminf(float(r.scale) * (2.0f * kFine / 63.0f), 3.402823466e38f)), end(fine ? kFine * kFine : kFine) {
+        step *= fine ? float(kFine) : 1.0f;
+    }
+    __device__ __forceinline__ bool have_fine() const { return step < 0x1p100f; }
     __device__ __forceinline__ int of(float x) const {
         const float d = (half - x * 0.5f) * step;
-        return d < float(kFine) ? int(d) : kFine;
+        return d < end ? int(d) : kNoBin;
     }
 };
 
@@ -1236,16 +1241,17 @@ template <typename T, typename F> __device__ __forceinline__ void for_share(cons
     }
 }
 
-// Counts and weights of a share of the logits in each bin.
+// Counts and weights of a share of the logits in each bin, or in each fine one of a bin, `first` on.
 template <typename T>
-__device__ __forceinline__ void fill_bins(const T *x, int V, int share, int shares, const Row &r, const Bins &bins, float least, WideShared &s) {
+__device__ __forceinline__ void fill_bins(const T *x, int V, int share, int shares, const Row &r, const Bins &bins, int first, float least,
+                                          WideShared &s) {
     __syncthreads();
     for (int i = threadIdx.x; i < kFine; i += kWide)
         s.mass[i] = s.count[i] = 0;
     __syncthreads();
     for_share(x, V, share, shares, [&](float v, int) {
-        const int bin = bins.of(v);
-        if (bin < kFine && v >= least) {
+        const int bin = bins.of(v) - first;
+        if (unsigned(bin) < unsigned(kFine) && v >= least) {
             atomicAdd(&s.count[bin], 1u);
             atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[bin]), (unsigned long long)r.weight(v));
         }
@@ -1285,6 +1291,31 @@ __device__ __forceinline__ int bin_of(bool by_mass, uint64_t target, uint64_t &l
     return s.found;
 }
 
+// The same bin, and where it has more entries than a list the fine one, for which the row is read once more.
+struct Place {
+    uint64_t left, above;
+    int bin, members;
+    bool fine;
+};
+template <typename T>
+__device__ __forceinline__ Place place_in_bins(const T *x, int V, const Row &r, float least, bool by_mass, uint64_t target, WideShared &s) {
+    Place p;
+    p.fine = false;
+    p.bin = bin_of(by_mass, target, p.left, p.above, s);
+    p.members = int(s.count[p.bin]);
+    const Bins bins(r, true);
+    if (p.members > kMembers && bins.have_fine()) {
+        uint64_t above;
+        fill_bins(x, V, 0, 1, r, bins, p.bin * kFine, least, s);
+        const int bin = bin_of(by_mass, p.left, p.left, above, s);
+        p.members = int(s.count[bin]);
+        p.bin = p.bin * kFine + bin;
+        p.above += above;
+        p.fine = true;
+    }
+    return p;
+}
+
 // What workgroups of a row leave for the last of them goes past their caches, each of which belongs to some of them only.
 template <typename V> __device__ __forceinline__ void leave(V *p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename V> __device__ __forceinline__ V left_at(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -1321,11 +1352,11 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
         const float least = w.least;
         const Row r(w.top, p.scale, a.shift);
         const Bins bins(r);
-        uint64_t last = least == -INFINITY ? 0 : entry_of(key_of(least), -1), left = 0, above;
-        int bin = kFine, members = 0;
+        uint64_t last = least == -INFINITY ? 0 : entry_of(key_of(least), -1);
+        Place place{0, 0, kNoBin, 0, false};
         bool by_mass = false;
         if (p.top_k < a.V || p.fraction < kOne) {
-            fill_bins(x, a.V, int(item - slot * shares), shares, r, bins, least, s);
+            fill_bins(x, a.V, int(item - slot * shares), shares, r, bins, 0, least, s);
             if (shares > 1) {
                 uint64_t *all = g.bins + slot * kFine;
                 unsigned *number = g.members + slot * kFine;
@@ -1350,50 +1381,50 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             there = WideBlock::sum(there, s.block);
             inside = WideBlock::sum(inside, s.block);
             const bool cut = uint64_t(p.top_k) < there; // otherwise what it cuts off is beyond the bins
-            if (cut) {
-                bin = bin_of(false, uint64_t(p.top_k), left, above, s);
-                members = int(s.count[bin]);
-            }
+            if (cut)
+                place = place_in_bins(x, a.V, r, least, false, uint64_t(p.top_k), s);
             if (cut && p.fraction < kOne) { // what top_p is a share of has to be known
-                if (members > kMembers)
+                const bool read_again = place.fine || place.members > kMembers;
+                if (place.members > kMembers)
                     last = WideBlock::place_of<false>(x, a.V, r, least, uint64_t(p.top_k), inside, s.mass, s.count, s.block);
                 else {
+                    const Bins fine(r, place.fine);
                     __syncthreads();
                     if (tid == 0)
                         s.n = 0;
                     __syncthreads();
                     for_share(x, a.V, 0, 1, [&](float v, int i) {
-                        if (bins.of(v) == bin && v >= least)
+                        if (fine.of(v) == place.bin && v >= least)
                             s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), i);
                     });
                     __syncthreads();
-                    List<kWide>::find<Order::kLogits>(false, left, s.list, members, 0, 0, 0, r, inside, s.find, s.block);
-                    inside += above;
+                    List<kWide>::find<Order::kLogits>(false, place.left, s.list, place.members, 0, 0, 0, r, inside, s.find, s.block);
+                    inside += place.above;
                     __syncthreads();
                 }
-                if (members > kMembers)
-                    fill_bins(x, a.V, 0, 1, r, bins, least, s);
+                if (read_again)
+                    fill_bins(x, a.V, 0, 1, r, bins, 0, least, s);
             }
             if (p.fraction < kOne) {
                 by_mass = true;
-                bin = bin_of(true, std::max(share_up(inside, p.fraction), uint64_t(1)), left, above, s);
-                members = int(s.count[bin]);
+                place = place_in_bins(x, a.V, r, least, true, std::max(share_up(inside, p.fraction), uint64_t(1)), s);
             }
-            if (members > kMembers) { // a great many near equals
+            if (place.members > kMembers) { // a great many equals, or as good as equal
                 __syncthreads();
                 const uint64_t target = by_mass ? std::max(share_up(inside, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
                 uint64_t unused;
                 last = by_mass ? WideBlock::place_of<true>(x, a.V, r, least, target, unused, s.mass, s.count, s.block)
                                : WideBlock::place_of<false>(x, a.V, r, least, target, unused, s.mass, s.count, s.block);
-                bin = kFine;
+                place.bin = kNoBin;
             }
         }
         if (tid == 0) {
             w.last = last;
-            w.left = left;
-            w.bin = bin;
-            w.members = members;
+            w.left = place.left;
+            w.bin = place.bin;
+            w.members = place.members;
             w.by_mass = by_mass;
+            w.fine = place.fine;
         }
         __syncthreads();
     }
@@ -1417,10 +1448,10 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
         const Params p = params_of(a, row);
         const T *x = logits + row * a.stride;
         const Row r(w.top, p.scale, a.shift);
-        const Bins bins(r);
+        const Bins bins(r, w.fine);
         const float least = w.least;
         const int bin = w.bin;
-        const bool exact = bin == kFine;
+        const bool exact = bin == kNoBin;
         const Last last(w.last);
         uint64_t *list = g.list + slot * kMembers, *kept_of = g.kept + slot * kMostParts; // where the row is shared
         double *lost_of = g.lost + slot * kMostParts;

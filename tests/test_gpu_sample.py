@@ -146,6 +146,21 @@ def test_many_equal_logits(T, V, levels):
             _check(T.tree_ens_sample(d.to(_torch_dtype(dtype)), _dev(u), **given), O.sample(x, u, **params), V, (V, levels, dtype, list(params)))
 
 
+@pytest.mark.parametrize("n", [3, 260])
+@pytest.mark.parametrize("V,spread", [(20_000, 0.001), (70_001, 0.02), (70_001, 0.5), (300_000, 0.2)])
+def test_many_near_equals(T, n, V, spread):
+    """Thousands of logits that differ little around the last kept one, in rows that workgroups share and in more of them."""
+    import torch
+    x = torch.empty(n, V, device="cuda").normal_(0, spread, generator=torch.Generator("cuda").manual_seed(V))
+    u = torch.rand(n, dtype=torch.float64, device="cuda", generator=torch.Generator("cuda").manual_seed(n))
+    some = [0, n // 2, n - 1]
+    for more in (dict(top_p=_f32(0.4)), dict(top_k=V // 2), dict(top_k=V // 3, top_p=_f32(0.6)), dict(top_k=V // 3, min_p=_f32(0.9)),
+                 dict(top_p=_f32(0.5), min_p=_f32(0.5))):
+        got = T.tree_ens_sample(x, u, **more)
+        want = O.sample(x[some].double().cpu().numpy(), u[some].cpu().numpy(), **more)
+        _check([g[some] for g in got], want, V, more)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [2_049, 2_055, 4_097, 6_143, 6_145, 50_001, 65_537, 65_541])
 def test_candidates_at_the_ends_of_the_row(T, dtype, V):
