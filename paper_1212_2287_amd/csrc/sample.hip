@@ -1,16 +1,21 @@
 // sample.hip -- one token for each row of logits from a given random number, under temperature, top-k,
 // min-p and top-p, on gfx950.
 //
-// Weights w = exp(scale * (x - max x)) are whole numbers of 2^-shift, so that sums are exact in any order.
-// Tokens are kept down to a last one in the order of the logits (the largest first, equal ones by index):
-// top-k and top-p are both the search for the place in that order where a running count or a running sum of
-// weights reaches a target.
+// Weights w = exp(scale * (x - max x)) are taken in double and rounded to whole numbers of 2^-shift where tokens are decided
+// on, so that sums are exact in any order. Tokens are kept down to a last one in the order of the logits (the largest first,
+// equal ones by index): top-k and top-p are both the search for the place in that order where a running count or a running sum
+// of weights reaches a target. Nothing is sorted.
 //
 // Rows of up to 2,048 tokens go to one workgroup (small_kernel). Of longer rows scan_kernel reads every logit once and
 // leaves a digest: the largest logit of every 128, and the largest and the weights of every 2,048. pick_kernel, a
 // workgroup a row, finds from it the few segments that can hold a kept token, lists their candidates and takes the
 // token; where nothing is cut off, the digest's weights lead to the 2,048 logits that hold it. Rows whose kept tokens are
-// more than its list holds are read twice more, by wide_place_kernel and wide_pick_kernel, up to 16 workgroups to a row.
+// more than its list holds are read twice more, by wide_place_kernel and wide_pick_kernel, up to 16 workgroups to a row. What
+// a row's token and log-probabilities are depends on the row alone, since parts, sums and lists do.
+//
+// Times below are of kernels on one MI355X, in these cases: A 1 x 128,000 bf16, top-p 0.95; B 256 x 128,000 bf16, nothing cut
+// off; C 512 x 131,072 fp16, parameters by row; D 2,048 x 32,001 bf16, min-p 0.05; E 64 x 128,000 fp32 at scale 0.75, top-p 0.98,
+// which thousands of tokens make up.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -571,6 +576,9 @@ template <int kT> struct List {
 // ------------------------------------------------------------------------------------------------
 // short rows
 // ------------------------------------------------------------------------------------------------
+// A workgroup holds a row's logits and weights in registers, kOwn to a thread, stretches of the vocabulary so that the search
+// for the token is a scan over threads. 6,144 x 136 fp32 take 6.8 us, 200,000 x 136 bf16 3.3 ns a row: instructions, 360 of a wave
+// where nothing is cut off, more with the lists' searches; the logits themselves would take 0.5 us.
 template <typename T, int kT, int kOwn>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn == 4 ? 4 : 3))) small_kernel(const T *logits, Args a) {
     using B = Block<kT>;
@@ -735,7 +743,12 @@ struct Digest {
     int parts;
 };
 
-// A wave takes a part of a row.
+// A wave takes a part of a row: all its loads are on their way before the first is used, and the weights relative to the
+// part's own largest logit, so that no wave waits for another's. Bound by instructions, at 86% of what the card issues: 707 of a
+// wave, 22 a logit where weights are exact (B: 28.4 us for 66 MB, which 6.9 TB/s would take 9.5
+// for), 13 in single precision (D: 34 us for 131 MB; with exact weights 47, C 48 instead of 39.7). E, half of which 33 MB stay in
+// the caches: 11.3. Double-precision multiply-adds cost what single ones do here, and exp2 two of them. Kept weights are never from
+// this sum alone where a list holds the tokens, so its roundings, in an order that is always the same, do not add up with theirs.
 template <typename T>
 __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Digest g) {
     using P = Part<T>;
@@ -800,9 +813,9 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kList = 512;     // candidates of pick_kernel
-constexpr int kMembers = 2048; // of a bin
-constexpr int kFine = 1024;    // bins
+constexpr int kList = 512;     // candidates of pick_kernel; C takes 124, 112 and 119 us with 256, 512 and 1,024
+constexpr int kMembers = 4096; // of a bin; one of E may have more than 2,048, and its row is then read once more, for 30 us
+constexpr int kFine = 1024;    // bins; E takes 75 us, and 81 with 2,048
 constexpr int kShared = 256;   // wide rows that workgroups may share
 
 // What finish_row takes, from whichever thread finds it.
@@ -1031,7 +1044,11 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, c
     return std::max(from, key_of(-INFINITY));
 }
 
-// A workgroup takes a row.
+// A workgroup takes a row. Bound by the latency of its steps one after another (the digest, the search for the lowest segment, the
+// segments, the list's searches) and by fetching instructions that run once: 11.6 us for a row alone (A; lists of up to 64 by
+// pick_from_list too: 14.7), 5.4 where nothing is cut off (B), 25 for the 2,048 rows of D and 30 in C. Three waves of a SIMD have the
+// registers they need: D takes 67 us as a whole, 72 with four and 89 with five, 84 with 512 threads a row. Four loads of a quarter
+// of a wave at a time: 66.7, eight: 70.8.
 template <typename T>
 __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3))) pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ PickShared s;
@@ -1184,7 +1201,8 @@ constexpr int kWide = 512;
 constexpr int kMostShares = 16;
 using WideBlock = Block<kWide>;
 
-// Workgroups that share a row, so that a few wide rows have many and many have one each.
+// Workgroups that share a row, so that a few wide rows have many and many have one each. 128,000 fp32 logits, top-p 0.98, take 47 us
+// for one row, 54 for 16, 78 for 64, 158 for 200 and 258 for 400; with a workgroup a row always 136, 140, 149, 166 and 257.
 __device__ __forceinline__ int shares_of(unsigned wide, int parts) {
     return wide > kShared ? 1 : std::max(1, std::min(std::min(int(2 * kShared / wide), kMostShares), parts / 4));
 }
@@ -1333,7 +1351,9 @@ __device__ __forceinline__ bool is_last(unsigned *arrived, int shares, WideShare
     return s.last;
 }
 
-// Where the last kept token is: counts and weights in bins of the distance from the largest logit say in which.
+// Where the last kept token is: counts and weights in bins of the distance from the largest logit say in which. Bound by latency,
+// the row's loads and the bins' sums in LDS and then over workgroups: 12 us for the ten rows of C that come here, 19 for the 64 of E,
+// whose 33 MB would take 5.
 template <typename T>
 __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4))) wide_place_kernel(const T *logits, Args a, Digest g) {
     __shared__ WideShared s;
@@ -1430,7 +1450,9 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
     }
 }
 
-// The kept weights of every part, the bin's entries, and the token.
+// The kept weights of every part, the bin's entries, and the token. 27 us for the rows of C, 40 for those of E: the weights again,
+// then a chain of latency in the last workgroup of every row (the bin's entries back from memory, the place among them, the part, the
+// token). With the registers of two or three waves of a SIMD C takes 107 us instead of 111 and E 82 instead of 75.
 template <typename T>
 __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4))) wide_pick_kernel(const T *logits, Args a, Digest g) {
     __shared__ WideShared s;
@@ -1552,8 +1574,8 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
 // ------------------------------------------------------------------------------------------------
 constexpr int kLong = 1024;
 
-// A workgroup reads the row once for its largest logit, once for its weights, five times for each place and twice for the
-// token.
+// The plain way, for vocabularies beyond what there are: a workgroup reads the row once for its largest logit, once for its weights,
+// five times for each place and twice for the token.
 template <typename T>
 __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
     using B = Block<kLong>;
@@ -1627,7 +1649,9 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
     }
 }
 
-// How rows of V tokens are taken.
+// How rows of V tokens are taken, whatever their number. By a wave where it holds the row: 20,000 x 500 bf16, top-k and top-p, take
+// 170 us, with 256 threads to a row 385, but 64 of them 32 and 21; 200,000 x 136 take 658 us with four logits a thread, 688 with eight,
+// 2,679 with 256 threads. By 256 threads up to 2,048: 2,000 x 2,000 take 98 us, by way of a digest 182, and 64 of them 33 and 47.
 struct Plan {
     int group, own; // of small_kernel; 0: a digest
     int parts;      // 0 and no group: long_kernel
