@@ -485,9 +485,16 @@ template <int kT> struct Block {
 // ------------------------------------------------------------------------------------------------
 enum class Order { kLogits, kVocabulary };
 
-// An entry as the order has it, the first one the largest: by index where the halves are changed over.
-template <Order kOrder> __device__ __forceinline__ uint64_t ordered(uint64_t entry) {
-    return kOrder == Order::kLogits ? entry : entry << 32 | entry >> 32;
+// An entry as the order has it, the first one the largest, without the bits that all entries of lists have alike: those of indexes
+// beyond 2^19, and of keys those that T has not. The fewer steps a search takes: the two of 240 fp16
+// candidates, many of them equal, 4 us instead of up to 11, and C 105 us instead of 113.
+constexpr int kIndexBits = 19;
+template <typename T> constexpr int kKeyDrop = 0;
+template <> constexpr int kKeyDrop<__bf16> = 16;
+template <> constexpr int kKeyDrop<_Float16> = 13;
+template <Order kOrder, typename T> __device__ __forceinline__ uint64_t ordered(uint64_t entry) {
+    const uint64_t index = entry & ((1u << kIndexBits) - 1);
+    return kOrder == Order::kLogits ? entry >> (32 + kKeyDrop<T>) << kIndexBits | index : index;
 }
 
 template <int kT> struct List {
@@ -502,9 +509,9 @@ template <int kT> struct List {
 
     // The entry of list[0, n) at which the count (by_mass: the weights) of those of at least `least` reaches `target`, which it
     // does; `inside` receives the weights down to it. By bins of the range that the entries have, as many as there are
-    // threads, and then of the range of the bin that holds it, until it is alone: two or three times, whatever the entries.
+    // threads, and then of the range of the bin that holds it, until it is alone.
     // `high` and `low`: bounds of the entries as the order has them, or 0 and 0.
-    template <Order kOrder>
+    template <Order kOrder, typename T>
     static __device__ __forceinline__ uint64_t find(bool by_mass, uint64_t target, const uint64_t *list, int n, uint64_t least, uint64_t high,
                                                     uint64_t low, const Row &r, uint64_t &inside, Shared &s, typename B::Shared &block) {
         const int tid = threadIdx.x;
@@ -512,8 +519,8 @@ template <int kT> struct List {
             low = ~uint64_t(0);
             for (int i = tid; i < n; i += kT)
                 if (list[i] >= least) {
-                    high = std::max(high, ordered<kOrder>(list[i]));
-                    low = std::min(low, ordered<kOrder>(list[i]));
+                    high = std::max(high, ordered<kOrder, T>(list[i]));
+                    low = std::min(low, ordered<kOrder, T>(list[i]));
                 }
             high = wave_max(high);
             low = ~wave_max(~low);
@@ -538,7 +545,7 @@ template <int kT> struct List {
             s.mass[tid] = s.count[tid] = 0;
             __syncthreads();
             for (int i = tid; i < n; i += kT) {
-                const uint64_t e = ordered<kOrder>(list[i]);
+                const uint64_t e = ordered<kOrder, T>(list[i]);
                 if (list[i] >= least && e <= high && e >= low) {
                     const int bin = int((high - e) >> shift);
                     atomicAdd(&s.count[bin], 1u);
@@ -566,7 +573,7 @@ template <int kT> struct List {
             }
         }
         for (int i = tid; i < n; i += kT)
-            if (list[i] >= least && ordered<kOrder>(list[i]) <= high && ordered<kOrder>(list[i]) >= low)
+            if (list[i] >= least && ordered<kOrder, T>(list[i]) <= high && ordered<kOrder, T>(list[i]) >= low)
                 s.entry = list[i];
         __syncthreads();
         return s.entry;
@@ -623,10 +630,10 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
             there = B::sum(there, s);
             __syncthreads();
             if (uint64_t(p.top_k) < there)
-                lowest = L::template find<Order::kLogits>(false, uint64_t(p.top_k), list, a.V, lowest, 0, 0, r, inside, find, s);
+                lowest = L::template find<Order::kLogits, T>(false, uint64_t(p.top_k), list, a.V, lowest, 0, 0, r, inside, find, s);
             uint64_t unused;
             if (p.fraction < kOne)
-                lowest = L::template find<Order::kLogits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, 0, 0, r, unused, find, s);
+                lowest = L::template find<Order::kLogits, T>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, 0, 0, r, unused, find, s);
         }
         uint64_t mine = 0;
         double lost = 0.0;
@@ -664,7 +671,7 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
 // the digest of a row
 // ------------------------------------------------------------------------------------------------
 constexpr int kPart = 2048, kSeg = 128, kSegs = kPart / kSeg;
-constexpr int kMostParts = (1 << 19) / kPart; // longer rows go to long_kernel
+constexpr int kMostParts = (1 << kIndexBits) / kPart; // longer rows go to long_kernel
 
 // 16 bytes of logits. A row may start anywhere, so what it is read through claims no alignment.
 template <typename T> struct Vec {
@@ -813,7 +820,7 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kList = 512;     // candidates of pick_kernel; C takes 124, 112 and 119 us with 256, 512 and 1,024
+constexpr int kList = 512;     // candidates of pick_kernel; C took 124, 112 and 119 us with 256, 512 and 1,024
 constexpr int kMembers = 4096; // of a bin; one of E may have more than 2,048, and its row is then read once more, for 30 us
 constexpr int kFine = 1024;    // bins; E takes 75 us, and 81 with 2,048
 constexpr int kShared = 256;   // wide rows that workgroups may share
@@ -914,6 +921,7 @@ template <typename F> __device__ __forceinline__ void for_entries(const PickShar
 // The token from s.list[0, n), which holds every token down to some place of the order. `whole`: all that min_p and top_k
 // leave is among them; otherwise `total` is the weight of all that top_p is a share of. `rest`: the weights of the tokens
 // beyond the list. False where the list ends before the last kept token does.
+template <typename T>
 __device__ __forceinline__ bool pick_from_list(const Args &a, const Row &r, const Params &p, uint32_t low, int n, bool whole, uint64_t total,
                                                double rest, PickShared &s) {
     using L = List<kPick>;
@@ -928,7 +936,8 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, const Row &r, cons
         const uint64_t target = pass ? std::max(share_up(whole ? kept : total, p.fraction), uint64_t(1)) : uint64_t(p.top_k);
         if (pass && kept < target)
             return false;
-        end = L::find<Order::kLogits>(pass, target, s.list, n, end, entry_of(key_of(float(r.m)), 0), entry_of(low, -1), r, kept, s.find,
+        end = L::find<Order::kLogits, T>(pass, target, s.list, n, end, ordered<Order::kLogits, T>(entry_of(key_of(float(r.m)), 0)),
+                                         ordered<Order::kLogits, T>(entry_of(low, -1)), r, kept, s.find,
                                       s.block);
     }
     Fine lost;
@@ -939,8 +948,8 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, const Row &r, cons
         lost = PickBlock::sum(lost, s.block);
     }
     // sums are whole numbers: past the random share of them is to reach the next one
-    const uint64_t token = L::find<Order::kVocabulary>(true, share_down(kept, p.at) + 1, s.list, n, end, ~uint64_t(0),
-                                                              ordered<Order::kVocabulary>(entry_of(0, a.V - 1)), r, unused, s.find, s.block);
+    const uint64_t token = L::find<Order::kVocabulary, T>(true, share_down(kept, p.at) + 1, s.list, n, end, ordered<Order::kVocabulary, T>(entry_of(0, 0)),
+                                                              ordered<Order::kVocabulary, T>(entry_of(0, a.V - 1)), r, unused, s.find, s.block);
     if (threadIdx.x == 0)
         s.out = {index_of(token), float_of(key_in(token)), double(kept), rest + lost.units(r.shift)};
     return true;
@@ -1046,7 +1055,7 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, c
 
 // A workgroup takes a row. Bound by the latency of its steps one after another (the digest, the search for the lowest segment, the
 // segments, the list's searches) and by fetching instructions that run once: 11.6 us for a row alone (A; lists of up to 64 by
-// pick_from_list too: 14.7), 5.4 where nothing is cut off (B), 25 for the 2,048 rows of D and 30 in C. Three waves of a SIMD have the
+// pick_from_list too: 14.7), 5.4 where nothing is cut off (B), 25 for the 2,048 rows of D and in C. Three waves of a SIMD have the
 // registers they need: D takes 67 us as a whole, 72 with four and 89 with five, 84 with 512 threads a row. Four loads of a quarter
 // of a wave at a time: 66.7, eight: 70.8.
 template <typename T>
@@ -1118,7 +1127,8 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
                 if (keys[i] >= low)
                     some[atomicAdd(&s.found, 1)] = uint16_t(i);
             __syncthreads();
-            const int many = s.found;
+            const int many = s.found <= kList ? s.found : 0; // each has a candidate: of more there is no list
+            wide = s.found > kList;
             const float lowest = float_of(low);
             constexpr int kLoads = 4; // of a quarter of a wave on their way at a time
             for (int i = tid / 16; i < many; i += kPick / 16 * (kLoads / Part<T>::kSame)) {
@@ -1148,7 +1158,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             }
             __syncthreads();
             const int n = s.n;
-            wide = n > kList;
+            wide = wide || n > kList;
             double rest = 0.0;
             if (!wide && wants_logp(a)) {
                 // what a part has beside the list's tokens, whose weights are those that its sum was made of: what is left of
@@ -1171,7 +1181,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             if (!wide && n <= kWave)
                 wide = __syncthreads_or(tid < kWave && !pick_from_few(a, r, p, n, whole, total, rest, s));
             else if (!wide)
-                wide = !pick_from_list(a, r, p, low, n, whole, total, rest, s);
+                wide = !pick_from_list<T>(a, r, p, low, n, whole, total, rest, s);
         }
         __syncthreads();
         if (!wide) {
@@ -1418,7 +1428,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                             s.list[atomicAdd(&s.n, 1)] = entry_of(key_of(v), i);
                     });
                     __syncthreads();
-                    List<kWide>::find<Order::kLogits>(false, place.left, s.list, place.members, 0, 0, 0, r, inside, s.find, s.block);
+                    List<kWide>::find<Order::kLogits, T>(false, place.left, s.list, place.members, 0, 0, 0, r, inside, s.find, s.block);
                     inside += place.above;
                     __syncthreads();
                 }
@@ -1450,9 +1460,9 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
     }
 }
 
-// The kept weights of every part, the bin's entries, and the token. 27 us for the rows of C, 40 for those of E: the weights again,
+// The kept weights of every part, the bin's entries, and the token. 25 us for the rows of C, 40 for those of E: the weights again,
 // then a chain of latency in the last workgroup of every row (the bin's entries back from memory, the place among them, the part, the
-// token). With the registers of two or three waves of a SIMD C takes 107 us instead of 111 and E 82 instead of 75. Four
+// token). With the registers of two or three waves of a SIMD C took 107 us instead of 111 and E 82 instead of 75. Four
 // loads at a time instead of a part's eight: E 74 instead of 76.
 template <typename T>
 __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4))) wide_pick_kernel(const T *logits, Args a, Digest g) {
@@ -1546,7 +1556,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                     s.list[i] = left_at(list + i);
             uint64_t unused;
             __syncthreads();
-            end = List<kWide>::find<Order::kLogits>(w.by_mass, w.left, s.list, n, 0, 0, 0, r, unused, s.find, s.block);
+            end = List<kWide>::find<Order::kLogits, T>(w.by_mass, w.left, s.list, n, 0, 0, 0, r, unused, s.find, s.block);
             for (int i = tid; i < n; i += kWide) {
                 const uint64_t e = s.list[i];
                 if (e >= end)
