@@ -486,15 +486,15 @@ template <int kT> struct Block {
 enum class Order { kLogits, kVocabulary };
 
 // An entry as the order has it, the first one the largest, without the bits that all entries of lists have alike: those of indexes
-// beyond 2^19, and of keys those that T has not. The fewer steps a search takes: the two of 240 fp16
+// beyond 2^kBits, and of keys those that T has not. The fewer steps a search takes: the two of 240 fp16
 // candidates, many of them equal, 4 us instead of up to 11, and C 105 us instead of 113.
 constexpr int kIndexBits = 19;
 template <typename T> constexpr int kKeyDrop = 0;
 template <> constexpr int kKeyDrop<__bf16> = 16;
 template <> constexpr int kKeyDrop<_Float16> = 13;
-template <Order kOrder, typename T> __device__ __forceinline__ uint64_t ordered(uint64_t entry) {
-    const uint64_t index = entry & ((1u << kIndexBits) - 1);
-    return kOrder == Order::kLogits ? entry >> (32 + kKeyDrop<T>) << kIndexBits | index : index;
+template <Order kOrder, typename T, int kBits = kIndexBits> __device__ __forceinline__ uint64_t ordered(uint64_t entry) {
+    const uint64_t index = entry & ((1u << kBits) - 1);
+    return kOrder == Order::kLogits ? entry >> (32 + kKeyDrop<T>) << kBits | index : index;
 }
 
 template <int kT> struct List {
@@ -511,7 +511,7 @@ template <int kT> struct List {
     // does; `inside` receives the weights down to it. By bins of the range that the entries have, as many as there are
     // threads, and then of the range of the bin that holds it, until it is alone.
     // `high` and `low`: bounds of the entries as the order has them, or 0 and 0.
-    template <Order kOrder, typename T>
+    template <Order kOrder, typename T, int kBits = kIndexBits>
     static __device__ __forceinline__ uint64_t find(bool by_mass, uint64_t target, const uint64_t *list, int n, uint64_t least, uint64_t high,
                                                     uint64_t low, const Row &r, uint64_t &inside, Shared &s, typename B::Shared &block) {
         const int tid = threadIdx.x;
@@ -519,8 +519,8 @@ template <int kT> struct List {
             low = ~uint64_t(0);
             for (int i = tid; i < n; i += kT)
                 if (list[i] >= least) {
-                    high = std::max(high, ordered<kOrder, T>(list[i]));
-                    low = std::min(low, ordered<kOrder, T>(list[i]));
+                    high = std::max(high, ordered<kOrder, T, kBits>(list[i]));
+                    low = std::min(low, ordered<kOrder, T, kBits>(list[i]));
                 }
             high = wave_max(high);
             low = ~wave_max(~low);
@@ -545,7 +545,7 @@ template <int kT> struct List {
             s.mass[tid] = s.count[tid] = 0;
             __syncthreads();
             for (int i = tid; i < n; i += kT) {
-                const uint64_t e = ordered<kOrder, T>(list[i]);
+                const uint64_t e = ordered<kOrder, T, kBits>(list[i]);
                 if (list[i] >= least && e <= high && e >= low) {
                     const int bin = int((high - e) >> shift);
                     atomicAdd(&s.count[bin], 1u);
@@ -573,7 +573,7 @@ template <int kT> struct List {
             }
         }
         for (int i = tid; i < n; i += kT)
-            if (list[i] >= least && ordered<kOrder, T>(list[i]) <= high && ordered<kOrder, T>(list[i]) >= low)
+            if (list[i] >= least && ordered<kOrder, T, kBits>(list[i]) <= high && ordered<kOrder, T, kBits>(list[i]) >= low)
                 s.entry = list[i];
         __syncthreads();
         return s.entry;
@@ -584,12 +584,13 @@ template <int kT> struct List {
 // short rows
 // ------------------------------------------------------------------------------------------------
 // A workgroup holds a row's logits and weights in registers, kOwn to a thread, stretches of the vocabulary so that the search
-// for the token is a scan over threads. 6,144 x 136 fp32 take 6.8 us, 200,000 x 136 bf16 3.3 ns a row: instructions, 360 of a wave
+// for the token is a scan over threads. 6,144 x 136 fp32 take 6.8 us, 200,000 x 136 bf16 with top-k and top-p 3.0 ns a row: instructions, 360 of a wave
 // where nothing is cut off, more with the lists' searches; the logits themselves would take 0.5 us.
 template <typename T, int kT, int kOwn>
 __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn == 4 ? 4 : 3))) small_kernel(const T *logits, Args a) {
     using B = Block<kT>;
     using L = List<kT>;
+    constexpr int kBits = 31 - __builtin_clz(kOwn * kT); // of an index
     __shared__ typename B::Shared s;
     __shared__ typename L::Shared find;
     __shared__ uint64_t list[kOwn * kT];
@@ -630,10 +631,10 @@ __global__ void __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(kOwn ==
             there = B::sum(there, s);
             __syncthreads();
             if (uint64_t(p.top_k) < there)
-                lowest = L::template find<Order::kLogits, T>(false, uint64_t(p.top_k), list, a.V, lowest, 0, 0, r, inside, find, s);
+                lowest = L::template find<Order::kLogits, T, kBits>(false, uint64_t(p.top_k), list, a.V, lowest, 0, 0, r, inside, find, s);
             uint64_t unused;
             if (p.fraction < kOne)
-                lowest = L::template find<Order::kLogits, T>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, 0, 0, r, unused, find, s);
+                lowest = L::template find<Order::kLogits, T, kBits>(true, std::max(share_up(inside, p.fraction), uint64_t(1)), list, a.V, lowest, 0, 0, r, unused, find, s);
         }
         uint64_t mine = 0;
         double lost = 0.0;
@@ -1211,8 +1212,8 @@ constexpr int kWide = 512;
 constexpr int kMostShares = 16;
 using WideBlock = Block<kWide>;
 
-// Workgroups that share a row, so that a few wide rows have many and many have one each. 128,000 fp32 logits, top-p 0.98, take 47 us
-// for one row, 54 for 16, 78 for 64, 158 for 200 and 258 for 400; with a workgroup a row always 136, 140, 149, 166 and 257.
+// Workgroups that share a row, so that a few wide rows have many and many have one each. 128,000 fp32 logits, top-p 0.98, take 46 us
+// for one row, 52 for 16, 76 for 64, 156 for 200 and 256 for 400; with a workgroup a row always 135, 139, 150, 166 and 255.
 __device__ __forceinline__ int shares_of(unsigned wide, int parts) {
     return wide > kShared ? 1 : std::max(1, std::min(std::min(int(2 * kShared / wide), kMostShares), parts / 4));
 }
@@ -1665,8 +1666,8 @@ __global__ void __launch_bounds__(kLong) long_kernel(const T *logits, Args a) {
 }
 
 // How rows of V tokens are taken, whatever their number. By a wave where it holds the row: 20,000 x 500 bf16, top-k and top-p, take
-// 170 us, with 256 threads to a row 385, but 64 of them 32 and 21; 200,000 x 136 take 658 us with four logits a thread, 688 with eight,
-// 2,679 with 256 threads. By 256 threads up to 2,048: 2,000 x 2,000 take 98 us, by way of a digest 182, and 64 of them 33 and 47.
+// 136 us, with 256 threads to a row 307, but 64 of them 19 and 14; 200,000 x 136 take 602 us with four logits a thread, 631 with eight,
+// 2,412 with 256 threads. By 256 threads up to 2,048: 2,000 x 2,000 take 69 us, by way of a digest 155, and 64 of them 21 and 39.
 struct Plan {
     int group, own; // of small_kernel; 0: a digest
     int parts;      // 0 and no group: long_kernel
