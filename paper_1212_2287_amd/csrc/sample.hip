@@ -294,15 +294,17 @@ struct Fine {
 
 // Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts.
 struct Quick {
-    float m, c, rest;
+    float m, c, rest, far;
     __device__ __forceinline__ Quick(float top, double scale) : m(top) {
         const double exact = scale * kLog2e;
         c = float(fmin(exact, 3.402823466e38));
         rest = float(exact - double(c));
         rest = exact > 3.402823466e38 ? 0.0f : rest;
+        far = float(fmax(-200.0 * __builtin_amdgcn_rcp(exact), -3.402823466e38));
     }
+    // Distances beyond `far`, masked logits' too, count as 0: a product of theirs alone may be infinite, with the sign of `rest`.
     __device__ __forceinline__ float power(float x) const {
-        const float d = fmaxf(x - m, -3.402823466e38f); // masked logits too: times 0 they would be NaN
+        const float d = fmaxf(x - m, far);
         return __builtin_amdgcn_exp2f(fmaf(d, c, d * rest));
     }
 };

@@ -440,3 +440,25 @@ def test_argument_errors(T):
     tokens, logp, log_kept = T.tree_ens_sample(torch.empty(0, 8, device="cuda"), u[:0])
     assert tokens.shape == logp.shape == log_kept.shape == (0,)
     assert (T.tree_ens_sample(d, u, top_k=2**40)[0] == T.tree_ens_sample(d, u)[0]).all()
+
+
+LARGE = [dict(top_k=1), dict(top_k=40), dict(min_p=0.05), dict(top_k=40, top_p=0.75), dict(top_p=0.5)]
+
+
+@pytest.mark.parametrize("V", [3_000, 9_001, 40_001])
+@pytest.mark.parametrize("scale", [7e7, 1e10, 1e12, 1e30])
+def test_masked_logits_under_large_scales(T, scale, V):
+    """Logits some 1 / scale apart, beside others (and ends of rows) whose distance is no float once it is scaled."""
+    import torch
+    scale, rng, n = _f32(scale), np.random.default_rng(V), 7
+    x = rng.normal(0, 2, (n, V)) / scale
+    x[1:3, rng.random(V) < 0.3] = -np.inf
+    x[3:5, rng.random(V) < 0.3] = torch.finfo(torch.float32).min
+    x[5] = -1.0
+    x[5, [0, V - 1]] = 0.0, -0.7 / scale
+    x[6] = -np.inf
+    x[6, [1, V // 2, V - 2]] = 0.0, -0.7 / scale, -1.5 / scale
+    x, u = x.astype(np.float32), rng.random(n)
+    for params in [*LARGE, dict(top_k=V // 2)]:
+        params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
+        _check(T.tree_ens_sample(_dev(x), _dev(u), scale=scale, **params), O.sample(x, u, scale, **params), V, (scale, params))
