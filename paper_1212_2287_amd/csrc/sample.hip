@@ -99,8 +99,9 @@ enum class Mass { kNone, kExact, kQuick };
 __device__ __forceinline__ Mass mass_of(const Args &a, int64_t row) {
     if (top_k_of(a, row) == a.V && !(min_p_of(a, row) > 0.0f))
         return Mass::kExact;
-    // below this scale a distance that is no float could have a weight
-    return !wants_logp(a) ? Mass::kNone : scale_of(a, row) < 0x1p-100 ? Mass::kExact : Mass::kQuick;
+    // below the one scale a distance that is no float could have a weight, beyond the other the exponents' factor is none
+    const unsigned exponent = __float_as_uint(float(scale_of(a, row))) >> 23;
+    return !wants_logp(a) ? Mass::kNone : exponent < 127 - 100 || exponent >= 127 + 100 ? Mass::kExact : Mass::kQuick;
 }
 
 __device__ __forceinline__ Params params_of(const Args &a, int64_t row) {
@@ -293,14 +294,14 @@ struct Fine {
 };
 
 // Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts.
+// For scales of 2^-100 to 2^100.
 struct Quick {
     float m, c, rest, far;
     __device__ __forceinline__ Quick(float top, double scale) : m(top) {
         const double exact = scale * kLog2e;
-        c = float(fmin(exact, 3.402823466e38));
+        c = float(exact);
         rest = float(exact - double(c));
-        rest = exact > 3.402823466e38 ? 0.0f : rest;
-        far = float(fmax(-200.0 * __builtin_amdgcn_rcp(exact), -3.402823466e38));
+        far = float(-200.0 * __builtin_amdgcn_rcp(exact));
     }
     // Distances beyond `far`, masked logits' too, count as 0: a product of theirs alone may be infinite, with the sign of `rest`.
     __device__ __forceinline__ float power(float x) const {

@@ -462,3 +462,17 @@ def test_masked_logits_under_large_scales(T, scale, V):
     for params in [*LARGE, dict(top_k=V // 2)]:
         params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
         _check(T.tree_ens_sample(_dev(x), _dev(u), scale=scale, **params), O.sample(x, u, scale, **params), V, (scale, params))
+
+
+@pytest.mark.parametrize("V", [700, 3_000, 9_001])
+@pytest.mark.parametrize("scale", [1e38, 2.4e38, 3.4e38])
+def test_scales_up_to_the_largest(T, scale, V):
+    """Scales that the exponential's base makes too large for a float, on logits that are subnormal."""
+    scale, rng, n = _f32(scale), np.random.default_rng(V), 4
+    x = rng.normal(0, 2, (n, V)) / scale
+    x[1, rng.random(V) < 0.3] = -np.inf
+    x[2:, V // 2:] = -1.0
+    x, u = x.astype(np.float32), rng.random(n)
+    for params in [*LARGE, dict(top_k=V // 2)]:
+        params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
+        _check(T.tree_ens_sample(_dev(x), _dev(u), scale=scale, **params), O.sample(x, u, scale, **params), V, (scale, params))
