@@ -274,8 +274,8 @@ struct Row {
     double m, scale, c, far;
     int shift;
     __device__ __forceinline__ Row(float top, double scale_, int shift_)
-        : m(double(top)), scale(scale_), c(scale_ * kLog2e), far(-64.0 * __builtin_amdgcn_rcp(scale_)), shift(shift_) {}
-    // The weight in units, not rounded. Masked logits are taken at `far`, where it is less than half of one.
+        : m(double(top)), scale(scale_), c(scale_ * kLog2e), far(-128.0 * __builtin_amdgcn_rcp(scale_)), shift(shift_) {}
+    // The weight in units, not rounded. Masked logits are taken at `far`: 2^31 times e^-128 is still nothing to the smallest float.
     __device__ __forceinline__ double power(float x) const { return power_of(fmax(double(x) - m, far), c, shift); }
     __device__ __forceinline__ double share(float x) const { return power_of(fmax(double(x) - m, far), c, 0); } // of the largest
     __device__ __forceinline__ uint64_t weight(float x) const { return whole_of(power(x)); }

@@ -476,3 +476,31 @@ def test_scales_up_to_the_largest(T, scale, V):
     for params in [*LARGE, dict(top_k=V // 2)]:
         params = {k: v if k == "top_k" else _f32(v) for k, v in params.items()}
         _check(T.tree_ens_sample(_dev(x), _dev(u), scale=scale, **params), O.sample(x, u, scale, **params), V, (scale, params))
+
+
+def _check_shares(got, want, V, quick, what):
+    """log_kept in proportion to the share D that is not kept, however small: the weights' and sums' errors twice (in D and in
+    the total), 152 u where single precision adds what is dropped, the rounding to float, half its smallest step at least."""
+    assert np.array_equal(got[0].cpu().numpy(), want[0]), what
+    D = -np.expm1(want[2])
+    off = 2.0 ** -39 + 2.0 ** -45 * V * max(1.0, V / 2 ** 18)
+    tol = D * (2 * off + (152 * U if quick else 0.0)) / (1 - D) + U * np.abs(want[2]) + 2.0 ** -150
+    err = np.abs(got[2].double().cpu().numpy() - want[2])
+    assert (err <= tol).all(), (what, got[2].tolist(), want[2].tolist(), (err / tol).max())
+
+
+@pytest.mark.parametrize("mask", ["-inf", "lowest"])
+@pytest.mark.parametrize("V,ahead", [(2, 1), (60, 3), (900, 20), (524_300, 2)])
+def test_far_tokens_not_kept(T, V, ahead, mask):
+    """What is dropped is e^-40 to e^-100 of the rest, and the other tokens are masked: in short rows and in rows too long for a digest."""
+    rng, n = np.random.default_rng(V), 13 if V < 1_000 else 4
+    x = np.full((n, V), -np.inf if mask == "-inf" else np.finfo(np.float32).min, np.float32)
+    for r, z in enumerate(np.linspace(40, 100, n)):
+        order = rng.permutation(V)
+        x[r, order[:ahead]] = rng.normal(0, 1, ahead)
+        x[r, order[0]] = 2.5  # the largest, with which a nucleus of half begins
+        far = order[ahead:ahead + max(1, V // 3)]
+        x[r, far] = 2.5 - z - rng.random(len(far))
+    u = rng.random(n)
+    for params in (dict(top_k=ahead), dict(top_k=ahead + V // 6), dict(min_p=_f32(1e-7))):
+        _check_shares(T.tree_ens_sample(_dev(x), _dev(u), **params), O.sample(x, u, **params), V, False, (V, mask, params))
