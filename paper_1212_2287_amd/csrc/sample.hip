@@ -1417,6 +1417,12 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             const bool cut = uint64_t(p.top_k) < there; // otherwise what it cuts off is beyond the bins
             if (cut)
                 place = place_in_bins(x, a.V, r, least, false, uint64_t(p.top_k), s);
+            else if (p.top_k < a.V && p.fraction == kOne && wants_logp(a)) { // the share of what it cuts off there, which has no part in the token
+                uint64_t all = 0;
+                for_share(x, a.V, 0, 1, [&](float v, int) { all += v >= least && v > -INFINITY; });
+                if (uint64_t(p.top_k) < WideBlock::sum(all, s.block))
+                    last = WideBlock::place_of<false>(x, a.V, r, least, uint64_t(p.top_k), inside, s.mass, s.count, s.block);
+            }
             if (cut && p.fraction < kOne) { // what top_p is a share of has to be known
                 const bool read_again = place.fine || place.members > kMembers;
                 if (place.members > kMembers)

@@ -504,3 +504,23 @@ def test_far_tokens_not_kept(T, V, ahead, mask):
     u = rng.random(n)
     for params in (dict(top_k=ahead), dict(top_k=ahead + V // 6), dict(min_p=_f32(1e-7))):
         _check_shares(T.tree_ens_sample(_dev(x), _dev(u), **params), O.sample(x, u, **params), V, False, (V, mask, params))
+
+
+@pytest.mark.parametrize("n", [13, 300])
+@pytest.mark.parametrize("V", [5_000, 40_001])
+@pytest.mark.parametrize("first,last", [(65, 100)])
+def test_far_tokens_of_wide_rows(T, first, last, V, n):
+    """Rows of which more is kept than a list holds, and further tokens e^-`first` to e^-`last` of those, of which some are kept
+    as well: in rows that workgroups share and in more of them."""
+    rng = np.random.default_rng(V)
+    x = np.full((n, V), -np.inf, np.float32)
+    for r, z in enumerate(np.linspace(first, last, n)):
+        order = rng.permutation(V)
+        x[r, order[:1_000]] = rng.normal(0, 1, 1_000)
+        x[r, order[0]] = 2.5
+        x[r, order[1_000:3_000]] = 2.5 - z - rng.random(2_000)
+    u, some = rng.random(n), np.arange(0, n, max(1, n // 13))
+    for params in (dict(top_k=1_000), dict(top_k=1_700), dict(top_k=3_000), dict(top_k=3_001), dict(top_k=1_700, min_p=_f32(1e-30)),
+                   dict(min_p=_f32(1e-7)), dict(top_p=_f32(0.95)), dict(top_k=1_700, top_p=_f32(0.95))):
+        got = [g[_dev(some)] for g in T.tree_ens_sample(_dev(x), _dev(u), **params)]
+        _check_shares(got, O.sample(x[some], u[some], **params), V, False, (first, V, n, params))
