@@ -277,20 +277,8 @@ struct Row {
         : m(double(top)), scale(scale_), c(scale_ * kLog2e), far(-128.0 * __builtin_amdgcn_rcp(scale_)), shift(shift_) {}
     // The weight in units, not rounded. Masked logits are taken at `far`: 2^31 times e^-128 is still nothing to the smallest float.
     __device__ __forceinline__ double power(float x) const { return power_of(fmax(double(x) - m, far), c, shift); }
-    __device__ __forceinline__ double share(float x) const { return power_of(fmax(double(x) - m, far), c, 0); } // of the largest
     __device__ __forceinline__ uint64_t weight(float x) const { return whole_of(power(x)); }
     __device__ __forceinline__ uint64_t key_weight(uint32_t k) const { return weight(float_of(k)); }
-};
-
-// A sum of weights of at most 1, in whole numbers of 2^-51 for those of 2^-28 and more and of 2^-79 for others: exact in any order,
-// and in proportion to itself, as what is not kept has to be.
-struct Fine {
-    uint64_t high = 0, low = 0;
-    __device__ __forceinline__ void add(double w) {
-        high += w >= 0x1p-28 ? whole_of(w * 0x1p51) : 0;
-        low += w >= 0x1p-28 ? 0 : whole_of(w * 0x1p79);
-    }
-    __device__ __forceinline__ double units(int shift) const { return ldexp(double(high), shift - 51) + ldexp(double(low), shift - 79); }
 };
 
 // Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts.
@@ -367,7 +355,6 @@ template <int kT> struct Block {
             v += s.part[w];
         return v;
     }
-    static __device__ __forceinline__ Fine sum(Fine v, Shared &s) { return {sum(v.high, s), sum(v.low, s)}; }
     static __device__ __forceinline__ double sum(double v, Shared &s) {
         v = wave_sum(v);
         if constexpr (kWaves == 1)
@@ -488,6 +475,9 @@ template <int kT> struct Block {
 // ------------------------------------------------------------------------------------------------
 enum class Order { kLogits, kVocabulary };
 
+constexpr int kList = 512;     // candidates of pick_kernel; C took 124, 112 and 119 us with 256, 512 and 1,024
+constexpr int kMembers = 4096; // of a bin; one of E may have more than 2,048, and its row is then read once more, for 30 us
+
 // An entry as the order has it, the first one the largest, without the bits that all entries of lists have alike: those of indexes
 // beyond 2^kBits, and of keys those that T has not. The fewer steps a search takes: the two of 240 fp16
 // candidates, many of them equal, 4 us instead of up to 11, and C 105 us instead of 113.
@@ -580,6 +570,21 @@ template <int kT> struct List {
                 s.entry = list[i];
         __syncthreads();
         return s.entry;
+    }
+
+    // The weights of the entries below `end`, in units, added in whole numbers of 2^-51 of the largest of them: exact in any order, and
+    // in proportion to itself, as what is not kept has to be.
+    static __device__ __forceinline__ double below(const uint64_t *list, int n, uint64_t end, const Row &r, typename B::Shared &block) {
+        static_assert(kMembers <= 1 << 12, "sums are below 2^64");
+        float top = -INFINITY;
+        for (int i = threadIdx.x; i < n; i += kT)
+            top = list[i] < end ? larger(top, float_of(key_in(list[i]))) : top;
+        top = B::max(top, block);
+        const Row own(top, r.scale, 51);
+        uint64_t sum = 0;
+        for (int i = threadIdx.x; i < n; i += kT)
+            sum += list[i] < end ? own.key_weight(key_in(list[i])) : 0;
+        return double(B::sum(sum, block)) * 0x1p-51 * r.power(top);
     }
 };
 
@@ -824,8 +829,6 @@ __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Dige
 // ------------------------------------------------------------------------------------------------
 // the token of a row
 // ------------------------------------------------------------------------------------------------
-constexpr int kList = 512;     // candidates of pick_kernel; C took 124, 112 and 119 us with 256, 512 and 1,024
-constexpr int kMembers = 4096; // of a bin; one of E may have more than 2,048, and its row is then read once more, for 30 us
 constexpr int kFine = 1024;    // bins; E takes 75 us, and 81 with 2,048
 constexpr int kShared = 256;   // wide rows that workgroups may share
 
@@ -944,18 +947,12 @@ __device__ __forceinline__ bool pick_from_list(const Args &a, const Row &r, cons
                                          ordered<Order::kLogits, T>(entry_of(low, -1)), r, kept, s.find,
                                       s.block);
     }
-    Fine lost;
-    if (wants_logp(a) && end) {
-        for (int i = threadIdx.x; i < n; i += kPick)
-            if (s.list[i] < end)
-                lost.add(r.share(float_of(key_in(s.list[i]))));
-        lost = PickBlock::sum(lost, s.block);
-    }
+    const double lost = wants_logp(a) && end ? L::below(s.list, n, end, r, s.block) : 0.0;
     // sums are whole numbers: past the random share of them is to reach the next one
     const uint64_t token = L::find<Order::kVocabulary, T>(true, share_down(kept, p.at) + 1, s.list, n, end, ordered<Order::kVocabulary, T>(entry_of(0, 0)),
                                                               ordered<Order::kVocabulary, T>(entry_of(0, a.V - 1)), r, unused, s.find, s.block);
     if (threadIdx.x == 0)
-        s.out = {index_of(token), float_of(key_in(token)), double(kept), rest + lost.units(r.shift)};
+        s.out = {index_of(token), float_of(key_in(token)), double(kept), rest + lost};
     return true;
 }
 
@@ -995,18 +992,19 @@ __device__ __forceinline__ bool pick_from_few(const Args &a, const Row &r, const
         wait();
     }
     const uint64_t kept = wave_sum(keep ? w : 0), target = share_down(kept, p.at);
-    Fine lost;
+    double lost = 0.0; // as List::below has it
     if (wants_logp(a)) {
-        if (lane < n && !keep)
-            lost.add(r.share(float_of(key_in(mine))));
-        lost = {wave_sum(lost.high), wave_sum(lost.low)};
+        const bool is_lost = lane < n && !keep;
+        const float x = float_of(key_in(mine)), top = wave_max(is_lost ? x : -INFINITY);
+        const Row own(top, r.scale, 51);
+        lost = double(wave_sum(is_lost ? own.weight(x) : 0)) * 0x1p-51 * r.power(top);
     }
     uint64_t before = 0;
     for_entries(s, n, [&](const Weighed &o) {
         before += uint32_t(o.entry) > uint32_t(mine) ? o.weight : 0; // indices before this one's
     });
     if (keep && before <= target && target < before + w)
-        s.out = {index_of(mine), float_of(key_in(mine)), double(kept), rest + lost.units(r.shift)};
+        s.out = {index_of(mine), float_of(key_in(mine)), double(kept), rest + lost};
     return true;
 }
 
@@ -1558,7 +1556,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
             s.kept[tid] = left_at(kept_of + tid);
             s.lost[tid] = left_at(lost_of + tid);
         }
-        Fine below; // of the bin's entries that are not kept
+        double below = 0.0; // of the bin's entries that are not kept
         if (!exact) {
             const int n = w.members;
             if (shares > 1)
@@ -1571,15 +1569,15 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
                 const uint64_t e = s.list[i];
                 if (e >= end)
                     atomicAdd(reinterpret_cast<unsigned long long *>(&s.kept[index_of(e) / kPart]), (unsigned long long)r.key_weight(key_in(e)));
-                else
-                    below.add(r.share(float_of(key_in(e))));
             }
+            if (wants)
+                below = List<kWide>::below(s.list, n, end, r, s.block);
         }
         __syncthreads();
         uint64_t kept;
         const uint64_t mine = tid < g.parts ? s.kept[tid] : 0;
         const uint64_t sum = WideBlock::before(mine, kept, s.block);
-        const double dropped = WideBlock::sum(tid < g.parts ? s.lost[tid] : 0.0, s.block) + WideBlock::sum(below, s.block).units(a.shift);
+        const double dropped = WideBlock::sum(tid < g.parts ? s.lost[tid] : 0.0, s.block) + below;
         const uint64_t target = share_down(kept, p.at);
         if (sum <= target && target < sum + mine) {
             s.found = tid;

@@ -508,7 +508,7 @@ def test_far_tokens_not_kept(T, V, ahead, mask):
 
 @pytest.mark.parametrize("n", [13, 300])
 @pytest.mark.parametrize("V", [5_000, 40_001])
-@pytest.mark.parametrize("first,last", [(65, 100)])
+@pytest.mark.parametrize("first,last", [(40, 66), (65, 100)])
 def test_far_tokens_of_wide_rows(T, first, last, V, n):
     """Rows of which more is kept than a list holds, and further tokens e^-`first` to e^-`last` of those, of which some are kept
     as well: in rows that workgroups share and in more of them."""
@@ -524,3 +524,18 @@ def test_far_tokens_of_wide_rows(T, first, last, V, n):
                    dict(min_p=_f32(1e-7)), dict(top_p=_f32(0.95)), dict(top_k=1_700, top_p=_f32(0.95))):
         got = [g[_dev(some)] for g in T.tree_ens_sample(_dev(x), _dev(u), **params)]
         _check_shares(got, O.sample(x[some], u[some], **params), V, False, (first, V, n, params))
+
+
+@pytest.mark.parametrize("V,ahead,there", [(2_500, 1, 3), (2_500, 40, 60), (2_500, 90, 300), (40_001, 5, 400), (5_000, 600, 700), (140_000, 600, 3_000)])
+def test_far_tokens_of_a_list(T, V, ahead, there):
+    """The same of tokens that a list of candidates holds beside the kept ones, the first `ahead` of `there`, or a bin of more
+    candidates than a list holds beside the last ones kept, 20 further ones."""
+    rng, n = np.random.default_rng(V + there), 9
+    x = np.full((n, V), -np.inf, np.float32)
+    for r, z in enumerate(np.linspace(30, 62, n)):
+        order = rng.permutation(V)[:there]
+        x[r, order] = -z - np.arange(there) * (3.0 / there)
+        x[r, order[:ahead]] = 0.0
+    u = rng.random(n)
+    params = dict(min_p=_f32(1e-30), top_p=_f32(1 - 0.5 / ahead)) if there <= 512 else dict(top_k=ahead + 20)
+    _check_shares(T.tree_ens_sample(_dev(x), _dev(u), **params), O.sample(x, u, **params), V, True, (V, there))
