@@ -281,19 +281,17 @@ struct Row {
     __device__ __forceinline__ uint64_t key_weight(uint32_t k) const { return weight(float_of(k)); }
 };
 
-// Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts.
-// For scales of 2^-100 to 2^100.
+// Weights in single precision, of which a sum has the relative error of their own: the exponents' factor is taken in two parts, both of
+// them positive, so that distances beyond the floats and masked logits' count as 0. For scales of 2^-100 to 2^100.
 struct Quick {
-    float m, c, rest, far;
+    float m, c, rest;
     __device__ __forceinline__ Quick(float top, double scale) : m(top) {
         const double exact = scale * kLog2e;
-        c = float(exact);
+        c = float(exact * (1.0 - 0x1p-23)); // below it, however that is rounded
         rest = float(exact - double(c));
-        far = float(-200.0 * __builtin_amdgcn_rcp(exact));
     }
-    // Distances beyond `far`, masked logits' too, count as 0: a product of theirs alone may be infinite, with the sign of `rest`.
     __device__ __forceinline__ float power(float x) const {
-        const float d = fmaxf(x - m, far);
+        const float d = x - m;
         return __builtin_amdgcn_exp2f(fmaf(d, c, d * rest));
     }
 };
