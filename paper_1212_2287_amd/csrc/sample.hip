@@ -887,6 +887,7 @@ struct PickShared {
     uint64_t found_mass, found_left;
     float found_top;
     int found, n;
+    bool little;
     Outcome out;
     int ge[2][PickBlock::kWaves];
 };
@@ -1053,6 +1054,64 @@ __device__ __forceinline__ uint32_t key_reached(bool by_mass, uint64_t target, c
     return std::max(from, key_of(-INFINITY));
 }
 
+// What is left of a part's sum without `n` of its tokens is off by up to (n + 20) 2^-52 of the sum: half a unit of 2^-51 for each of the
+// tokens, and the 38 roundings on the way to any lane's share of the sum. Below this share of the sum that is more than 2^-19 of what is left.
+__device__ __forceinline__ double little_from(int n) { return double(n + 20) * 0x1p-33; }
+
+constexpr int kSegLoads = 4; // of a quarter of a wave, which takes a segment, on their way at a time
+
+// The j-th of kSegLoads vectors that the thread's quarter of a wave has from some[i] on of `many` segments, in steps of as many as there are
+// quarters: `at` receives where it begins, `first` its first element's index. Elements before `at`, or all beyond the last segment, are -inf.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::type read_seg(const T *x, int V, const uint16_t *some, int many, int i, int j, int &at, int &first) {
+    const int k = i + j / Part<T>::kSame * (kPick / 16);
+    const int seg = k < many ? some[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
+    at = k < many ? seg / kSegs * kPart + Part<T>::at(load + j % Part<T>::kSame, quarter * 16 + threadIdx.x % 16) : V;
+    return read_at(x, V, at, first);
+}
+template <typename T> constexpr int kSegStep = kPick / 16 * (kSegLoads / Part<T>::kSame);
+
+// The weights below `lowest`, in units, of the parts whose threads want them, which hold a token that is likeliest by far, or a few that
+// a mask leaves over. `some` has room for the list of their segments, whose order makes that of the sum.
+template <typename T>
+__device__ __forceinline__ double little_of(const T *x, int V, const uint32_t *keys, uint16_t *some, int segs, float lowest, const Row &r, bool wanted,
+                                            PickShared &s) {
+    const int tid = threadIdx.x;
+    s.listed[tid] = wanted;
+    __syncthreads();
+    const auto takes = [&](int i) { return s.listed[i / kSegs] && keys[i] > key_of(-INFINITY); };
+    uint64_t mine = 0, many;
+    for (int i = tid; i < segs; i += kPick)
+        mine += takes(i);
+    int to = int(PickBlock::before(mine, many, s.block));
+    for (int i = tid; i < segs; i += kPick)
+        if (takes(i))
+            some[to++] = uint16_t(i);
+    __syncthreads();
+    double sum = 0.0;
+    const auto counts = [&](float v) { return v < lowest && v > -INFINITY; };
+    for (int i = tid / 16; i < int(many); i += kSegStep<T>) {
+        int at, first;
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < kSegLoads; ++j) {
+            const auto q = read_seg(x, V, some, int(many), i, j, at, first);
+#pragma unroll
+            for (int k = 0; k < Part<T>::N; ++k)
+                any = any || counts(float(q[k]));
+        }
+        if (any)
+#pragma unroll 1
+            for (int j = 0; j < kSegLoads; ++j) { // once more, as there are as a rule none
+                const auto q = read_seg(x, V, some, int(many), i, j, at, first);
+#pragma unroll
+                for (int k = 0; k < Part<T>::N; ++k)
+                    sum += counts(float(q[k])) ? r.power(float(q[k])) : 0.0;
+            }
+    }
+    return PickBlock::sum(sum, s.block);
+}
+
 // A workgroup takes a row. Bound by the latency of its steps one after another (the digest, the search for the lowest segment, the
 // segments, the list's searches) and by fetching instructions that run once: 11.6 us for a row alone (A; lists of up to 64 by
 // pick_from_list too: 14.7), 5.4 where nothing is cut off (B), 25 for the 2,048 rows of D and in C. Three waves of a SIMD have the
@@ -1119,7 +1178,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             // segments that have a candidate, and their candidates
             __syncthreads();
             if (tid == 0)
-                s.found = s.n = 0;
+                s.found = s.n = s.little = 0;
             s.tops[tid] = top;
             s.listed[tid] = 0;
             __syncthreads();
@@ -1130,19 +1189,14 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             const int many = s.found <= kList ? s.found : 0; // each has a candidate: of more there is no list
             wide = s.found > kList;
             const float lowest = float_of(low);
-            constexpr int kLoads = 4; // of a quarter of a wave on their way at a time
-            for (int i = tid / 16; i < many; i += kPick / 16 * (kLoads / Part<T>::kSame)) {
-                typename Vec<T>::type q[kLoads];
-                int at[kLoads], first[kLoads];
+            for (int i = tid / 16; i < many; i += kSegStep<T>) {
+                typename Vec<T>::type q[kSegLoads];
+                int at[kSegLoads], first[kSegLoads];
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) {
-                    const int k = i + j / Part<T>::kSame * (kPick / 16);
-                    const int seg = k < many ? some[k] : 0, quarter = seg % 4, load = seg / 4 % 4 * Part<T>::kSame;
-                    at[j] = k < many ? seg / kSegs * kPart + Part<T>::at(load + j % Part<T>::kSame, quarter * 16 + tid % 16) : a.V;
-                    q[j] = read_at(x, a.V, at[j], first[j]);
-                }
+                for (int j = 0; j < kSegLoads; ++j)
+                    q[j] = read_seg(x, a.V, some, many, i, j, at[j], first[j]);
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) {
+                for (int j = 0; j < kSegLoads; ++j) {
                     unsigned hits = 0;
 #pragma unroll
                     for (int k = 0; k < Part<T>::N; ++k)
@@ -1161,8 +1215,7 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
             wide = wide || n > kList;
             double rest = 0.0;
             if (!wide && wants_logp(a)) {
-                // what a part has beside the list's tokens, whose weights are those that its sum was made of: what is left of
-                // the roundings of a sum counts as nothing
+                // what a part has beside the list's tokens, whose weights are those that its sum was made of
                 const bool quick = mass_of(a, row) == Mass::kQuick;
                 for (int i = tid; i < n; i += kPick) {
                     const int part = index_of(s.list[i]) / kPart;
@@ -1172,11 +1225,14 @@ __global__ void __launch_bounds__(kPick) __attribute__((amdgpu_waves_per_eu(3)))
                     atomicAdd(reinterpret_cast<unsigned long long *>(&s.listed[part]), (unsigned long long)whole_of(w));
                 }
                 __syncthreads();
-                if (tid < g.parts) {
-                    const double left = part_mass - ldexp(double(s.listed[tid]), a.shift - 51);
-                    rest = left > part_mass * 0x1p-44 ? left * factor : 0.0;
-                }
-                rest = PickBlock::sum(rest, s.block);
+                const double left = part_mass - ldexp(double(s.listed[tid]), a.shift - 51);
+                const bool little = s.listed[tid] != 0 && left < part_mass * little_from(n);
+                const double ample = little ? 0.0 : left * factor;
+                if (little)
+                    s.little = true;
+                rest = PickBlock::sum(ample, s.block);
+                if (s.little)
+                    rest += little_of(x, a.V, keys, some, segs, lowest, r, little, s);
             }
             if (!wide && n <= kWave)
                 wide = __syncthreads_or(tid < kWave && !pick_from_few(a, r, p, n, whole, total, rest, s));

@@ -539,3 +539,29 @@ def test_far_tokens_of_a_list(T, V, ahead, there):
     u = rng.random(n)
     params = dict(min_p=_f32(1e-30), top_p=_f32(1 - 0.5 / ahead)) if there <= 512 else dict(top_k=ahead + 20)
     _check_shares(T.tree_ens_sample(_dev(x), _dev(u), **params), O.sample(x, u, **params), V, True, (V, there))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2_049, 4_096, 40_001, 140_000])
+def test_far_tokens_beside_a_list(T, dtype, V):
+    """The same of tokens that share a part of the row with the kept ones and are in no list: some rows have them in every part,
+    some in one, and some none at all."""
+    rng, n = np.random.default_rng(V), 16
+    x = np.full((n, V), -np.inf)
+    for r, z in enumerate(np.linspace(12, 100, n)):
+        at = rng.integers(0, V)
+        if r % 4 == 1:
+            x[r] = -z - rng.random(V)
+        elif r % 4 == 2:
+            x[r, max(0, at - 300):at + 300] = -z
+        elif r % 4 == 3:
+            x[r, (at + 1) % V] = -z
+        x[r, at] = 0.0
+        if r % 3 == 0:
+            x[r, rng.integers(0, V, 20)] = -rng.random(20)
+    d = _dev(x).to(_torch_dtype(dtype))
+    x, u = d.double().cpu().numpy(), rng.random(n)
+    for params in (dict(top_k=1), dict(top_k=15), dict(min_p=_f32(1e-3)), dict(top_p=0.25), dict(top_p=_f32(0.99))):
+        got, want = T.tree_ens_sample(d, _dev(u), **params), O.sample(x, u, **params)
+        _check_shares(got, want, V, True, (dtype, V, params))
+        assert not got[2].cpu().numpy()[want[2] == 0.0].any()
