@@ -660,7 +660,7 @@ def tree_ens_sample(logits, uniform, scale=1.0, top_k=0, top_p=1.0, min_p=0.0, w
     lib = load_library()
     _keep, work, size = _workspace(lib, dev, "tree_ens_sample_workspace", code, n, v)
     _check(lib.tree_ens_sample(_stream_on(dev), _ptr(logits), code, n, v, stride, _ptr(uniform), float(scale_),
-           min(int(top_k_), 2**31 - 1), float(top_p_), float(min_p_), _ptr(row_scale), _ptr(row_top_k), _ptr(row_top_p),
+           max(-1, min(int(top_k_), 2**31 - 1)), float(top_p_), float(min_p_), _ptr(row_scale), _ptr(row_top_k), _ptr(row_top_p),
            _ptr(row_min_p), _ptr(tokens), _ptr(logp), _ptr(log_kept), work, size), "tree_ens_sample")
     return tokens, logp, log_kept
 

@@ -565,3 +565,13 @@ def test_far_tokens_beside_a_list(T, dtype, V):
         got, want = T.tree_ens_sample(d, _dev(u), **params), O.sample(x, u, **params)
         _check_shares(got, want, V, True, (dtype, V, params))
         assert not got[2].cpu().numpy()[want[2] == 0.0].any()
+
+
+def test_numbers_of_tokens_to_keep_that_are_no_int32(T):
+    d, _, u = _logits("f32", 3, 8)
+    u = _dev(u)
+    for top_k in (-2**31, -2**31 - 1, -2**32 + 5, -2**40):
+        with pytest.raises(T.TreeEnsError) as ei:
+            T.tree_ens_sample(d, u, top_k=top_k)
+        assert ei.value.code == T.TREE_ENS_E_ARG
+    assert (T.tree_ens_sample(d, u, top_k=2**32 + 1)[0] == T.tree_ens_sample(d, u)[0]).all()
