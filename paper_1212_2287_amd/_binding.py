@@ -700,8 +700,9 @@ def _address(values):
 
 
 def tree_ens_grad_norm(grads, norm=None, stream=None):
-    """The 2-norm of the elements of all tensors of ``grads`` together, such as ``[p.grad for p in parameters]``: a float32
-    scalar on their device (``norm``, if given). Types may be mixed; tensors are dense, in any order of their dimensions."""
+    """The 2-norm of the elements of all tensors of ``grads`` together, one or more of them, such as the ``p.grad`` of all
+    parameters that have one: a float32 scalar on their device (``norm``, if given). Types may be mixed; tensors are dense, in
+    any order of their dimensions."""
     import torch
     dev, grads, ptrs, counts, codes = _check_grads(grads)
     elsewhere = _elsewhere(dev, stream)
