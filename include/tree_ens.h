@@ -406,7 +406,8 @@ int tree_ens_policy_workspace(int64_t n_tokens, int64_t n_seqs, int64_t *bytes);
  * an order that is the row's own, so a row's token depends neither on the rows beside it nor on their number.
  * Weights below half of 2^-44 (of more from an n_vocab of 2^19 on: the sums stay below 2^63) count as 0 where
  * tokens are kept. Weights that top_k and min_p leave out are added in single precision, by themselves: the share
- * not kept is off by at most 2^-16 of itself, logp and log_kept by as much of that share, however small it is.
+ * not kept is off by at most 2^-16 of itself, logp and log_kept by as much of that share, however small it is
+ * (beside their rounding to float).
  */
 int tree_ens_sample(void *stream, const void *logits, int32_t dtype, int64_t n_tokens,
                     int64_t n_vocab, int64_t row_stride, const double *uniform, float scale,
