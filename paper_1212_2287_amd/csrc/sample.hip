@@ -758,10 +758,10 @@ struct Digest {
 };
 
 // A wave takes a part of a row: all its loads are on their way before the first is used, and the weights relative to the
-// part's own largest logit, so that no wave waits for another's. Bound by instructions, at 86% of what the card issues: 707 of a
-// wave, 22 a logit where weights are exact (B: 28.4 us for 66 MB, which 6.9 TB/s would take 9.5
-// for), 13 in single precision (D: 34 us for 131 MB; with exact weights 47, C 48 instead of 39.7). E, half of which 33 MB stay in
-// the caches: 11.3. Double-precision multiply-adds cost what single ones do here, and exp2 two of them. Kept weights are never from
+// part's own largest logit, so that no wave waits for another's. Bound by instructions: 705 of a wave, 22 a logit, where weights
+// are exact, which are 18.8 us of B's 28.4 if each takes four cycles of a SIMD, and longer as some of the 64-bit ones take more; its 66 MB would
+// take 9.5 us at 6.9 TB/s. 12 a logit in single precision (D: 33 us for 131 MB; with exact weights 47, C 48 instead of 38.5). E, half of
+// which 33 MB stay in the caches: 11.3. Double-precision multiply-adds cost what single ones do here, and exp2 two of them. Kept weights are never from
 // this sum alone where a list holds the tokens, so its roundings, in an order that is always the same, do not add up with theirs.
 template <typename T>
 __global__ void __launch_bounds__(256) scan_kernel(const T *logits, Args a, Digest g) {
@@ -1073,6 +1073,8 @@ template <typename T> constexpr int kSegStep = kPick / 16 * (kSegLoads / Part<T>
 
 // The weights below `lowest`, in units, of the parts whose threads want them, which hold a token that is likeliest by far, or a few that
 // a mask leaves over. `some` has room for the list of their segments, whose order makes that of the sum.
+// 64 rows of 128,000 bf16 with 100 tokens each that a mask leaves, in 50 parts or so, take 27 us under top_k 50; by a wave a
+// part 42, and 24 if what is left is taken as it is.
 template <typename T>
 __device__ __forceinline__ double little_of(const T *x, int V, const uint32_t *keys, uint16_t *some, int segs, float lowest, const Row &r, bool wanted,
                                             PickShared &s) {
@@ -1113,8 +1115,8 @@ __device__ __forceinline__ double little_of(const T *x, int V, const uint32_t *k
 }
 
 // A workgroup takes a row. Bound by the latency of its steps one after another (the digest, the search for the lowest segment, the
-// segments, the list's searches) and by fetching instructions that run once: 11.6 us for a row alone (A; lists of up to 64 by
-// pick_from_list too: 14.7), 5.4 where nothing is cut off (B), 25 for the 2,048 rows of D and in C. Three waves of a SIMD have the
+// segments, the list's searches) and by fetching instructions that run once: 11.5 us for a row alone (A; lists of up to 64 by
+// pick_from_list too: 14.7), 5.7 where nothing is cut off (B), 25 for the 2,048 rows of D and in C. Three waves of a SIMD have the
 // registers they need: D takes 67 us as a whole, 72 with four and 89 with five, 84 with 512 threads a row. Four loads of a quarter
 // of a wave at a time: 66.7, eight: 70.8.
 template <typename T>
@@ -1267,8 +1269,8 @@ constexpr int kWide = 512;
 constexpr int kMostShares = 16;
 using WideBlock = Block<kWide>;
 
-// Workgroups that share a row, so that a few wide rows have many and many have one each. 128,000 fp32 logits, top-p 0.98, take 46 us
-// for one row, 52 for 16, 76 for 64, 156 for 200 and 256 for 400; with a workgroup a row always 135, 139, 150, 166 and 255.
+// Workgroups that share a row, so that a few wide rows have many and many have one each. 128,000 fp32 logits, top-p 0.98, take 47 us
+// for one row, 49 for 16, 71 for 64, 151 for 200 and 253 for 400; with a workgroup a row always 135, 139, 147, 164 and 251.
 __device__ __forceinline__ int shares_of(unsigned wide, int parts) {
     return wide > kShared ? 1 : std::max(1, std::min(std::min(int(2 * kShared / wide), kMostShares), parts / 4));
 }
@@ -1288,7 +1290,7 @@ struct WideShared {
 };
 
 // The bin of a logit by its distance from the largest, which never decreases as logits do; kNoBin: beyond 63 in units of the
-// exponent, where neither what is kept nor what is not is felt any more. Halves, because the distance itself may be no float.
+// exponent, where a token has no part in what is kept. Halves, because the distance itself may be no float.
 // Fine ones are kFine to each of the others, exactly, since a power of two scales the distance.
 constexpr int kNoBin = kFine * kFine;
 struct Bins {
@@ -1522,7 +1524,7 @@ __global__ void __launch_bounds__(kWide) __attribute__((amdgpu_waves_per_eu(4)))
     }
 }
 
-// The kept weights of every part, the bin's entries, and the token. 25 us for the rows of C, 40 for those of E: the weights again,
+// The kept weights of every part, the bin's entries, and the token. 20 us for the rows of C, 36 for those of E: the weights again,
 // then a chain of latency in the last workgroup of every row (the bin's entries back from memory, the place among them, the part, the
 // token). With the registers of two or three waves of a SIMD C took 107 us instead of 111 and E 82 instead of 75. Four
 // loads at a time instead of a part's eight: E 74 instead of 76.
