@@ -26,6 +26,7 @@ Prints ONE JSON line on stdout (progress goes to stderr):
 from __future__ import annotations
 
 import argparse
+import gc
 import hashlib
 import json
 import os
@@ -141,19 +142,28 @@ def time_steps(model, Xd, out, steps, warmup):
     right before and after each scoring launch: the dominant kernel alone, without the coding
     pass, the split reduction or launch gaps) with their number per step. The launch events
     come from a second pass of the same steps: recording them between the kernels of a call
-    adds gaps to the stream, so the timed steps run without them."""
+    adds gaps to the stream, so the timed steps run without them. Python's collector is off
+    meanwhile: one pass over all that the imports made takes 35 to 55 ms, some 300 steps, and what
+    was allocated before decides whether it falls into them."""
     import torch
-    for _ in range(warmup):
-        model.predict(Xd, out)
-    torch.cuda.synchronize()
-    evs = [torch.cuda.Event(enable_timing=True) for _ in range(steps + 1)]
-    t0 = time.perf_counter()
-    evs[0].record()
-    for i in range(steps):
-        model.predict(Xd, out)
-        evs[i + 1].record()
-    torch.cuda.synchronize()
-    wall = time.perf_counter() - t0
+    collects = gc.isenabled()
+    gc.collect()
+    gc.disable()
+    try:
+        for _ in range(warmup):
+            model.predict(Xd, out)
+        torch.cuda.synchronize()
+        evs = [torch.cuda.Event(enable_timing=True) for _ in range(steps + 1)]
+        t0 = time.perf_counter()
+        evs[0].record()
+        for i in range(steps):
+            model.predict(Xd, out)
+            evs[i + 1].record()
+        torch.cuda.synchronize()
+        wall = time.perf_counter() - t0
+    finally:
+        if collects:
+            gc.enable()
     model.kernel_timing(True)
     for _ in range(steps):
         model.predict(Xd, out)

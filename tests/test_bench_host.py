@@ -98,3 +98,44 @@ def test_depths_above_terminals():
                 for c in (le[n], ri[n]):
                     walk(c, d + 1, k + (height(n) > 2))
         walk(0, 0, 0)
+
+
+def test_no_collection_in_the_timed_steps(monkeypatch):
+    """Python's collector is off from the warmup to the end of the timed steps, and back on afterwards, also after an error."""
+    import gc
+
+    import torch
+    seen, fails = [], []
+
+    class Event:
+        def __init__(self, enable_timing):
+            pass
+
+        def record(self):
+            seen.append(gc.isenabled())
+
+        def elapsed_time(self, other):
+            return 1.0
+
+    class Model:
+        def predict(self, x, out):
+            seen.append(gc.isenabled())
+            if fails:
+                raise RuntimeError
+
+        def kernel_timing(self, on):
+            pass
+
+        def kernel_time(self):
+            return 1.0, 1
+
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda: None)
+    assert gc.isenabled()
+    bench.time_steps(Model(), None, None, 4, 2)
+    timed = 2 + 1 + 2 * 4
+    assert not any(seen[:timed]) and all(seen[timed:]) and gc.isenabled()
+    fails.append(1)
+    with pytest.raises(RuntimeError):
+        bench.time_steps(Model(), None, None, 4, 2)
+    assert gc.isenabled()
